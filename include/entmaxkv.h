@@ -59,7 +59,9 @@ typedef enum {
   EKV_OP_DECODE_SPARSE = 2,
   EKV_OP_DECODE_FULL = 3,
   EKV_OP_DECODE_SPARSE_SOFTMAX = 4,
-  EKV_OP_SELECT_BOX_THRESHOLD = 5
+  EKV_OP_SELECT_BOX_THRESHOLD = 5,
+  EKV_OP_DECODE8_SPARSE_SOFTMAX = 6,
+  EKV_OP_DECODE8_FULL_SOFTMAX = 7
 } ekv_op;
 
 /* Problem description (host struct).  head_dim must be 128; page_size a multiple of 4 in [4,64];
@@ -292,6 +294,103 @@ ekv_status ekv_decode_sparse_softmax(const ekv_config* cfg, const void* q,
                                      const ekv_cache_view* cache, const int32_t* page_idx,
                                      const int32_t* n_sel, float* out, float* lse_sel,
                                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- the cache held in 8 bits ---------------------------------------------------------------------------------
+ * An extension (the paper keeps K and V in 16 bits): half the bytes of every stream and gather, and a context twice as
+ * long in the same memory.  Everything in front of the attention -- statistics, scores, selections -- works unchanged on
+ * the statistics that ekv_cache8_append writes; the ekv_decode8_* calls take the place of the decode calls.
+ *
+ * Pools are laid out as in ekv_cache_view with one byte per element: uint8 [n_phys][pool heads][P][d], OCP E4M3 codes (see
+ * box8).  Each page of each KV head has a scale, float32 [n_phys][pool heads], for K and for V: element = code * scale.
+ * Scales are powers of two between 2^-100 and 2^119 (normal numbers; what is written otherwise by a caller of its own gives
+ * undefined values, no undefined access).  A floating-point code gains nothing from a scale between two powers of two, and
+ * with these code * scale is exact in bf16 and float32: scores, thresholds and page statistics are those of the stored
+ * values.  cfg->kv_dtype is the type of q, of k_new / v_new and of the statistics.
+ * Range: n_phys_pages * pool heads * P < 2^30 (else EKV_ERR_UNSUPPORTED): 128 GiB a pool. */
+typedef struct {
+  void* k_pool;
+  void* v_pool;
+  float* k_scale;
+  float* v_scale;
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  int32_t n_phys_pages;
+} ekv_cache8_view;
+
+/* The new tokens of a step, packed: sequence b's tokens are rows start[b] .. start[b+1]-1 of k_new / v_new.
+ *   slots int64 [max_tokens]: physical page * P + token in the page; -1: the row goes nowhere
+ *   seq   int32 [max_tokens]: its sequence, pos int32 [max_tokens]: its position there (-1, -1 where slots is -1)
+ *   start int32 [B+1], n_mapped int32 [B] (tokens of the sequence that got slots: all of them or none): not read by
+ *         ekv_cache8_append and may be NULL there. */
+typedef struct {
+  int64_t* slots;
+  int32_t* seq;
+  int32_t* pos;
+  int32_t* start;
+  int32_t* n_mapped;
+  int32_t max_tokens;
+} ekv_token_map;
+
+/* Block tables and slots from request lengths.  n_new int32 [B] tokens (<= 0: none) join sequences of seq_lens tokens; pages
+ * are taken from the end of free_pages int32 [free_capacity], of which n_free int32 [1] are free, in the order of the sequences:
+ * the k-th new page of the call is free_pages[n_free - 1 - k].  A sequence is served whole or not at all: not if its rows end
+ * beyond max_tokens, if it would outgrow its row of the block table, or if the pages that it and the sequences before it
+ * need (those that fail for another reason need none) are more than there are; a sequence that needs no new page is served
+ * all the same.  start counts the rows of all sequences, served or not (where they are more than 2^30 together it stays there).
+ * block_table: entries of the new pages are written, the others are left.  new_lens int32 [B] = seq_lens + n_mapped, n_left
+ * int32 [1] = free pages that remain.  tokens->max_tokens entries of slots, seq and pos are written, -1 behind the last row.
+ * free_pages is not changed.  new_lens and n_left must not alias seq_lens and n_free: a program keeps two of each and
+ * swaps them.  One launch, no workspace.  Range: batch <= 4096, max_tokens < 2^30 (else EKV_ERR_UNSUPPORTED). */
+ekv_status ekv_map_tokens(const ekv_config* cfg, const int32_t* seq_lens, const int32_t* n_new, int32_t* block_table,
+                          const int32_t* free_pages, const int32_t* n_free, int32_t free_capacity,
+                          const ekv_token_map* tokens, int32_t* new_lens, int32_t* n_left, void* stream);
+
+/* Ended sequences give their pages back: for every b with release[b] != 0 (int32 [B]) the ceil(n_b/P) pages of its block-table
+ * row are appended to free_pages behind the n_free that are there, sequence by sequence in logical order, and new_lens[b] = 0;
+ * the other lengths are copied.  n_left = n_free + the pages returned.  Pages beyond free_capacity are dropped and n_left
+ * stops there.  A page that two rows name is returned twice.  Aliasing, range and launches as ekv_map_tokens. */
+ekv_status ekv_release_pages(const ekv_config* cfg, const int32_t* release, const int32_t* seq_lens,
+                             const int32_t* block_table, int32_t* free_pages, const int32_t* n_free,
+                             int32_t free_capacity, int32_t* new_lens, int32_t* n_left, void* stream);
+
+/* The quantising append: row i of k_new and v_new [max_tokens][Hkv][d] (kv_dtype; rows k_stride and v_stride elements apart,
+ * multiples of 8, so that parts of a fused projection need no copy) goes to slots[i] of the 8-bit pools.
+ * A run is a stretch of rows with consecutive slots of one page; a call may name a page in one run only (two runs on one page
+ * leave its scale and codes undefined).  For a run that begins at token t0 of its page, and each of K and V:
+ *   s_new = the least power of two in range with max |x| <= 448 s over the run's finite elements
+ *   s     = s_new if t0 == 0, else max(s_new, the page's scale); if that grows, the page's t0 older tokens are rounded again
+ *   code  = x / s to nearest, ties to even, at most +-448; NaN for what is no finite number
+ * Slots of the page behind the run are left as they were.  Slots outside the pool (-1) are skipped.
+ * stats may be NULL; if not, box and gauss (both) and, if given, box8 of page pos/P of sequence seq are written for the stored
+ * keys of tokens 0 .. t0 + run - 1, with the values that ekv_stats_build computes for a cache of kv_dtype that holds
+ * them.  tokens->seq and pos are only read then (pages outside the table are passed over).  seq_lens and block_table of
+ * `cache` are not read and may be NULL. */
+ekv_status ekv_cache8_append(const ekv_config* cfg, const ekv_cache8_view* cache, const ekv_stats_view* stats,
+                             const ekv_token_map* tokens, const void* k_new, int64_t k_stride, const void* v_new,
+                             int64_t v_stride, void* stream);
+
+/* ekv_decode_sparse, ekv_decode_sparse_group and ekv_decode_full over an 8-bit cache: same arguments, outputs, extras and
+ * workspaces (EKV_OP_DECODE_SPARSE, EKV_OP_DECODE_FULL). */
+ekv_status ekv_decode8_sparse(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache,
+                              const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau,
+                              int32_t* supp, const ekv_decode_extras* extras, void* workspace,
+                              size_t workspace_bytes, void* stream);
+ekv_status ekv_decode8_sparse_group(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache,
+                                    const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau,
+                                    int32_t* supp, const ekv_decode_extras* extras, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+ekv_status ekv_decode8_full(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, float* out,
+                            float* tau, int32_t* supp, const ekv_decode_extras* extras, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Softmax attention over an 8-bit cache: restricted to page lists per query head as ekv_decode_sparse_softmax, and over every
+ * page.  out f32 [B][Hq][d], lse f32 [B][Hq] (log-sum-exp of scale * q.k; -inf and a zero output for an empty row).
+ * Workspaces EKV_OP_DECODE8_SPARSE_SOFTMAX, EKV_OP_DECODE8_FULL_SOFTMAX. */
+ekv_status ekv_decode8_sparse_softmax(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache,
+                                      const int32_t* page_idx, const int32_t* n_sel, float* out, float* lse_sel,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+ekv_status ekv_decode8_full_softmax(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, float* out,
+                                    float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Measurement aid, no part of the method: reads n_pages pages of page_bytes bytes (4096 or 8192) of the device
  * buffer `base` and discards the data, four pages per wavefront.  Page i of the launch is page page_ids[i] of the

@@ -6,7 +6,7 @@ The shared library is loaded on first use and its absence is an error: there is 
 """
 import ctypes
 import os
-from ctypes import c_float, c_int32, c_size_t, c_void_p, POINTER, byref
+from ctypes import c_float, c_int32, c_int64, c_size_t, c_void_p, POINTER, byref
 
 import torch
 
@@ -18,15 +18,18 @@ EKV_F32, EKV_BF16 = 0, 1
 EKV_SCORE_BOX, EKV_SCORE_GAUSS, EKV_SCORE_BOTH, EKV_SCORE_GROUP_MAX, EKV_SCORE_BOX8 = 1, 2, 3, 4, 8
 EKV_STATIC_SCRATCH_BYTES = 32 << 20
 EKV_OP_SELECT_TOPK, EKV_OP_SELECT_GAUSS, EKV_OP_DECODE_SPARSE, EKV_OP_DECODE_FULL, \
-    EKV_OP_DECODE_SPARSE_SOFTMAX, EKV_OP_SELECT_BOX_THRESHOLD = range(6)
+    EKV_OP_DECODE_SPARSE_SOFTMAX, EKV_OP_SELECT_BOX_THRESHOLD, EKV_OP_DECODE8_SPARSE_SOFTMAX, \
+    EKV_OP_DECODE8_FULL_SOFTMAX = range(8)
 
 # every symbol the header declares
 EXPORTS = ["ekv_stats_build", "ekv_stats_append", "ekv_score_pages", "ekv_append_score_pages", "ekv_select_topk",
            "ekv_select_gauss",
            "ekv_select_box_threshold", "ekv_decode_sparse", "ekv_decode_sparse_group", "ekv_decode_full",
            "ekv_decode_sparse_softmax", "ekv_workspace_bytes", "ekv_probe_read", "ekv_decode_sparse_static",
-           "ekv_probe_handoff", "ekv_status_string", "ekv_last_hip_error", "ekv_version"]
-_STATUS_CALLS = EXPORTS[:15]      # entry points that return ekv_status
+           "ekv_probe_handoff", "ekv_map_tokens", "ekv_release_pages", "ekv_cache8_append", "ekv_decode8_sparse",
+           "ekv_decode8_sparse_group", "ekv_decode8_full", "ekv_decode8_sparse_softmax", "ekv_decode8_full_softmax",
+           "ekv_status_string", "ekv_last_hip_error", "ekv_version"]
+_STATUS_CALLS = EXPORTS[:23]      # entry points that return ekv_status
 
 
 class ekv_config(ctypes.Structure):
@@ -48,6 +51,16 @@ class ekv_decode_extras(ctypes.Structure):
     _fields_ = [("support_tokens", c_void_p), ("support_cap", c_int32), ("tau_ref", c_void_p),
                 ("kept_mass_ref", c_void_p), ("kept_supp_ref", c_void_p), ("lse", c_void_p),
                 ("tau_seed", c_void_p), ("solve_evals", c_void_p), ("score_pass_only", c_int32)]
+
+
+class ekv_cache8_view(ctypes.Structure):
+    _fields_ = [("k_pool", c_void_p), ("v_pool", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p),
+                ("block_table", c_void_p), ("seq_lens", c_void_p), ("n_phys_pages", c_int32)]
+
+
+class ekv_token_map(ctypes.Structure):
+    _fields_ = [("slots", c_void_p), ("seq", c_void_p), ("pos", c_void_p), ("start", c_void_p), ("n_mapped", c_void_p),
+                ("max_tokens", c_int32)]
 
 
 class EkvError(RuntimeError):
@@ -95,6 +108,21 @@ def load_library():
                                              c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
     lib.ekv_probe_read.argtypes = [c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p]
     lib.ekv_probe_handoff.argtypes = [c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_void_p]
+    lib.ekv_map_tokens.argtypes = [P(ekv_config), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int32,
+                                   P(ekv_token_map), c_void_p, c_void_p, c_void_p]
+    lib.ekv_release_pages.argtypes = [P(ekv_config), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int32,
+                                      c_void_p, c_void_p, c_void_p]
+    lib.ekv_cache8_append.argtypes = [P(ekv_config), P(ekv_cache8_view), P(ekv_stats_view), P(ekv_token_map), c_void_p,
+                                      c_int64, c_void_p, c_int64, c_void_p]
+    lib.ekv_decode8_sparse.argtypes = [P(ekv_config), c_void_p, P(ekv_cache8_view), c_void_p, c_void_p, c_void_p,
+                                       c_void_p, c_void_p, P(ekv_decode_extras), c_void_p, c_size_t, c_void_p]
+    lib.ekv_decode8_sparse_group.argtypes = lib.ekv_decode8_sparse.argtypes
+    lib.ekv_decode8_full.argtypes = [P(ekv_config), c_void_p, P(ekv_cache8_view), c_void_p, c_void_p, c_void_p,
+                                     P(ekv_decode_extras), c_void_p, c_size_t, c_void_p]
+    lib.ekv_decode8_sparse_softmax.argtypes = [P(ekv_config), c_void_p, P(ekv_cache8_view), c_void_p, c_void_p,
+                                               c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.ekv_decode8_full_softmax.argtypes = [P(ekv_config), c_void_p, P(ekv_cache8_view), c_void_p, c_void_p, c_void_p,
+                                             c_size_t, c_void_p]
     for name in _STATUS_CALLS:
         getattr(lib, name).restype = c_int32
     _lib = lib
@@ -148,6 +176,15 @@ def cache_view_heads(k_pool, v_pool, block_table, seq_lens, first_kv_head):
 
 def stats_view(box, gauss, box8=None):
     return ekv_stats_view(_ptr(box), _ptr(gauss), _ptr(box8))
+
+
+def cache8_view(k_pool, v_pool, k_scale, v_scale, block_table=None, seq_lens=None):
+    return ekv_cache8_view(_ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale), _ptr(block_table), _ptr(seq_lens),
+                           k_pool.shape[0])
+
+
+def token_map(slots, seq=None, pos=None, start=None, n_mapped=None):
+    return ekv_token_map(_ptr(slots), _ptr(seq), _ptr(pos), _ptr(start), _ptr(n_mapped), slots.numel())
 
 
 def decode_extras(support_tokens=None, tau_ref=None, kept_mass_ref=None, kept_supp_ref=None, lse=None,
@@ -248,3 +285,63 @@ def ekv_decode_sparse_static(cfg, q, cache, page_idx, n_sel, out, tau, supp, ext
 
 def ekv_probe_handoff(data, counter, out, n_workgroups, mode, stream=None):
     _check(load_library().ekv_probe_handoff(_ptr(data), _ptr(counter), _ptr(out), n_workgroups, mode, _stream(stream)))
+
+
+def ekv_map_tokens(cfg, seq_lens, n_new, block_table, free_pages, n_free, tokens, new_lens, n_left, stream=None):
+    _check(load_library().ekv_map_tokens(byref(cfg), _ptr(seq_lens), _ptr(n_new), _ptr(block_table), _ptr(free_pages),
+                                         _ptr(n_free), free_pages.numel(), byref(tokens), _ptr(new_lens), _ptr(n_left),
+                                         _stream(stream)))
+
+
+def ekv_release_pages(cfg, release, seq_lens, block_table, free_pages, n_free, new_lens, n_left, stream=None):
+    _check(load_library().ekv_release_pages(byref(cfg), _ptr(release), _ptr(seq_lens), _ptr(block_table),
+                                            _ptr(free_pages), _ptr(n_free), free_pages.numel(), _ptr(new_lens),
+                                            _ptr(n_left), _stream(stream)))
+
+
+def _rows(t):
+    """Pointer and row stride of [tokens][Hkv][d] rows that may be parts of longer ones."""
+    assert t.dim() == 3 and t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == t.shape[2]), \
+        "the heads of a row must follow each other"
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def ekv_cache8_append(cfg, cache, stats, tokens, k_new, v_new, stream=None):
+    assert k_new.shape[0] >= tokens.max_tokens and v_new.shape[0] >= tokens.max_tokens, "a row for every token of the map"
+    (k, ks), (v, vs) = _rows(k_new), _rows(v_new)
+    _check(load_library().ekv_cache8_append(byref(cfg), byref(cache), byref(stats) if stats is not None else None,
+                                            byref(tokens), k, ks, v, vs, _stream(stream)))
+
+
+def ekv_decode8_sparse(cfg, q, cache, page_idx, n_sel, out, tau, supp, workspace, extras=None, stream=None):
+    nbytes = workspace.numel() * workspace.element_size()
+    ex = byref(extras) if extras is not None else None
+    _check(load_library().ekv_decode8_sparse(byref(cfg), _ptr(q), byref(cache), _ptr(page_idx), _ptr(n_sel), _ptr(out),
+                                             _ptr(tau), _ptr(supp), ex, _ptr(workspace), nbytes, _stream(stream)))
+
+
+def ekv_decode8_sparse_group(cfg, q, cache, page_idx, n_sel, out, tau, supp, workspace, extras=None, stream=None):
+    nbytes = workspace.numel() * workspace.element_size()
+    ex = byref(extras) if extras is not None else None
+    _check(load_library().ekv_decode8_sparse_group(byref(cfg), _ptr(q), byref(cache), _ptr(page_idx), _ptr(n_sel),
+                                                   _ptr(out), _ptr(tau), _ptr(supp), ex, _ptr(workspace), nbytes,
+                                                   _stream(stream)))
+
+
+def ekv_decode8_full(cfg, q, cache, out, tau, supp, workspace, extras=None, stream=None):
+    nbytes = workspace.numel() * workspace.element_size()
+    ex = byref(extras) if extras is not None else None
+    _check(load_library().ekv_decode8_full(byref(cfg), _ptr(q), byref(cache), _ptr(out), _ptr(tau), _ptr(supp), ex,
+                                           _ptr(workspace), nbytes, _stream(stream)))
+
+
+def ekv_decode8_sparse_softmax(cfg, q, cache, page_idx, n_sel, out, lse_sel, workspace, stream=None):
+    nbytes = workspace.numel() * workspace.element_size()
+    _check(load_library().ekv_decode8_sparse_softmax(byref(cfg), _ptr(q), byref(cache), _ptr(page_idx), _ptr(n_sel),
+                                                     _ptr(out), _ptr(lse_sel), _ptr(workspace), nbytes, _stream(stream)))
+
+
+def ekv_decode8_full_softmax(cfg, q, cache, out, lse, workspace, stream=None):
+    nbytes = workspace.numel() * workspace.element_size()
+    _check(load_library().ekv_decode8_full_softmax(byref(cfg), _ptr(q), byref(cache), _ptr(out), _ptr(lse),
+                                                   _ptr(workspace), nbytes, _stream(stream)))

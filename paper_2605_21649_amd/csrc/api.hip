@@ -11,6 +11,7 @@ static thread_local int32_t g_last_hip_error = 0;
 
 static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 static inline bool ok_ptr(const void* p) { return p != nullptr && aligned16(p); }
+static inline bool ok_ptr8(const void* p) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
 static inline bool ok_ptr4(const void* p) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 static ekv_status make_dims(const ekv_config* cfg, Dims& dm) {
@@ -56,6 +57,16 @@ static ekv_status check_pool_rows(const ekv_cache_view* c, const Dims& dm) {
   return EKV_OK;
 }
 
+// Pools in 8 bits: rows are divided by the page size as numbers below 2^30 (page_div).
+static ekv_status check_cache8(const ekv_cache8_view* c, const Dims& dm, bool tables) {
+  if (c == nullptr || !ok_ptr(c->k_pool) || !ok_ptr(c->v_pool) || !ok_ptr4(c->k_scale) || !ok_ptr4(c->v_scale)) return EKV_ERR_INVALID_ARG;
+  if (c->n_phys_pages <= 0 || (tables && (!ok_ptr4(c->block_table) || !ok_ptr4(c->seq_lens)))) return EKV_ERR_INVALID_ARG;
+  if ((int64_t)c->n_phys_pages * dm.HkvPool * dm.P >= (int64_t)1 << 30) return EKV_ERR_UNSUPPORTED;
+  return EKV_OK;
+}
+
+constexpr int kMapBatchMost = 4096;      // sequences whose prefix sums a workgroup keeps in LDS
+
 static ekv_status finish(hipStream_t) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) { g_last_hip_error = (int32_t)e; return EKV_ERR_HIP; }
@@ -94,7 +105,7 @@ static ekv_status check_box8(const Dims& dm, const ekv_stats_view* stats, bool r
 
 extern "C" {
 
-int32_t ekv_version(void) { return 102; }
+int32_t ekv_version(void) { return 103; }
 
 int32_t ekv_last_hip_error(void) { return g_last_hip_error; }
 
@@ -125,6 +136,8 @@ ekv_status ekv_workspace_bytes(const ekv_config* cfg, int32_t op, size_t* bytes)
       if (!select_box_supported(dm)) return EKV_ERR_UNSUPPORTED;
       b = select_box_ws_bytes(dm);
       break;
+    case EKV_OP_DECODE8_SPARSE_SOFTMAX: b = softmax8_ws_bytes(dm, false); break;
+    case EKV_OP_DECODE8_FULL_SOFTMAX: b = softmax8_ws_bytes(dm, true); break;
     default: return EKV_ERR_INVALID_ARG;
   }
   *bytes = b;
@@ -252,15 +265,23 @@ ekv_status ekv_select_box_threshold(const ekv_config* cfg, const float* box, con
   return finish((hipStream_t)stream);
 }
 
+// c8: the cache is held in 8 bits (cache is null)
 static ekv_status decode_common(const ekv_config* cfg, bool dense, bool grouped, const void* q, const ekv_cache_view* cache,
                                 const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau,
                                 int32_t* supp, const ekv_decode_extras* extras, void* workspace,
-                                size_t workspace_bytes, void* stream) {
+                                size_t workspace_bytes, void* stream, const ekv_cache8_view* c8 = nullptr) {
   Dims dm;
   ekv_status s = make_dims(cfg, dm);
   if (s != EKV_OK) return s;
-  if ((s = check_cache(cache, true)) != EKV_OK) return s;
-  if ((s = check_pool_rows(cache, dm)) != EKV_OK) return s;
+  ekv_cache_view pools;
+  if (c8 != nullptr) {
+    if ((s = check_cache8(c8, dm, true)) != EKV_OK) return s;
+    pools = {c8->k_pool, c8->v_pool, c8->block_table, c8->seq_lens, c8->n_phys_pages};
+    cache = &pools;
+  } else {
+    if ((s = check_cache(cache, true)) != EKV_OK) return s;
+    if ((s = check_pool_rows(cache, dm)) != EKV_OK) return s;
+  }
   if (!ok_ptr(q) || !ok_ptr4(out) || !ok_ptr4(tau) || !ok_ptr4(supp)) return EKV_ERR_INVALID_ARG;
   if (!dense && (!ok_ptr4(page_idx) || !ok_ptr4(n_sel))) return EKV_ERR_INVALID_ARG;
   ekv_decode_extras ex;
@@ -274,7 +295,7 @@ static ekv_status decode_common(const ekv_config* cfg, bool dense, bool grouped,
   const size_t need = decode_ws_carve(dm, dense, nullptr, nullptr);
   if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < need) return EKV_ERR_WORKSPACE;
   decode_ws_carve(dm, dense, workspace, &ws);
-  launch_decode(dm, dense, grouped, q, *cache, page_idx, n_sel, out, tau, supp, ex, ws, (hipStream_t)stream);
+  launch_decode(dm, dense, grouped, q, *cache, page_idx, n_sel, out, tau, supp, ex, ws, (hipStream_t)stream, c8);
   return finish((hipStream_t)stream);
 }
 
@@ -357,6 +378,110 @@ ekv_status ekv_decode_sparse_softmax(const ekv_config* cfg, const void* q, const
     return EKV_ERR_WORKSPACE;
   launch_decode_sparse_softmax(dm, q, *cache, page_idx, n_sel, out, lse_sel, workspace, (hipStream_t)stream);
   return finish((hipStream_t)stream);
+}
+
+ekv_status ekv_map_tokens(const ekv_config* cfg, const int32_t* seq_lens, const int32_t* n_new, int32_t* block_table,
+                          const int32_t* free_pages, const int32_t* n_free, int32_t free_capacity,
+                          const ekv_token_map* tokens, int32_t* new_lens, int32_t* n_left, void* stream) {
+  Dims dm;
+  const ekv_status s = make_dims(cfg, dm);
+  if (s != EKV_OK) return s;
+  if (!ok_ptr4(seq_lens) || !ok_ptr4(n_new) || !ok_ptr4(block_table) || !ok_ptr4(free_pages) || !ok_ptr4(n_free) ||
+      !ok_ptr4(new_lens) || !ok_ptr4(n_left) || free_capacity <= 0 || tokens == nullptr)
+    return EKV_ERR_INVALID_ARG;
+  if (!ok_ptr8(tokens->slots) || !ok_ptr4(tokens->seq) || !ok_ptr4(tokens->pos) || !ok_ptr4(tokens->start) ||
+      !ok_ptr4(tokens->n_mapped) || tokens->max_tokens <= 0)
+    return EKV_ERR_INVALID_ARG;
+  if (new_lens == seq_lens || new_lens == n_new || n_left == n_free || free_pages == block_table) return EKV_ERR_INVALID_ARG;
+  if (dm.B > kMapBatchMost || tokens->max_tokens >= 1 << 30) return EKV_ERR_UNSUPPORTED;
+  launch_map_tokens(dm, seq_lens, n_new, block_table, free_pages, n_free, free_capacity, *tokens, new_lens, n_left,
+                    (hipStream_t)stream);
+  return finish((hipStream_t)stream);
+}
+
+ekv_status ekv_release_pages(const ekv_config* cfg, const int32_t* release, const int32_t* seq_lens,
+                             const int32_t* block_table, int32_t* free_pages, const int32_t* n_free,
+                             int32_t free_capacity, int32_t* new_lens, int32_t* n_left, void* stream) {
+  Dims dm;
+  const ekv_status s = make_dims(cfg, dm);
+  if (s != EKV_OK) return s;
+  if (!ok_ptr4(release) || !ok_ptr4(seq_lens) || !ok_ptr4(block_table) || !ok_ptr4(free_pages) || !ok_ptr4(n_free) ||
+      !ok_ptr4(new_lens) || !ok_ptr4(n_left) || free_capacity <= 0)
+    return EKV_ERR_INVALID_ARG;
+  if (new_lens == seq_lens || new_lens == release || n_left == n_free || free_pages == block_table) return EKV_ERR_INVALID_ARG;
+  if (dm.B > kMapBatchMost) return EKV_ERR_UNSUPPORTED;
+  launch_release_pages(dm, release, seq_lens, block_table, free_pages, n_free, free_capacity, new_lens, n_left,
+                       (hipStream_t)stream);
+  return finish((hipStream_t)stream);
+}
+
+ekv_status ekv_cache8_append(const ekv_config* cfg, const ekv_cache8_view* cache, const ekv_stats_view* stats,
+                             const ekv_token_map* tokens, const void* k_new, int64_t k_stride, const void* v_new,
+                             int64_t v_stride, void* stream) {
+  Dims dm;
+  ekv_status s = make_dims(cfg, dm);
+  if (s != EKV_OK) return s;
+  if ((s = check_cache8(cache, dm, false)) != EKV_OK) return s;
+  if (tokens == nullptr || !ok_ptr8(tokens->slots) || tokens->max_tokens <= 0 || !ok_ptr(k_new) || !ok_ptr(v_new))
+    return EKV_ERR_INVALID_ARG;
+  const int64_t row = (int64_t)dm.Hkv * cfg->head_dim;
+  if (k_stride < row || v_stride < row || k_stride % 8 != 0 || v_stride % 8 != 0) return EKV_ERR_INVALID_ARG;
+  if (stats != nullptr) {
+    if (!ok_ptr(stats->box) || !ok_ptr(stats->gauss) || !ok_ptr4(tokens->seq) || !ok_ptr4(tokens->pos)) return EKV_ERR_INVALID_ARG;
+    if ((s = check_box8(dm, stats, false)) != EKV_OK) return s;
+  }
+  if (tokens->max_tokens >= 1 << 30) return EKV_ERR_UNSUPPORTED;
+  launch_cache8_append(dm, *cache, stats, *tokens, k_new, k_stride, v_new, v_stride, (hipStream_t)stream);
+  return finish((hipStream_t)stream);
+}
+
+ekv_status ekv_decode8_sparse(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache,
+                              const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau, int32_t* supp,
+                              const ekv_decode_extras* extras, void* workspace, size_t workspace_bytes, void* stream) {
+  if (cache == nullptr) return EKV_ERR_INVALID_ARG;
+  return decode_common(cfg, false, false, q, nullptr, page_idx, n_sel, out, tau, supp, extras, workspace, workspace_bytes,
+                       stream, cache);
+}
+
+ekv_status ekv_decode8_sparse_group(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache,
+                                    const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau,
+                                    int32_t* supp, const ekv_decode_extras* extras, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  if (cache == nullptr) return EKV_ERR_INVALID_ARG;
+  return decode_common(cfg, false, true, q, nullptr, page_idx, n_sel, out, tau, supp, extras, workspace, workspace_bytes,
+                       stream, cache);
+}
+
+ekv_status ekv_decode8_full(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, float* out, float* tau,
+                            int32_t* supp, const ekv_decode_extras* extras, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  if (cache == nullptr) return EKV_ERR_INVALID_ARG;
+  return decode_common(cfg, true, false, q, nullptr, nullptr, nullptr, out, tau, supp, extras, workspace, workspace_bytes,
+                       stream, cache);
+}
+
+static ekv_status decode8_softmax_common(const ekv_config* cfg, bool dense, const void* q, const ekv_cache8_view* cache,
+                                         const int32_t* page_idx, const int32_t* n_sel, float* out, float* lse,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
+  Dims dm;
+  ekv_status s = make_dims(cfg, dm);
+  if (s != EKV_OK) return s;
+  if ((s = check_cache8(cache, dm, true)) != EKV_OK) return s;
+  if (!ok_ptr(q) || !ok_ptr4(out) || !ok_ptr4(lse) || (!dense && (!ok_ptr4(page_idx) || !ok_ptr4(n_sel)))) return EKV_ERR_INVALID_ARG;
+  if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < softmax8_ws_bytes(dm, dense)) return EKV_ERR_WORKSPACE;
+  launch_decode8_softmax(dm, dense, q, *cache, page_idx, n_sel, out, lse, workspace, (hipStream_t)stream);
+  return finish((hipStream_t)stream);
+}
+
+ekv_status ekv_decode8_sparse_softmax(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache,
+                                      const int32_t* page_idx, const int32_t* n_sel, float* out, float* lse_sel,
+                                      void* workspace, size_t workspace_bytes, void* stream) {
+  return decode8_softmax_common(cfg, false, q, cache, page_idx, n_sel, out, lse_sel, workspace, workspace_bytes, stream);
+}
+
+ekv_status ekv_decode8_full_softmax(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, float* out,
+                                    float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  return decode8_softmax_common(cfg, true, q, cache, nullptr, nullptr, out, lse, workspace, workspace_bytes, stream);
 }
 
 ekv_status ekv_probe_read(const void* base, const int32_t* page_ids, const int32_t* lookup, int32_t n_pages,

@@ -12,7 +12,7 @@
 //           p_j > 0.
 // Short per-head lists take both passes in one launch with the scores in LDS (decode_row_kernel).
 // All reductions have a fixed order, so results are bit-reproducible.
-#include "ekv_scores.h"
+#include "ekv_attn8.h"
 
 namespace ekv {
 
@@ -869,6 +869,7 @@ struct SolveArgs {
   int HkvPool;
   // per-row overflow list in the workspace for candidate lists beyond the LDS list (null / 0 when rows cannot have one)
   float* spill_u; int32_t* spill_pos; int spill_cap;
+  const float* v_scale; PageDiv page_div;      // 8-bit caches only
 };
 
 // V row index (phys*Hkv + hkv)*P + tok of candidate position `pos`.
@@ -878,6 +879,12 @@ __device__ __forceinline__ uint32_t v_row_of(const SolveArgs& A, int b, int bh, 
   const int lp = DENSE ? slot : clampi(A.page_idx[(size_t)bh * A.cap + slot], 0, A.Mmax - 1);
   const int phys = clampi(A.block_table[(size_t)b * A.Mmax + lp], 0, A.n_phys - 1);
   return (uint32_t)((phys * A.HkvPool + hkv) * A.P + tok);
+}
+// Weight of a value row as loaded: an 8-bit cache's rows are codes, whose page has a scale (a power of two: exact).
+template <typename T>
+__device__ __forceinline__ float row_weight(const SolveArgs& A, uint32_t row, float p) {
+  if constexpr (sizeof(T) == 1) return p * A.v_scale[page_div(row, A.page_div)];
+  else return p;
 }
 template <bool DENSE>
 __device__ __forceinline__ int token_of(const SolveArgs& A, int bh, int pos) {
@@ -916,7 +923,7 @@ __device__ __forceinline__ void sum_partials(const SH& sh, float* __restrict__ o
 // slots x 16 lanes, eight independent 16-byte loads in flight per lane (clamped entries carry weight 0).  A row
 // slot adds its entries in ascending order.
 template <typename T, typename SH>
-__device__ __forceinline__ void gather_support(const T* __restrict__ v_pool, const SH& sh, int tot, float (&acc)[8]) {
+__device__ __forceinline__ void gather_support(const SolveArgs& A, const T* __restrict__ v_pool, const SH& sh, int tot, float (&acc)[8]) {
   const int rs = threadIdx.x >> 4, c = threadIdx.x & 15;
   constexpr int kSlots = 4 * SH::kWaves;
   for (int e0 = 0; e0 < tot; e0 += 8 * kSlots) {
@@ -925,7 +932,7 @@ __device__ __forceinline__ void gather_support(const T* __restrict__ v_pool, con
     for (int j = 0; j < 8; ++j) {
       const int e = e0 + kSlots * j + rs;
       const int ec = min(e, tot - 1);
-      pw[j] = e < tot ? sh.list_u[ec] : 0.f;
+      pw[j] = row_weight<T>(A, sh.list_row[ec], e < tot ? sh.list_u[ec] : 0.f);
       load_raw8(v_pool + (size_t)sh.list_row[ec] * kD + 8 * c, vr[j]);
     }
 #pragma unroll
@@ -1046,7 +1053,7 @@ __device__ __forceinline__ void finish_row_wave(const SolveArgs& A, const RowRef
     for (int j = 0; j < 8; ++j) {
       const int e = e0 + 4 * j + rs;
       const int ec = min(e, n_sup - 1);                              // clamped: loads stay unconditional
-      pw[j] = e < n_sup ? lu[ec] : 0.f;
+      pw[j] = row_weight<T>(A, lr[ec], e < n_sup ? lu[ec] : 0.f);
       load_raw8(v_pool + (size_t)lr[ec] * kD + 8 * c, vr[j]);
     }
 #pragma unroll
@@ -1390,7 +1397,7 @@ __device__ __forceinline__ void finish_row_block(const SolveArgs& A, const RowRe
     for (int q = 0; q < 8; ++q) acc[q] = 0.f;
     uint32_t left = full;
     int at = 0;
-    constexpr int U = sizeof(T) == 2 ? 16 : 8;
+    constexpr int U = sizeof(T) <= 2 ? 16 : 8;
     while (left != 0) {                                                 // wave-uniform, as everything about the steps
       Raw8<T> vr[U]; float pw[U];
       int ends[U];                                                      // the segment that ends with the step, or -1
@@ -1399,8 +1406,9 @@ __device__ __forceinline__ void finish_row_block(const SolveArgs& A, const RowRe
         const int i = left != 0 ? __builtin_ctz(left) : 0;
         const bool real = left != 0;
         const uint2 e = seg0[i * SH::kSegCap + min(at + rs, SH::kSegCap - 1)];
-        pw[j] = real ? __uint_as_float(e.x) : 0.f;
-        load_raw8(v_pool + (size_t)(real ? e.y : row[0]) * kD + 8 * c, vr[j]);
+        const uint32_t vrow = real ? e.y : row[0];
+        pw[j] = row_weight<T>(A, vrow, real ? __uint_as_float(e.x) : 0.f);
+        load_raw8(v_pool + (size_t)vrow * kD + 8 * c, vr[j]);
         at += 4;
         ends[j] = -1;
         if (real && at >= __builtin_amdgcn_readlane(ns_of, i)) { ends[j] = i; left &= left - 1; at = 0; }
@@ -1435,7 +1443,7 @@ __device__ __forceinline__ void finish_row_block(const SolveArgs& A, const RowRe
       for (int e0 = 0; e0 < ns; e0 += 64) {
         const uint32_t row_now = row;
         row = v_row_of<DENSE>(A, R.b, R.lrow, R.hkv, (int)seg[min(e0 + 64 + lane, ns - 1)].y);
-        const float p_now = e0 + lane < ns ? __uint_as_float(seg[e0 + lane].x) : 0.f;
+        const float p_now = row_weight<T>(A, row_now, e0 + lane < ns ? __uint_as_float(seg[e0 + lane].x) : 0.f);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           Raw8<T> vr[8]; float pw[8];
@@ -1893,7 +1901,7 @@ __global__ __launch_bounds__(64 * SH::kWaves) __attribute__((aligned(4096))) voi
     float acc[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = 0.f;
-    gather_support<T>(v_pool, sh, n_sup, acc);
+    gather_support<T>(A, v_pool, sh, n_sup, acc);
     __syncthreads();
     store_partial(acc, sh, w);
     sum_partials<NW>(sh, out);
@@ -1947,7 +1955,7 @@ __global__ __launch_bounds__(64 * SH::kWaves) __attribute__((aligned(4096))) voi
           off += __popcll(mk);
         }
         __syncthreads();
-        gather_support<T>(v_pool, sh, tot, acc);
+        gather_support<T>(A, v_pool, sh, tot, acc);
         if (A.ex.support_tokens != nullptr) {
           int32_t* dst = A.ex.support_tokens + (size_t)bh * A.ex.support_cap;
           for (int e = tid; e < tot && n_out + e < A.ex.support_cap; e += NT)
@@ -2299,6 +2307,12 @@ static void launch_rows(const Dims& dm, const ScoreArgs& sa, const SolveArgs& so
   else launch_rows_T<bf16_t, 0>(dm, sa, so, st);
 }
 
+void launch_unit_prefix(int mode, const ScoreArgs& sa, int32_t* pre_out, hipStream_t st) {
+  if (mode == kPerHead) hipLaunchKernelGGL((unit_prefix_kernel<kPerHead>), dim3(1), dim3(1024), 0, st, sa, pre_out);
+  else if (mode == kAllPages) hipLaunchKernelGGL((unit_prefix_kernel<kAllPages>), dim3(1), dim3(1024), 0, st, sa, pre_out);
+  else hipLaunchKernelGGL((unit_prefix_kernel<kGroupList>), dim3(1), dim3(1024), 0, st, sa, pre_out);
+}
+
 size_t decode_ws_carve(const Dims& dm, bool dense, void* base, DecodeWorkspace* ws) {
   const size_t slots = dense ? dm.Mmax : dm.cap;
   const size_t rows = (size_t)dm.B * dm.Hq;
@@ -2339,7 +2353,7 @@ size_t decode_ws_carve(const Dims& dm, bool dense, void* base, DecodeWorkspace* 
 
 void launch_decode(const Dims& dm, bool dense, bool grouped, const void* q, const ekv_cache_view& c,
                    const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau, int32_t* supp,
-                   const ekv_decode_extras& ex, const DecodeWorkspace& ws, hipStream_t st) {
+                   const ekv_decode_extras& ex, const DecodeWorkspace& ws, hipStream_t st, const ekv_cache8_view* c8) {
   ScoreArgs sa{q, c.k_pool, c.block_table, c.seq_lens, page_idx, n_sel, ws.z, ws.pmax,
                dm.Hq, dm.Hkv, dm.P, dm.Mmax, dm.cap, ws.n_chunks_max, c.n_phys_pages, ws.zstride, dm.a * dm.scale,
                dm.HkvPool, 0, nullptr, 1};
@@ -2355,6 +2369,26 @@ void launch_decode(const Dims& dm, bool dense, bool grouped, const void* q, cons
                 ws.zstride, dm.beta, dm.ibeta};
   dim3 fgrid(ws.n_slices_max, dm.B * dm.Hq), fblock(kFilterThreads);
   const int rows = dm.B * dm.Hq;
+  if (c8 != nullptr) {
+    so.v_scale = c8->v_scale;
+    so.page_div = make_page_div(dm.P);
+    const int mode = dense ? kAllPages : grouped && dm.G > 1 ? kGroupList : kPerHead;
+    sa.U = mode == kPerHead ? dm.B * dm.Hq : dm.B * dm.Hkv;
+    launch_scores8(dm, mode, sa, c8->k_scale, ws.unit_pre, st);
+    if (ex.score_pass_only) return;
+    if (ws.fcount != nullptr) {
+      if (dense) {
+        hipLaunchKernelGGL((filter_level_kernel<true>), dim3(rows), fblock, 0, st, fa);
+        hipLaunchKernelGGL((filter_compact_kernel<true>), fgrid, fblock, 0, st, fa);
+      } else {
+        hipLaunchKernelGGL((filter_level_kernel<false>), dim3(rows), fblock, 0, st, fa);
+        hipLaunchKernelGGL((filter_compact_kernel<false>), fgrid, fblock, 0, st, fa);
+      }
+    }
+    if (dense) launch_solve<e4m3_t, true>(rows, ws.n_chunks_max, so, st);
+    else launch_solve<e4m3_t, false>(rows, ws.n_chunks_max, so, st);
+    return;
+  }
   if (dense) {
     sa.U = dm.B * dm.Hkv;
     switch (dm.G) {

@@ -1,0 +1,387 @@
+// Softmax attention of one query token per sequence over the 8-bit cache: every page, or a page list per query head.
+//
+// One pass over K and V with the running maximum and sum; scores and weighted values both go through the matrix cores
+// (ekv_attn8.h has the scores' tiles).  Steps of 32 tokens, two tiles: lane (c, g) then holds the scores of head c % G for tokens
+// 4g..4g+3 of either tile, and that is the layout in which the next product wants its rows (row c, eight tokens of group g),
+// so the weights go from one product to the next without leaving the lane.  Float32 weights are three bf16 terms that
+// sum to them exactly (8 + 8 + 8 bits); the columns that repeat the heads hold them: copy 0 of the heads contributes the first
+// term, copy 1 the second, copy 2 the third, as rows of one product (with eight heads there are two copies and a second
+// product).  Values are 8 bytes of each token's row per lane, transposed in pairs of tokens by byte permutes and widened with
+// their page's scale (exact), so that sums are float32 sums of exact products.
+// The maximum only has to keep exp in range: it is brought up to date, with the exchange and the rescaling that takes, when a
+// score passes it by more than 2^kSlack, not at every step.
+#include "ekv_attn8.h"
+
+namespace ekv {
+
+constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / 64;
+constexpr int kStep = 32;                        // tokens per step of a wavefront
+constexpr int kRec = kD + 2;                     // floats per head of a partial result: o[128], maximum, sum
+constexpr float kSlack = 8.f;                    // weights stay below 2^8
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+
+struct Attn8Args {
+  ScoreArgs s;                                   // q, lists, lengths, sizes; k_pool: codes; zscale: scale * log2(e)
+  const float* k_scale; const float* v_scale; const e4m3_t* v_pool;
+  float* out; float* lse;
+  float* part;                                   // [grid + U][G][kRec]
+  int32_t* pre;                                  // [U + 1] steps before a unit, for the join
+  PageDiv page_div;
+};
+
+template <bool DENSE>
+__device__ __forceinline__ int unit_steps(const ScoreArgs& A, int u) {
+  if (DENSE) return (int)(((int64_t)clampi(A.seq_lens[u / A.Hkv], 0, A.Mmax * A.P) + kStep - 1) / kStep);
+  return (int)(((int64_t)clampi(A.n_sel[u], 0, A.cap) * A.P + kStep - 1) / kStep);
+}
+
+template <bool DENSE>
+__global__ __launch_bounds__(1024) void attn8_prefix_kernel(const Attn8Args A) {
+  __shared__ int wsum[16];
+  block_exclusive_prefix<1024>(A.s.U, [&](int u) { return unit_steps<DENSE>(A.s, u); }, A.pre, wsum);
+}
+
+// A step's data as loaded.  K: token c of either tile; V: channels 8c..8c+7 of tokens 4g..4g+3 of either tile.
+struct Step8 {
+  KeyTile k[2];
+  uint2 v[8];
+  float ks[2], vs[2];
+  int left[2];                                   // valid tokens from the lane's first on (4 or more: all)
+};
+
+template <typename T, int G, bool DENSE, bool TILED>
+__global__ __launch_bounds__(kAttnThreads) void attn8_kernel(const Attn8Args AA) {
+  const ScoreArgs& A = AA.s;
+  extern __shared__ int pre_lds[];
+  __shared__ int wsum[kAttnWaves];
+  __shared__ float s_o[kAttnWaves][G][kD];
+  __shared__ float s_m[kAttnWaves][G], s_l[kAttnWaves][G];
+  const int P = A.P, lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+  const e4m3_t* k_pool = (const e4m3_t*)A.k_pool + 16 * g;
+  const e4m3_t* v_pool = AA.v_pool + 8 * c;
+  const bool in_lds = A.pre_g == nullptr;
+  int first_unit, begin, end;
+  auto range = [&](auto pre) {                   // this workgroup's steps
+    const int total = uniform(pre[A.U]), W = gridDim.x, i = blockIdx.x, per = total / W, rem = total - per * W;
+    begin = i * per + min(i, rem);
+    end = begin + per + (i < rem ? 1 : 0);
+    first_unit = wave_last_at_most(pre, A.U, begin);
+  };
+  if (in_lds) {
+    block_exclusive_prefix<kAttnThreads>(A.U, [&](int u) { return unit_steps<DENSE>(A, u); }, pre_lds, wsum);
+    range((const int*)pre_lds);
+    if (blockIdx.x == 0)
+      for (int u = threadIdx.x; u <= A.U; u += kAttnThreads) AA.pre[u] = pre_lds[u];
+  } else {
+    range(A.pre_g);
+  }
+  const int last = (DENSE ? A.Mmax : A.cap) - 1;
+  const uint32_t take1 = c / G >= 1 ? 0xffff0000u : 0u, take2 = c / G >= 2 ? 0xffff0000u : 0u;
+  const uint32_t keep = c / G < 3 ? ~0u : 0u, first = c / G == 0 ? ~0u : 0u;
+
+  int unit = first_unit;
+  for (int at = begin; at < end;) {
+    int u_begin = 0, u_end = 0;
+    auto bounds = [&](auto pre) {
+      while (at >= uniform(pre[unit + 1])) ++unit;
+      u_begin = uniform(pre[unit]); u_end = uniform(pre[unit + 1]);
+    };
+    if (in_lds) bounds((const int*)pre_lds); else bounds(A.pre_g);
+    const int seg_end = min(end, u_end), n_steps = seg_end - at;
+    const int b = DENSE ? unit / A.Hkv : unit / A.Hq, hkv = DENSE ? unit % A.Hkv : unit % A.Hq / (A.Hq / A.Hkv);
+    const size_t row0 = DENSE ? (size_t)b * A.Hq + hkv * G : (size_t)unit;
+    const int n = clampi(uniform_load(A.seq_lens + b), 0, A.Mmax * P);
+    const int n_pos = DENSE ? n : clampi(uniform_load(A.n_sel + unit), 0, A.cap) * P;      // positions of the unit
+    // a quarter of the segment for each wavefront
+    const int st0 = at - u_begin + n_steps * w / kAttnWaves, st1 = at - u_begin + n_steps * (w + 1) / kAttnWaves;
+
+    float m = -INFINITY, l = 0.f;
+    f32x4_t acc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    if (st0 < st1) {
+      Query8<T, G> qb;
+      qb.load((const T*)A.q + row0 * kD);
+      // page slots [slot_base, slot_base + 64), one per lane
+      int slot_base = -64, l_lp = 0, l_page = 0;
+      float l_ks = 0.f, l_vs = 0.f;
+      auto look_up = [&](int pos) {
+        slot_base = uniform((int)page_div((uint32_t)pos, AA.page_div));
+        const int slot = min(slot_base + lane, last);
+        l_lp = clampi(DENSE ? slot : A.page_idx[(size_t)unit * A.cap + slot], 0, A.Mmax - 1);
+        const int phys = clampi(A.block_table[(size_t)b * A.Mmax + l_lp], 0, A.n_phys - 1);
+        l_page = phys * A.HkvPool + hkv;
+        l_ks = AA.k_scale[l_page];
+        l_vs = AA.v_scale[l_page];
+      };
+      auto request = [&](int st, Step8& x) {
+        const int p0 = st * kStep;
+        if ((int)page_div((uint32_t)(p0 + kStep - 1), AA.page_div) >= slot_base + 64) look_up(p0);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if constexpr (TILED) {
+            const int slot = uniform((int)page_div((uint32_t)(p0 + 16 * t), AA.page_div)), tok = p0 + 16 * t - slot * P, sl = slot - slot_base;
+            const int page = __builtin_amdgcn_readlane(l_page, sl);
+            x.ks[t] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l_ks), sl));
+            x.vs[t] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l_vs), sl));
+            const size_t row = (size_t)page * P + tok;
+            load_keys<false>(k_pool + (row + c) * kD, x.k[t]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x.v[4 * t + j] = *reinterpret_cast<const uint2*>(v_pool + (row + 4 * g + j) * kD);
+            const int lp = __builtin_amdgcn_readlane(l_lp, sl);
+            x.left[t] = p0 + 16 * t < n_pos ? n - (lp * P + tok) - 4 * g : 0;
+          } else {
+            const int pk = p0 + 16 * t + c, pv = p0 + 16 * t + 4 * g;
+            const int sk = (int)page_div((uint32_t)pk, AA.page_div), sv = (int)page_div((uint32_t)pv, AA.page_div);
+            const int page_k = __shfl(l_page, sk - slot_base), page_v = __shfl(l_page, sv - slot_base);
+            x.ks[t] = __shfl(l_ks, sk - slot_base);
+            x.vs[t] = __shfl(l_vs, sv - slot_base);
+            load_keys<false>(k_pool + ((size_t)page_k * P + (pk - sk * P)) * kD, x.k[t]);
+            const size_t row = (size_t)page_v * P + (pv - sv * P);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x.v[4 * t + j] = *reinterpret_cast<const uint2*>(v_pool + (row + j) * kD);
+            const int lp = __shfl(l_lp, sv - slot_base);
+            x.left[t] = pv < n_pos ? n - (lp * P + (pv - sv * P)) : 0;
+          }
+        }
+      };
+      auto consume = [&](Step8& x) {
+        f32x4_t z[2];
+        float top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          z[t] = tile_scores<T, G>(x.k[t], x.ks[t], qb);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            z[t][r] = r < x.left[t] ? A.zscale * z[t][r] : -INFINITY;
+            top = fmaxf(top, z[t][r]);
+          }
+        }
+        if (__any(x.left[0] < 4 || x.left[1] < 4)) {           // what a page holds behind the last token counts for nothing, NaN too
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j % 4 >= x.left[j / 4]) x.v[j] = make_uint2(0u, 0u);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            if (x.left[t] <= 0) x.vs[t] = 1.f;               // ... nor does the scale of a page that nobody has
+        }
+        if (__any(top > m + kSlack)) {
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float m_new = fmaxf(m, top);
+          const float f = m_new > -INFINITY ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
+          m = m_new;
+          l *= f;
+          f32x4_t fr;                                        // the factors of result rows 4g..4g+3
+#pragma unroll
+          for (int r = 0; r < 4; ++r) fr[r] = __shfl(f, 4 * g + r);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][r] *= fr[r];
+          }
+        }
+        const float m_use = m > -INFINITY ? m : 0.f;
+        u32x4_t pa, pb;                                      // rows of the second product: this lane's term of its head's weights
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+          for (int r = 0; r < 4; r += 2) {
+            uint32_t bits[2], low[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float p = __builtin_amdgcn_exp2f(z[t][r + e] - m_use);
+              l += p;
+              float y = p - __uint_as_float(__float_as_uint(p) & take1);
+              if constexpr (G == 8) {
+                const float rest = p - __uint_as_float(__float_as_uint(p) & 0xffff0000u);
+                low[e] = __float_as_uint(rest - __uint_as_float(__float_as_uint(rest) & 0xffff0000u));
+              } else {
+                y -= __uint_as_float(__float_as_uint(y) & take2);
+              }
+              bits[e] = __float_as_uint(y) & keep;
+            }
+            pa[2 * t + r / 2] = __builtin_amdgcn_perm(bits[1], bits[0], 0x07060302u);
+            if constexpr (G == 8) pb[2 * t + r / 2] = __builtin_amdgcn_perm(low[1], low[0], 0x07060302u) & first;
+          }
+        }
+        // channel 8c + i of tokens 0..7 of the lane, i = 0..7: pairs of tokens side by side, then widened
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t lo[4], hi[4];                             // (token 2j, 2j + 1) of channels 0, 1 and of channels 2, 3 of the half
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t a = half ? x.v[2 * j].y : x.v[2 * j].x, d = half ? x.v[2 * j + 1].y : x.v[2 * j + 1].x;
+            lo[j] = __builtin_amdgcn_perm(d, a, 0x05010400u);
+            hi[j] = __builtin_amdgcn_perm(d, a, 0x07030602u);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            u32x4_t vb;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t src = i < 2 ? lo[j] : hi[j];
+              vb[j] = i & 1 ? widen2<true>(src, x.vs[j / 2]) : widen2<false>(src, x.vs[j / 2]);
+            }
+            const bf16x8_t vv = __builtin_bit_cast(bf16x8_t, vb);
+            f32x4_t& d = acc[4 * half + i];
+            if constexpr (G == 8) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, pb), vv, d, 0, 0, 0);
+            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, pa), vv, d, 0, 0, 0);
+          }
+        }
+      };
+      Step8 x0, x1;
+      request(st0, x0);
+      for (int st = st0; st < st1; st += 2) {
+        request(min(st + 1, st1 - 1), x1);
+        consume(x0);
+        if (st + 1 >= st1) break;
+        request(min(st + 2, st1 - 1), x0);
+        consume(x1);
+      }
+    }
+    // the wavefront's sums: rows h + G * term of the second product belong to head h
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    __syncthreads();                                         // the previous segment's partial results have been read
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      f32x4_t s = acc[i];
+      if constexpr (G == 1) { s[0] += s[1]; s[2] += s[3]; s[0] += s[2]; }
+      if constexpr (G == 2) { s[0] += s[2]; s[1] += s[3]; }
+      constexpr int R = G < 4 ? G : 4;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if constexpr (G < 8) s[r] += __shfl_xor(s[r], 16);
+        s[r] += __shfl_xor(s[r], 32);
+        if (g < (G == 8 ? 2 : 1)) s_o[w][4 * g + r][8 * c + i] = s[r];
+      }
+    }
+    if (lane < G) { s_m[w][lane] = m; s_l[w][lane] = l; }
+    __syncthreads();
+    const bool whole = at == u_begin && seg_end == u_end;    // the unit is this workgroup's alone: no record, no join
+    float* rec = AA.part + (size_t)(blockIdx.x + unit) * G * kRec;
+    for (int e = threadIdx.x; e < G * kD; e += kAttnThreads) {
+      const int h = e / kD, ch = e % kD;
+      float M = s_m[0][h];
+#pragma unroll
+      for (int i = 1; i < kAttnWaves; ++i) M = fmaxf(M, s_m[i][h]);
+      float L = 0.f, o = 0.f;
+#pragma unroll
+      for (int i = 0; i < kAttnWaves; ++i) {
+        const float f = s_m[i][h] > -INFINITY ? __builtin_amdgcn_exp2f(s_m[i][h] - M) : 0.f;
+        L = fmaf(s_l[i][h], f, L);
+        o = fmaf(s_o[i][h][ch], f, o);
+      }
+      if (whole) {
+        AA.out[(row0 + h) * kD + ch] = L > 0.f ? o / L : (L == 0.f ? 0.f : o);
+        if (ch == 0) AA.lse[row0 + h] = L == 0.f ? -INFINITY : M * kLn2 + __logf(L);
+      } else {
+        rec[h * kRec + ch] = o;
+        if (ch == 0) { rec[h * kRec + kD] = M; rec[h * kRec + kD + 1] = L; }
+      }
+    }
+    at = seg_end;
+  }
+}
+
+// Joins the partial results of the units that several workgroups worked on, in their order, and writes those that have no token.
+// One workgroup per unit and head; eight groups of 128 threads take the records in turn.
+constexpr int kJoinGroups = 8;
+__global__ __launch_bounds__(kJoinGroups * kD) void attn8_join_kernel(const Attn8Args A, int G, int W) {
+  __shared__ float red[kJoinGroups * kD / 64];
+  __shared__ float g_o[kJoinGroups][kD], g_l[kJoinGroups];
+  const int unit = blockIdx.x / G, h = blockIdx.x % G, tid = threadIdx.x, t = tid & (kD - 1), grp = tid >> 7;
+  const size_t row = (size_t)unit * G + h;                   // [B][Hq]: units are (b, KV head) or (b, query head)
+  const int begin = A.pre[unit], end = A.pre[unit + 1];
+  if (begin == end) {
+    if (tid < kD) A.out[row * kD + tid] = 0.f;
+    if (tid == 0) A.lse[row] = -INFINITY;
+    return;
+  }
+  const int total = A.pre[A.s.U], per = total / W, rem = total - per * W;
+  auto wg_of = [&](int step) { return step < rem * (per + 1) ? step / (per + 1) : rem + (step - rem * (per + 1)) / per; };
+  const int w0 = wg_of(begin), w1 = wg_of(end - 1);
+  if (w0 == w1) return;                                      // written by that workgroup
+  const float* rec0 = A.part + ((size_t)(w0 + unit) * G + h) * kRec;
+  const int n = w1 - w0 + 1;
+  float mx = -INFINITY;
+  for (int i = tid; i < n; i += kJoinGroups * kD) mx = fmaxf(mx, rec0[(size_t)i * G * kRec + kD]);
+  const float M = block_max(mx, red);
+  float L = 0.f, o = 0.f;
+  for (int i0 = grp; i0 < n; i0 += 4 * kJoinGroups) {
+    float rm[4], rl[4], ro[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float* rec = rec0 + (size_t)min(i0 + u * kJoinGroups, n - 1) * G * kRec;
+      rm[u] = rec[kD]; rl[u] = rec[kD + 1]; ro[u] = rec[t];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float f = i0 + u * kJoinGroups < n && rm[u] > -INFINITY ? __builtin_amdgcn_exp2f(rm[u] - M) : 0.f;
+      L = fmaf(rl[u], f, L);
+      o = fmaf(ro[u], f, o);
+    }
+  }
+  g_o[grp][t] = o;
+  if (t == 0) g_l[grp] = L;
+  __syncthreads();
+  if (tid < kD) {
+    float Ls = 0.f, os = 0.f;
+    for (int i = 0; i < kJoinGroups; ++i) { Ls += g_l[i]; os += g_o[i][tid]; }
+    A.out[row * kD + tid] = Ls > 0.f ? os / Ls : (Ls == 0.f ? 0.f : os);
+    if (tid == 0) A.lse[row] = Ls == 0.f ? -INFINITY : M * kLn2 + __logf(Ls);
+  }
+}
+
+// Workgroups: four per compute unit, no more than there can be steps for their wavefronts.  Workspaces are sized for kMostWgs.
+constexpr int kMostWgs = 1024;
+static long long attn8_units(const Dims& dm, bool dense) { return (long long)dm.B * (dense ? dm.Hkv : dm.Hq); }
+static int attn8_grid(const Dims& dm, bool dense, int most) {
+  const long long steps = attn8_units(dm, dense) * (((long long)(dense ? dm.Mmax : dm.cap) * dm.P + kStep - 1) / kStep);
+  const long long wgs = (steps + kAttnWaves - 1) / kAttnWaves;
+  return (int)(wgs < most ? wgs : most);
+}
+static size_t attn8_pre_bytes(const Dims& dm, bool dense) { return (((size_t)attn8_units(dm, dense) + 1) * sizeof(int32_t) + 255) & ~(size_t)255; }
+
+size_t softmax8_ws_bytes(const Dims& dm, bool dense) {
+  const size_t recs = (size_t)attn8_units(dm, dense) + (size_t)attn8_grid(dm, dense, kMostWgs);
+  return attn8_pre_bytes(dm, dense) + recs * (dense ? dm.G : 1) * kRec * sizeof(float);
+}
+
+template <typename T, int G, bool DENSE>
+static void launch_attn8(const Dims& dm, Attn8Args a, hipStream_t st) {
+  const int cus = device_compute_units(), W = attn8_grid(dm, DENSE, 4 * cus < kMostWgs ? 4 * cus : kMostWgs);
+  if (a.s.U > kUnitsLdsMax) {
+    hipLaunchKernelGGL(attn8_prefix_kernel<DENSE>, dim3(1), dim3(1024), 0, st, a);
+    a.s.pre_g = a.pre;
+  }
+  const size_t lds = a.s.pre_g != nullptr ? 0 : (size_t)(a.s.U + 1) * sizeof(int);
+  if (dm.P % 16 == 0) hipLaunchKernelGGL((attn8_kernel<T, G, DENSE, true>), dim3(W), dim3(kAttnThreads), lds, st, a);
+  else hipLaunchKernelGGL((attn8_kernel<T, G, DENSE, false>), dim3(W), dim3(kAttnThreads), lds, st, a);
+  hipLaunchKernelGGL(attn8_join_kernel, dim3(a.s.U * G), dim3(kJoinGroups * kD), 0, st, a, G, W);
+}
+template <typename T>
+static void launch_attn8_T(const Dims& dm, bool dense, const Attn8Args& a, hipStream_t st) {
+  if (!dense) launch_attn8<T, 1, false>(dm, a, st);
+  else if (dm.G == 1) launch_attn8<T, 1, true>(dm, a, st);
+  else if (dm.G == 2) launch_attn8<T, 2, true>(dm, a, st);
+  else if (dm.G == 4) launch_attn8<T, 4, true>(dm, a, st);
+  else launch_attn8<T, 8, true>(dm, a, st);
+}
+
+void launch_decode8_softmax(const Dims& dm, bool dense, const void* q, const ekv_cache8_view& c, const int32_t* page_idx,
+                            const int32_t* n_sel, float* out, float* lse, void* ws, hipStream_t st) {
+  Attn8Args a{};
+  a.s = ScoreArgs{q, c.k_pool, c.block_table, c.seq_lens, page_idx, n_sel, nullptr, nullptr, dm.Hq, dm.Hkv, dm.P, dm.Mmax, dm.cap,
+                  0, c.n_phys_pages, 0, dm.scale * kLog2e, dm.HkvPool, (int)attn8_units(dm, dense), nullptr, 1};
+  a.k_scale = c.k_scale; a.v_scale = c.v_scale; a.v_pool = (const e4m3_t*)c.v_pool;
+  a.out = out; a.lse = lse;
+  a.pre = (int32_t*)ws;
+  a.part = (float*)((char*)ws + attn8_pre_bytes(dm, dense));
+  a.page_div = make_page_div(dm.P);
+  if (dm.dtype == EKV_F32) launch_attn8_T<float>(dm, dense, a, st);
+  else launch_attn8_T<bf16_t>(dm, dense, a, st);
+}
+
+}  // namespace ekv

@@ -68,7 +68,8 @@ void launch_select_gauss(const Dims& dm, const float* mu, const float* sigma, co
 // grouped: page_idx/n_sel have one row per (b, KV head), shared by the G query heads of the group
 void launch_decode(const Dims& dm, bool dense, bool grouped, const void* q, const ekv_cache_view& c,
                    const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau, int32_t* supp,
-                   const ekv_decode_extras& ex, const DecodeWorkspace& ws, hipStream_t st);
+                   const ekv_decode_extras& ex, const DecodeWorkspace& ws, hipStream_t st,
+                   const ekv_cache8_view* c8 = nullptr);      // c8: the cache is held in 8 bits, c has its pools
 void launch_decode_sparse_softmax(const Dims& dm, const void* q, const ekv_cache_view& c,
                                   const int32_t* page_idx, const int32_t* n_sel, float* out,
                                   float* lse_sel, void* ws, hipStream_t st);
@@ -82,6 +83,19 @@ void launch_probe_read(const void* base, const int32_t* page_ids, const int32_t*
                        float* out, uint32_t* sink, hipStream_t st);
 
 void launch_probe_handoff(float* data, uint32_t* counter, float* out, int n_workgroups, int mode, hipStream_t st);
+
+void launch_map_tokens(const Dims& dm, const int32_t* seq_lens, const int32_t* n_new, int32_t* block_table,
+                       const int32_t* free_pages, const int32_t* n_free, int capacity, const ekv_token_map& tok,
+                       int32_t* new_lens, int32_t* n_left, hipStream_t st);
+void launch_release_pages(const Dims& dm, const int32_t* release, const int32_t* seq_lens, const int32_t* block_table,
+                          int32_t* free_pages, const int32_t* n_free, int capacity, int32_t* new_lens, int32_t* n_left,
+                          hipStream_t st);
+void launch_cache8_append(const Dims& dm, const ekv_cache8_view& c, const ekv_stats_view* stats, const ekv_token_map& tok,
+                          const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, hipStream_t st);
+// dense: over every page, else over a list per query head
+void launch_decode8_softmax(const Dims& dm, bool dense, const void* q, const ekv_cache8_view& c, const int32_t* page_idx,
+                            const int32_t* n_sel, float* out, float* lse, void* ws, hipStream_t st);
+size_t softmax8_ws_bytes(const Dims& dm, bool dense);
 
 size_t select_topk_ws_bytes(const Dims& dm);
 size_t select_box_ws_bytes(const Dims& dm);

@@ -95,4 +95,8 @@ static inline int device_compute_units() {
 // kernels of decode.hip are the faster ones or the call has a form that it does not take.
 template <int G> bool launch_scores_windows(const Dims& dm, const ScoreArgs& sa, long long items, size_t k_bytes, hipStream_t st);
 
+// Pass 1 over an 8-bit cache (decode8_scores.hip), and the item prefix of launches with more units than LDS holds.
+void launch_scores8(const Dims& dm, int mode, ScoreArgs sa, const float* k_scale, int32_t* pre_ws, hipStream_t st);
+void launch_unit_prefix(int mode, const ScoreArgs& sa, int32_t* pre_out, hipStream_t st);
+
 }  // namespace ekv

@@ -1,0 +1,120 @@
+"""What the entry points of the 8-bit cache refuse, on the host and before anything is launched."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2605_21649_amd import binding as ekv
+from tests.test_abi_cpu import good_cfg
+
+INVALID, UNSUPPORTED, WORKSPACE = 1, 2, 3
+A = [0x1000 * i for i in range(1, 20)]
+
+
+def tokens(**kw):
+    base = dict(slots=A[0], seq=A[1], pos=A[2], start=A[3], n_mapped=A[4], max_tokens=64)
+    base.update(kw)
+    return ekv.ekv_token_map(**base)
+
+
+def cache(**kw):
+    base = dict(k_pool=A[0], v_pool=A[1], k_scale=A[2], v_scale=A[3], block_table=A[4], seq_lens=A[5], n_phys_pages=100)
+    base.update(kw)
+    return ekv.ekv_cache8_view(**base)
+
+
+def status(name, *args):
+    lib = ekv.load_library()
+    return getattr(lib, name)(*(ctypes.byref(a) if isinstance(a, ctypes.Structure) else a for a in args))
+
+
+MAP = dict(cfg=good_cfg(batch=3), seq_lens=A[5], n_new=A[6], block_table=A[7], free_pages=A[8], n_free=A[9], capacity=10,
+           tok=tokens(), new_lens=A[10], n_left=A[11], stream=None)
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(cfg=None), INVALID), (dict(cfg=good_cfg(page_size=6)), UNSUPPORTED), (dict(seq_lens=None), INVALID),
+    (dict(n_new=0x1002), INVALID), (dict(block_table=None), INVALID), (dict(free_pages=None), INVALID), (dict(n_free=None), INVALID),
+    (dict(capacity=0), INVALID), (dict(capacity=-1), INVALID), (dict(tok=None), INVALID), (dict(tok=tokens(slots=None)), INVALID),
+    (dict(tok=tokens(slots=0x1004)), INVALID), (dict(tok=tokens(seq=None)), INVALID), (dict(tok=tokens(pos=None)), INVALID),
+    (dict(tok=tokens(start=None)), INVALID), (dict(tok=tokens(n_mapped=None)), INVALID), (dict(tok=tokens(max_tokens=0)), INVALID),
+    (dict(tok=tokens(max_tokens=-5)), INVALID), (dict(tok=tokens(max_tokens=1 << 30)), UNSUPPORTED), (dict(new_lens=None), INVALID),
+    (dict(n_left=None), INVALID), (dict(new_lens=A[5]), INVALID), (dict(n_left=A[9]), INVALID), (dict(new_lens=A[6]), INVALID),
+    (dict(cfg=good_cfg(batch=4097)), UNSUPPORTED), (dict(free_pages=A[7]), INVALID),
+])
+def test_map_tokens_refuses(bad, code):
+    assert status("ekv_map_tokens", *dict(MAP, **bad).values()) == code
+
+
+RELEASE = dict(cfg=good_cfg(batch=3), release=A[4], seq_lens=A[5], block_table=A[7], free_pages=A[8], n_free=A[9], capacity=10,
+               new_lens=A[10], n_left=A[11], stream=None)
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(cfg=None), INVALID), (dict(release=None), INVALID), (dict(seq_lens=None), INVALID), (dict(block_table=None), INVALID),
+    (dict(free_pages=None), INVALID), (dict(n_free=None), INVALID), (dict(capacity=0), INVALID), (dict(new_lens=None), INVALID),
+    (dict(n_left=None), INVALID), (dict(new_lens=A[5]), INVALID), (dict(new_lens=A[4]), INVALID), (dict(n_left=A[9]), INVALID),
+    (dict(free_pages=A[7]), INVALID), (dict(cfg=good_cfg(batch=5000)), UNSUPPORTED),
+])
+def test_release_pages_refuses(bad, code):
+    assert status("ekv_release_pages", *dict(RELEASE, **bad).values()) == code
+
+
+APPEND = dict(cfg=good_cfg(), cache=cache(), stats=None, tok=tokens(seq=None, pos=None, start=None, n_mapped=None), k_new=A[10],
+              k_stride=1024, v_new=A[11], v_stride=1024, stream=None)
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(cfg=None), INVALID), (dict(cache=None), INVALID), (dict(cache=cache(k_pool=None)), INVALID),
+    (dict(cache=cache(v_pool=0x1008)), INVALID), (dict(cache=cache(k_scale=None)), INVALID), (dict(cache=cache(v_scale=0x1001)), INVALID),
+    (dict(cache=cache(n_phys_pages=0)), INVALID), (dict(cache=cache(n_phys_pages=1 << 23)), UNSUPPORTED),
+    (dict(tok=None), INVALID), (dict(tok=tokens(slots=None)), INVALID), (dict(tok=tokens(max_tokens=0)), INVALID),
+    (dict(tok=tokens(max_tokens=1 << 30)), UNSUPPORTED), (dict(k_new=None), INVALID), (dict(v_new=None), INVALID),
+    (dict(k_new=0x1008), INVALID), (dict(k_stride=1016), INVALID), (dict(v_stride=1028), INVALID), (dict(k_stride=-1024), INVALID),
+    (dict(stats=ekv.ekv_stats_view(A[12], None, None)), INVALID), (dict(stats=ekv.ekv_stats_view(A[12], A[13], None)), INVALID),
+    (dict(stats=ekv.ekv_stats_view(A[12], A[13], 0x1008), tok=tokens()), INVALID),
+    (dict(cfg=good_cfg(kv_dtype="f32"), stats=ekv.ekv_stats_view(A[12], A[13], A[14]), tok=tokens()), UNSUPPORTED),
+])
+def test_append_refuses(bad, code):
+    assert status("ekv_cache8_append", *dict(APPEND, **bad).values()) == code
+
+
+SPARSE = dict(cfg=good_cfg(), q=A[6], cache=cache(), page_idx=A[7], n_sel=A[8], out=A[9], tau=A[10], supp=A[11], extras=None,
+              ws=A[12], nbytes=1 << 40, stream=None)
+ATTENTION = [(dict(cfg=None), INVALID), (dict(q=None), INVALID), (dict(cache=None), INVALID), (dict(cache=cache(block_table=None)), INVALID),
+             (dict(cache=cache(seq_lens=None)), INVALID), (dict(cache=cache(k_scale=None)), INVALID), (dict(cache=cache(n_phys_pages=-3)), INVALID),
+             (dict(cache=cache(n_phys_pages=1 << 24)), UNSUPPORTED), (dict(cfg=good_cfg(head_dim=64)), UNSUPPORTED), (dict(out=None), INVALID),
+             (dict(tau=None), INVALID), (dict(ws=None), WORKSPACE), (dict(ws=0x1004), WORKSPACE), (dict(nbytes=16), WORKSPACE)]
+
+
+@pytest.mark.parametrize("name", ["ekv_decode8_sparse", "ekv_decode8_sparse_group", "ekv_decode8_full", "ekv_decode8_sparse_softmax",
+                                  "ekv_decode8_full_softmax"])
+@pytest.mark.parametrize("bad,code", ATTENTION + [(dict(page_idx=None), INVALID), (dict(n_sel=None), INVALID), (dict(supp=None), INVALID)])
+def test_attention_refuses(name, bad, code):
+    args = dict(SPARSE, **bad)
+    if "full" in name:
+        if "page_idx" in bad or "n_sel" in bad:
+            pytest.skip("no lists")
+        del args["page_idx"], args["n_sel"]
+    if "softmax" in name:
+        if "supp" in bad:
+            pytest.skip("no support")
+        del args["supp"], args["extras"]
+    assert status(name, *args.values()) == code
+
+
+def test_workspaces_of_the_softmax_do_not_grow_with_the_lists():
+    small, large = good_cfg(max_sel_pages=16), good_cfg(max_sel_pages=65536)
+    for op, rows in ((ekv.EKV_OP_DECODE8_SPARSE_SOFTMAX, 1), (ekv.EKV_OP_DECODE8_FULL_SOFTMAX, 4)):
+        assert 0 < ekv.ekv_workspace_bytes(small, op) <= ekv.ekv_workspace_bytes(large, op) <= (1024 + 64) * rows * 130 * 4
+
+
+def test_the_binding_takes_rows_of_a_longer_projection_and_no_other_strides():
+    rows = torch.zeros(5, 3, 2, 128)
+    assert ekv._rows(rows[:, 1]) == (rows.data_ptr() + 2 * 128 * 4, 3 * 2 * 128)
+    assert ekv._rows(rows[:1, 0])[1] == 256
+    for bad in (rows[:, 0].transpose(0, 1), rows[..., ::2][:, 0], rows[:, :, 0].transpose(1, 2)):
+        with pytest.raises(AssertionError):
+            ekv._rows(bad)
+    with pytest.raises(AssertionError):                      # fewer rows than the map has tokens
+        ekv.ekv_cache8_append(good_cfg(), cache(), None, tokens(max_tokens=6), rows[:, 0], rows[:, 1])

@@ -1,0 +1,319 @@
+"""Block tables, slots and the quantising append against plain forms.  Whole numbers, codes and scales have to be equal: scales
+are powers of two, so that quotients are exact, and each code is the format's nearest value.  Statistics equal, to the last bit,
+those that ekv_stats_build computes for a cache of the config's type that holds the stored values."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_21649_amd import binding as ekv
+from tests.cache8 import D, HIGH, LOW, VALUES, round_codes, scale_for
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- block tables and slots ---------------------------------------------------------------------------------------
+def plain_map(lens, new, table, free, n_free, P, max_tokens):
+    table = table.copy()
+    M = table.shape[1]
+    slots, seq, pos = (np.full(max_tokens, -1, dtype=np.int64) for _ in range(3))
+    start, mapped, out = [0], [], []
+    needed = taken = 0
+    for b, (n, c) in enumerate(zip(lens, new)):
+        at, c0 = start[-1], max(c, 0)
+        start.append(min(at + c0, 2 ** 30))
+        need = -(-(n + c0) // P) - -(-n // P)
+        fits = c0 > 0 and start[-1] <= max_tokens and n + c0 <= M * P
+        if fits and need:
+            needed += need
+            fits = needed <= n_free
+        mapped.append(c0 if fits else 0)
+        out.append(n + mapped[-1])
+        if not fits:
+            continue
+        for k in range(need):
+            table[b, -(-n // P) + k] = free[n_free - 1 - taken - k]
+        taken += need
+        for i in range(c0):
+            p = n + i
+            slots[at + i], seq[at + i], pos[at + i] = int(table[b, p // P]) * P + p % P, b, p
+    return dict(table=table, slots=slots, seq=seq, pos=pos, start=start, mapped=mapped, lens=out, left=n_free - taken)
+
+
+def run_map(lens, new, table, free, n_free, P, max_tokens, dtype="bf16"):
+    B, M = table.shape
+    i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    cfg = ekv.make_config(B, 1, 1, D, P, dtype, 1.5, 1.0, M, M)
+    out = [torch.full((max_tokens,), 77, dtype=torch.int64 if i == 0 else torch.int32, device="cuda") for i in range(3)]
+    start, mapped, new_lens, left = (torch.full((k,), 77, dtype=torch.int32, device="cuda") for k in (B + 1, B, B, 1))
+    t = i32(table)
+    ekv.ekv_map_tokens(cfg, i32(lens), i32(new), t, i32(free), i32([n_free]), ekv.token_map(*out, start, mapped), new_lens, left)
+    torch.cuda.synchronize()
+    a = lambda x: x.cpu().numpy().astype(np.int64)  # noqa: E731
+    return dict(table=a(t), slots=a(out[0]), seq=a(out[1]), pos=a(out[2]), start=a(start), mapped=a(mapped), lens=a(new_lens), left=a(left)[0])
+
+
+def same_map(lens, new, table, free, n_free, P, max_tokens):
+    ref, got = plain_map(lens, new, table, free, n_free, P, max_tokens), run_map(lens, new, table, free, n_free, P, max_tokens)
+    for k in ref:
+        assert np.array_equal(np.asarray(ref[k]), got[k]), k
+    return got
+
+
+@pytest.mark.parametrize("P", [4, 12, 16, 64])
+@pytest.mark.parametrize("B,most", [(1, 1), (1, 5000), (3, 40), (64, 1), (64, 300), (257, 70), (1000, 9)])
+def test_slots_of_new_tokens(B, most, P):
+    rng = np.random.default_rng(B + P)
+    lens = rng.integers(0, 200, B)
+    new = rng.integers(-2, most + 1, B)
+    if most == 1:
+        new = np.ones(B, dtype=np.int64)
+    M = -(-(200 + most) // P) + 1
+    table = rng.integers(0, 100000, (B, M))
+    total = int(np.maximum(new, 0).sum())
+    for slack in (0, 37):
+        n_free = int(sum(-(-(n + max(c, 0)) // P) - -(-n // P) for n, c in zip(lens, new))) + slack
+        free = rng.permutation(n_free + 10)
+        got = same_map(lens, new, table, free, n_free, P, max(1, total + slack))
+        assert got["left"] == slack
+
+
+def test_pages_run_out_and_rows_do_not_fit():
+    rng = np.random.default_rng(5)
+    P, B = 16, 50
+    lens = rng.integers(0, 90, B)
+    lens[7] = 160                            # its row of the block table is full
+    new = rng.integers(0, 60, B)
+    new[7], new[30], new[31] = 5, 1, 0
+    lens[30] = 33                            # needs no page: is served behind those that are not
+    table = rng.integers(0, 1000, (B, 10))
+    free = rng.permutation(1000)
+    for n_free in (0, 1, 7, 40, 60, 500):
+        got = same_map(lens, new, table, free, n_free, P, 3000)
+        assert got["mapped"][30] == 1 and got["mapped"][7] == 0
+    same_map(lens, new, table, free, 500, P, 400)          # more rows than max_tokens
+    same_map(lens, new, table, free, 500, P, 1)
+
+
+def test_nothing_to_map_and_counts_beyond_any_range():
+    table = np.arange(12).reshape(3, 4)
+    same_map([3, 0, 64], [0, 0, 0], table, np.arange(5), 5, 16, 9)
+    same_map([3, 0, 60], [0, 2 ** 31 - 1, 4], table, np.arange(5), 5, 16, 9)          # rows of the third lie behind the second's
+    big = run_map([0] * 3, [2 ** 31 - 1] * 3, table, np.arange(5), 5, 16, 9)
+    assert big["left"] == 5 and np.all(big["mapped"] == 0) and np.all(big["slots"] == -1) and big["start"][3] == 2 ** 30
+    got = run_map([3, -4, 10 ** 6], [1, 1, 1], table, np.arange(5), 2 ** 31 - 1, 16, 3)   # lengths out of range, more free than there are
+    assert got["mapped"].tolist() == [1, 0, 0] and got["left"] == 5
+
+
+def test_the_largest_batch():
+    rng = np.random.default_rng(9)
+    B = 4096
+    same_map(rng.integers(0, 60, B), rng.integers(0, 3, B), rng.integers(0, 10 ** 5, (B, 5)), rng.permutation(10 ** 4), 1500, 16, 2 * B)
+
+
+@pytest.mark.parametrize("P", [4, 16, 60])
+@pytest.mark.parametrize("B", [1, 5, 300, 4096])
+def test_pages_come_back(B, P):
+    rng = np.random.default_rng(B)
+    M = 9
+    lens, gone = rng.integers(0, M * P + 1, B), rng.integers(0, 2, B)
+    table = rng.permutation(B * M).reshape(B, M)
+    back = [p for b in range(B) if gone[b] for p in table[b, :-(-lens[b] // P)]]
+    for n_free, capacity in ((11, 11 + len(back) + 3), (0, max(1, len(back))), (4, 4 + len(back) // 2 + 1)):
+        free = np.full(capacity, -9)
+        free[:n_free] = np.arange(n_free)
+        i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+        cfg = ekv.make_config(B, 1, 1, D, P, "bf16", 1.5, 1.0, M, M)
+        f, new_lens, left = i32(free), i32(np.full(B, 77)), i32([77])
+        ekv.ekv_release_pages(cfg, i32(gone), i32(lens), i32(table), f, i32([n_free]), new_lens, left)
+        torch.cuda.synchronize()
+        kept = back[:capacity - n_free]
+        ref = free.copy()
+        ref[n_free:n_free + len(kept)] = kept
+        assert np.array_equal(f.cpu().numpy(), ref) and int(left[0]) == n_free + len(kept)
+        assert np.array_equal(new_lens.cpu().numpy(), np.where(gone, 0, lens))
+
+
+# ---- the quantising append ----------------------------------------------------------------------------------------
+class Pools:
+    def __init__(self, n_phys, heads, P, rng):
+        self.P, self.heads = P, heads
+        self.codes = [rng.integers(0, 256, (n_phys, heads, P, D)).astype(np.uint8) for _ in range(2)]
+        self.scales = [2.0 ** rng.integers(-4, 4, (n_phys, heads)) for _ in range(2)]
+
+    def device(self):
+        return [torch.from_numpy(c).cuda() for c in self.codes] + [torch.from_numpy(s.astype(np.float32)).cuda() for s in self.scales]
+
+    def append(self, runs, x):
+        """runs: (page, first token, first row, rows).  Values of the touched slots and scales."""
+        for side in range(2):
+            value = VALUES[self.codes[side]]
+            for page, t0, row, n in runs:
+                for h in range(self.heads):
+                    new = x[side][row:row + n, h].astype(np.float64)
+                    s, was = scale_for(new), self.scales[side][page, h]
+                    if t0 and was >= s:
+                        s = was
+                    elif t0:
+                        with np.errstate(invalid="ignore"):
+                            value[page, h, :t0] = round_codes(value[page, h, :t0] * was / s)
+                    value[page, h, t0:t0 + n] = round_codes(new / s)
+                    self.scales[side][page, h] = s
+            yield value
+
+
+def deal(rng, pages, P, T, ragged=True):
+    """Rows for runs on distinct pages, some rows without a slot; every second run begins in the middle of its page."""
+    runs, slots = [], []
+    for page in pages:
+        if len(slots) >= T:
+            break
+        t0 = int(rng.integers(0, P)) if ragged and rng.random() < 0.5 else 0
+        n = int(rng.integers(1, P - t0 + 1)) if ragged else P
+        n = min(n, T - len(slots))
+        runs.append((int(page), t0, len(slots), n))
+        slots += [int(page) * P + t0 + i for i in range(n)]
+        if ragged and rng.random() < 0.2:
+            slots += [-1] * int(rng.integers(1, 4))
+    return runs, slots
+
+
+def new_rows(rng, T, heads, dtype, kind="usual"):
+    x = rng.standard_normal((T, 3, heads, D)).astype(np.float32)
+    if kind == "usual":
+        x *= (2.0 ** rng.integers(-3, 6, (T, 1, 1, 1))).astype(np.float32)
+    elif kind == "strange":
+        with np.errstate(over="ignore"):
+            x *= np.exp2(rng.integers(-140, 128, (T, 1, heads, 1)).astype(np.float64)).astype(np.float32)
+        flat = x.reshape(-1)
+        for v in (np.nan, np.inf, -np.inf, 0.0, -0.0, 3.4028234e38, -3.4028234e38, 1e-45, 448.0, 464.0, 480.0):
+            flat[rng.integers(0, flat.size, max(1, flat.size // 200))] = v
+        x[:T // 3] = np.float32(0.0)
+    elif kind == "ties":                                                # halves of steps, and maxima at 448 times a power of two
+        x = (rng.integers(-480, 481, x.shape) * 2.0 ** rng.integers(-11, 3, (T, 1, heads, 1))).astype(np.float32)
+    t = torch.from_numpy(x)
+    t = t.to(torch.bfloat16) if dtype == "bf16" else t
+    return t.cuda(), t.float().numpy()
+
+
+def check_append(rng, P, heads, T, n_phys, dtype="bf16", kind="usual", ragged=True, pages=None):
+    pool = Pools(n_phys, heads, P, rng)
+    runs, slots = deal(rng, pages if pages is not None else rng.permutation(n_phys), P, T, ragged)
+    dev, host = new_rows(rng, len(slots), heads, dtype, kind)
+    kp, vp, ks, vs = pool.device()
+    before = [c.copy() for c in pool.codes]
+    cfg = ekv.make_config(1, heads, heads, D, P, dtype, 1.5, 1.0, 4, 4)
+    ekv.ekv_cache8_append(cfg, ekv.cache8_view(kp, vp, ks, vs), None,
+                          ekv.token_map(torch.tensor(slots, dtype=torch.int64, device="cuda")), dev[:, 1], dev[:, 2])
+    torch.cuda.synchronize()
+    touched = np.zeros((n_phys, P), dtype=bool)
+    rewritten = np.zeros((n_phys, P), dtype=bool)
+    for page, t0, row, n in runs:
+        touched[page, t0:t0 + n] = True
+        rewritten[page, :t0] = True
+    for side, (value, got, scale) in enumerate(zip(pool.append(runs, [host[:, 1], host[:, 2]]), (kp, vp), (ks, vs))):
+        got, scale = got.cpu().numpy(), scale.cpu().numpy().astype(np.float64)
+        assert np.array_equal(scale, pool.scales[side])
+        assert np.array_equal(VALUES[got], value, equal_nan=True)
+        rest = ~(touched | rewritten)
+        assert np.array_equal(got[np.broadcast_to(rest[:, None], got.shape[:3])], before[side][np.broadcast_to(rest[:, None], got.shape[:3])])
+
+
+@pytest.mark.parametrize("kind", ["usual", "strange", "ties"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("P", [4, 12, 16, 20, 32, 48, 64])
+def test_codes_and_scales(P, dtype, kind):
+    rng = np.random.default_rng(P)
+    check_append(rng, P, 3, 150, 80, dtype, kind)
+    check_append(rng, P, 1, 1, 4, dtype, kind)
+
+
+@pytest.mark.parametrize("T", [1, 63, 64, 65, 127, 128, 129, 2000, 9001])
+def test_runs_over_wavefronts_and_workgroups(T):
+    rng = np.random.default_rng(T)
+    check_append(rng, 16, 2, T, T // 4 + 9)
+    check_append(rng, 64, 2, T, T // 16 + 9, ragged=False)
+    check_append(rng, 64, 1, T, T // 16 + 9, dtype="f32")
+
+
+def test_pages_that_follow_each_other_are_runs_of_their_own():
+    check_append(np.random.default_rng(3), 16, 2, 16 * 40, 64, ragged=False, pages=range(64))
+
+
+def test_rows_whose_slots_lie_outside_the_pool_are_passed_over():
+    rng = np.random.default_rng(4)
+    pool = Pools(5, 2, 16, rng)
+    kp, vp, ks, vs = pool.device()
+    keep = [t.clone() for t in (kp, vp, ks, vs)]
+    dev, _ = new_rows(rng, 6, 2, "bf16")
+    slots = torch.tensor([-1, -2 ** 62, 5 * 16, 5 * 16 + 1, 2 ** 40, 2 ** 63 - 1], dtype=torch.int64, device="cuda")
+    cfg = ekv.make_config(1, 2, 2, D, 16, "bf16", 1.5, 1.0, 4, 4)
+    ekv.ekv_cache8_append(cfg, ekv.cache8_view(kp, vp, ks, vs), None, ekv.token_map(slots), dev[:, 1], dev[:, 2])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(keep, (kp, vp, ks, vs)))
+
+
+@pytest.mark.parametrize("with8", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("P", [4, 12, 16, 32, 64])
+def test_statistics_are_those_of_the_stored_keys(P, dtype, with8):
+    """Prompts, then single tokens (some larger than anything before, so that pages are rounded again): after every step all
+    statistics equal ekv_stats_build's of a cache that holds the stored keys."""
+    if with8 and dtype == "f32":
+        pytest.skip("8-bit bounds are of bf16 statistics")
+    rng = np.random.default_rng(P)
+    B, H, M = 4, 2, 160 // P + 2
+    n_phys = B * M
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    cfg = ekv.make_config(B, H, H, D, P, dtype, 1.5, 1.0, M, M)
+    kp, vp = (torch.full((n_phys, H, P, D), 0x7F, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.full((n_phys, H), float("nan"), device="cuda") for _ in range(2))
+    table = torch.zeros(B, M, dtype=torch.int32, device="cuda")
+    free = torch.from_numpy(rng.permutation(n_phys).astype(np.int32)).cuda()
+    lens, n_free = torch.zeros(B, dtype=torch.int32, device="cuda"), torch.tensor([n_phys], dtype=torch.int32, device="cuda")
+    box, gauss = (torch.zeros(B, H, M, 2, D, dtype=dt, device="cuda") for _ in range(2))
+    box8 = torch.zeros(B, H, M, 16, 2, 8, dtype=torch.uint8, device="cuda") if with8 else None
+    for step, counts in enumerate([[37, 1, 0, 90]] + [[1, 1, 1, 1]] * 6 + [[0, 5, 30, 2], [1, 0, 1, 1]]):
+        T = sum(counts)
+        i32 = lambda k: torch.zeros(k, dtype=torch.int32, device="cuda")  # noqa: E731
+        slots, seq, pos, start, mapped, new_lens, left = torch.zeros(T, dtype=torch.int64, device="cuda"), i32(T), i32(T), i32(B + 1), i32(B), i32(B), i32(1)
+        tokens = ekv.token_map(slots, seq, pos, start, mapped)
+        ekv.ekv_map_tokens(cfg, lens, torch.tensor(counts, dtype=torch.int32, device="cuda"), table, free, n_free, tokens, new_lens, left)
+        dev, _ = new_rows(rng, T, H, dtype)
+        ekv.ekv_cache8_append(cfg, ekv.cache8_view(kp, vp, ks, vs), ekv.stats_view(box, gauss, box8), tokens, dev[:, 1], dev[:, 2])
+        lens, n_free = new_lens, left
+        torch.cuda.synchronize()
+        stored = torch.from_numpy(VALUES[kp.cpu().numpy()]).cuda() * ks.double()[:, :, None, None]
+        stored = torch.nan_to_num(stored).to(dt)
+        ref = [torch.zeros_like(box), torch.zeros_like(gauss)]
+        ref8 = torch.zeros_like(box8) if with8 else None
+        ekv.ekv_stats_build(cfg, ekv.cache_view(stored, stored, table, lens), ekv.stats_view(*ref, ref8))
+        torch.cuda.synchronize()
+        for b in range(B):
+            m = -(-int(lens[b]) // P)
+            for got, want in ((box, ref[0]), (gauss, ref[1])) + (((box8, ref8),) if with8 else ()):
+                assert torch.equal(got[b, :, :m].contiguous().view(torch.uint8), want[b, :, :m].contiguous().view(torch.uint8)), (step, b)
+
+
+def test_a_sequence_outside_the_table_leaves_the_statistics():
+    rng = np.random.default_rng(8)
+    kp, vp, ks, vs = Pools(4, 1, 16, rng).device()
+    dev, _ = new_rows(rng, 3, 1, "bf16")
+    box, gauss = (torch.zeros(2, 1, 3, 2, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    tokens = ekv.token_map(torch.tensor([0, 16, 32], dtype=torch.int64, device="cuda"), i32([2, -1, 0]), i32([0, 0, 48]))
+    cfg = ekv.make_config(2, 1, 1, D, 16, "bf16", 1.5, 1.0, 3, 3)
+    ekv.ekv_cache8_append(cfg, ekv.cache8_view(kp, vp, ks, vs), ekv.stats_view(box, gauss), tokens, dev[:, 1], dev[:, 2])
+    torch.cuda.synchronize()
+    assert not box.any() and not gauss.any()
+
+
+def test_scales_at_the_ends_of_their_range():
+    rng = np.random.default_rng(9)
+    for big, exponent in ((3.4e38, HIGH), (1e-44, LOW), (0.0, LOW)):
+        kp, vp, ks, vs = Pools(1, 1, 4, rng).device()
+        x = torch.full((1, 1, D), big, device="cuda")
+        cfg = ekv.make_config(1, 1, 1, D, 4, "f32", 1.5, 1.0, 1, 1)
+        ekv.ekv_cache8_append(cfg, ekv.cache8_view(kp, vp, ks, vs), None, ekv.token_map(torch.zeros(1, dtype=torch.int64, device="cuda")), x, x)
+        torch.cuda.synchronize()
+        assert float(ks[0, 0]) == 2.0 ** exponent and float(vs[0, 0]) == 2.0 ** exponent
+        assert int(kp[0, 0, 0, 0]) == (0x7E if big > 1 else 0)

@@ -1,0 +1,172 @@
+"""Serving steps on the 8-bit cache, as a program makes them: lengths -> pages and slots -> append -> page scores -> selection ->
+attention, and ended sequences' pages back.  Eagerly, recorded into a graph, and on another stream."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import entmaxkv_oracle as orc
+from paper_2605_21649_amd import binding as ekv
+from tests.cache8 import D, VALUES, score_error
+
+pytestmark = pytest.mark.gpu
+
+
+class Server:
+    """Buffers of a batch of sequences on one 8-bit cache; step() only launches."""
+
+    def __init__(self, B=4, Hq=8, Hkv=2, P=16, M=20, n_phys=70, max_tokens=400, dtype="bf16", k_pages=4, seed=0):
+        dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.dims = B, Hq, Hkv, P, M
+        g = torch.Generator().manual_seed(seed)
+        dev = "cuda"
+        f32, i32 = dict(device=dev, dtype=torch.float32), dict(device=dev, dtype=torch.int32)
+        self.cfg = ekv.make_config(B, Hq, Hkv, D, P, dtype, 1.5, 1.0 / np.sqrt(D), M, M)
+        self.kp, self.vp = (torch.full((n_phys, Hkv, P, D), 0x7F, device=dev, dtype=torch.uint8) for _ in range(2))
+        self.ks, self.vs = (torch.full((n_phys, Hkv), float("nan"), **f32) for _ in range(2))
+        self.table = torch.zeros(B, M, **i32)
+        self.lens, self.lens2 = torch.zeros(B, **i32), torch.zeros(B, **i32)
+        self.free = torch.randperm(n_phys, generator=g).to(torch.int32).cuda()
+        self.n_free, self.n_free2 = torch.tensor([n_phys], **i32), torch.zeros(1, **i32)
+        self.counts, self.gone = torch.zeros(B, **i32), torch.zeros(B, **i32)
+        self.slots, self.seq, self.pos = torch.zeros(max_tokens, device=dev, dtype=torch.int64), torch.zeros(max_tokens, **i32), torch.zeros(max_tokens, **i32)
+        self.start, self.mapped = torch.zeros(B + 1, **i32), torch.zeros(B, **i32)
+        self.tokens = ekv.token_map(self.slots, self.seq, self.pos, self.start, self.mapped)
+        self.box_stats, self.gauss_stats = (torch.zeros(B, Hkv, M, 2, D, device=dev, dtype=dt) for _ in range(2))
+        self.rows = torch.zeros(max_tokens, 3, Hkv, D, device=dev, dtype=dt)      # one projection: queries' share unused
+        self.q = torch.zeros(B, Hq, D, device=dev, dtype=dt)
+        self.box = torch.zeros(B, Hq, M, **f32)
+        self.idx, self.n_sel = torch.zeros(B, Hq, M, **i32), torch.zeros(B, Hq, **i32)
+        self.out, self.tau, self.supp = torch.zeros(B, Hq, D, **f32), torch.zeros(B, Hq, **f32), torch.zeros(B, Hq, **i32)
+        self.full, self.full_tau, self.full_supp = torch.zeros(B, Hq, D, **f32), torch.zeros(B, Hq, **f32), torch.zeros(B, Hq, **i32)
+        self.soft, self.lse = torch.zeros(B, Hq, D, **f32), torch.zeros(B, Hq, **f32)
+        self.soft_sel, self.lse_sel = torch.zeros(B, Hq, D, **f32), torch.zeros(B, Hq, **f32)
+        self.ws = {op: torch.empty(max(256, ekv.ekv_workspace_bytes(self.cfg, op)), device=dev, dtype=torch.uint8) for op in range(8)}
+        self.k = k_pages
+
+    def view(self):
+        return ekv.cache8_view(self.kp, self.vp, self.ks, self.vs, self.table, self.lens)
+
+    def stats(self):
+        return ekv.stats_view(self.box_stats, self.gauss_stats)
+
+    def step(self):
+        c = self.cfg
+        ekv.ekv_release_pages(c, self.gone, self.lens, self.table, self.free, self.n_free, self.lens2, self.n_free2)
+        ekv.ekv_map_tokens(c, self.lens2, self.counts, self.table, self.free, self.n_free2, self.tokens, self.lens, self.n_free)
+        ekv.ekv_cache8_append(c, self.view(), self.stats(), self.tokens, self.rows[:, 1], self.rows[:, 2])
+        ekv.ekv_score_pages(c, self.q, self.stats(), self.lens, ekv.EKV_SCORE_BOX, self.box)
+        ekv.ekv_select_topk(c, self.box, self.lens, self.k, self.idx, self.n_sel, self.ws[ekv.EKV_OP_SELECT_TOPK])
+        ekv.ekv_decode8_sparse(c, self.q, self.view(), self.idx, self.n_sel, self.out, self.tau, self.supp, self.ws[ekv.EKV_OP_DECODE_SPARSE])
+        ekv.ekv_decode8_full(c, self.q, self.view(), self.full, self.full_tau, self.full_supp, self.ws[ekv.EKV_OP_DECODE_FULL])
+        ekv.ekv_decode8_sparse_softmax(c, self.q, self.view(), self.idx, self.n_sel, self.soft_sel, self.lse_sel,
+                                       self.ws[ekv.EKV_OP_DECODE8_SPARSE_SOFTMAX])
+        ekv.ekv_decode8_full_softmax(c, self.q, self.view(), self.soft, self.lse, self.ws[ekv.EKV_OP_DECODE8_FULL_SOFTMAX])
+
+    def feed(self, counts, gone, rng):
+        self.counts.copy_(torch.tensor(counts, dtype=torch.int32))
+        self.gone.copy_(torch.tensor(gone, dtype=torch.int32))
+        self.rows.copy_(torch.from_numpy(rng.standard_normal(self.rows.shape).astype(np.float32)))
+        self.q.copy_(torch.from_numpy(2.0 * rng.standard_normal(self.q.shape).astype(np.float32)))
+
+    def results(self):
+        return [t.clone() for t in (self.out, self.tau, self.supp, self.full, self.full_tau, self.full_supp, self.soft, self.lse,
+                                    self.soft_sel, self.lse_sel, self.lens, self.n_free, self.box, self.ks, self.vs, self.table)]
+
+
+# counts of new tokens and ended sequences of consecutive steps: prompts, single tokens, an end and a new prompt in its place
+STEPS = [([70, 0, 5, 200], [0, 0, 0, 0])] + [([1, 0, 1, 1], [0, 0, 0, 0])] * 3 + [([1, 33, 1, 90], [0, 0, 0, 1])] + \
+        [([1, 1, 1, 1], [0, 0, 0, 0])] * 3 + [([0, 1, 0, 0], [1, 0, 1, 0]), ([16, 1, 300, 1], [0, 0, 0, 0])]
+
+
+def test_steps_against_the_oracle():
+    s, rng = Server(), np.random.default_rng(1)
+    B, Hq, Hkv, P, M = s.dims
+    lens = [0] * B
+    kept = [[np.zeros((0, Hkv, D))] * 2 for _ in range(B)]        # what was appended, before quantisation
+    for counts, gone in STEPS:
+        s.feed(counts, gone, rng)
+        s.step()
+        torch.cuda.synchronize()
+        at = 0
+        for b in range(B):
+            if gone[b]:
+                lens[b], kept[b] = 0, [np.zeros((0, Hkv, D))] * 2
+            new = s.rows[at:at + counts[b]].float().cpu().numpy()
+            kept[b] = [np.concatenate((kept[b][i], new[:, 1 + i])) for i in range(2)]
+            lens[b] += counts[b]
+            at += counts[b]
+        assert s.lens.tolist() == lens
+        used = sum(-(-n // P) for n in lens)
+        assert int(s.n_free[0]) == s.free.numel() - used
+        table = s.table.cpu().numpy()
+        owned = [p for b in range(B) for p in table[b, :-(-lens[b] // P)]] + s.free[:int(s.n_free[0])].tolist()
+        assert sorted(owned) == list(range(s.free.numel()))       # every page once
+        codes, scales = [s.kp.cpu().numpy(), s.vp.cpu().numpy()], [s.ks.cpu().numpy().astype(np.float64), s.vs.cpu().numpy().astype(np.float64)]
+        for b in range(B):
+            for h in range(Hq):
+                if lens[b] == 0:
+                    assert not s.out[b, h].any() and not s.full[b, h].any() and not s.soft[b, h].any() and float(s.lse[b, h]) == -np.inf
+                    continue
+                rows = table[b, :-(-lens[b] // P)]
+                K, V = ((VALUES[codes[i][rows, h // 4]] * scales[i][rows, h // 4][:, None, None]).reshape(-1, D)[:lens[b]] for i in range(2))
+                for x, y in zip((K, V), kept[b]):                 # a quantised value is within half a step, 2^-4, or the last place of the
+                    y = y[:, h // 4]                              # smallest ones; one more for every time that its page was rounded again
+                    assert np.all(np.abs(x - y) <= 2.0 ** -4 * np.abs(y) * 1.1 + 2.0 ** -9 * np.abs(y).max())
+                q = s.q[b, h].float().cpu().numpy().astype(np.float64)
+                e = score_error(q, K, s.cfg.scale)
+                pages = s.idx[b, h, :int(s.n_sel[b, h])].cpu().numpy()
+                tok = orc.pages_to_tokens(pages, P, lens[b])
+                full, sparse = orc.entmax_attention(q, K, V, 1.5, s.cfg.scale), orc.entmax_attention(q, K, V, 1.5, s.cfg.scale, tok)
+                soft, soft_sel = orc.softmax_attention(q, K, V, s.cfg.scale), orc.softmax_attention(q, K, V, s.cfg.scale, tok)
+                assert abs(float(s.full_tau[b, h]) - full["tau"]) <= e + 4e-6 * max(1, abs(full["tau"]))
+                assert abs(float(s.tau[b, h]) - sparse["tau"]) <= e + 4e-6 * max(1, abs(sparse["tau"]))
+                assert abs(float(s.lse[b, h]) - soft["lse"]) <= e + 1e-5 and abs(float(s.lse_sel[b, h]) - soft_sel["lse"]) <= e + 1e-5
+                for got, ref in ((s.full, full), (s.out, sparse), (s.soft, soft), (s.soft_sel, soft_sel)):
+                    r = ref["o"]
+                    assert np.linalg.norm(got[b, h].cpu().numpy() - r) <= (4 * e + 2e-5) * np.linalg.norm(np.abs(ref["p"]) @ np.abs(V if len(ref["p"]) == len(V) else V[tok]))
+                kmin, kmax = orc.page_stats(K, P)[:2]             # page scores bound the stored keys' scores
+                assert np.allclose(s.box[b, h, :len(rows)].cpu().numpy(), orc.box_scores(q, kmin, kmax, s.cfg.scale), atol=3 * e + 1e-6)
+                top = orc.box_scores(q, kmin, kmax, s.cfg.scale)
+                assert np.all(top[np.arange(lens[b]) // P] >= s.cfg.scale * (K @ q) - 1e-9)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_recorded_step_gives_the_bits_of_the_eager_ones(dtype):
+    eager, taped = Server(dtype=dtype), Server(dtype=dtype)
+    side = torch.cuda.Stream()
+    taped.feed([0, 0, 0, 0], [0, 0, 0, 0], np.random.default_rng(0))
+    with torch.cuda.stream(side):
+        taped.step()                                              # nothing to append: a warm-up without effect
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        taped.step()
+    a, b = np.random.default_rng(5), np.random.default_rng(5)
+    for counts, gone in STEPS:
+        eager.feed(counts, gone, a)
+        eager.step()
+        ref = eager.results()
+        taped.feed(counts, gone, b)
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(ref, taped.results()):
+            assert torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8))
+
+
+def test_two_servers_on_streams_of_their_own():
+    """Steps of two batches at the same time, each on its stream with its workspaces, against the same steps alone."""
+    alone, both = [Server(seed=i) for i in range(2)], [Server(seed=i) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for n, (counts, gone) in enumerate(STEPS):
+        for i in range(2):
+            alone[i].feed(counts, gone, np.random.default_rng(10 * n + i))
+            both[i].feed(counts, gone, np.random.default_rng(10 * n + i))
+            alone[i].step()
+        torch.cuda.synchronize()
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                both[i].step()
+        torch.cuda.synchronize()
+        for i in range(2):
+            for x, y in zip(alone[i].results(), both[i].results()):
+                assert torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8))
