@@ -35,16 +35,6 @@ __global__ __launch_bounds__(1024) void unit_prefix_kernel(const ScoreArgs A, in
   block_exclusive_prefix<1024>(A.U, [&](int u) { return (unit_slots<MODE>(A, u) + gp - 1) / gp; }, pre_out, wsum);
 }
 
-// first item of a unit of n items that belongs to the part
-__device__ __forceinline__ int part_first(const Part& p, int group, int n) {
-  return p.count == 1 ? 0 : (int)(((unsigned)n * (unsigned)((p.index + group) % kXcds)) / kXcds);
-}
-__device__ __forceinline__ int part_length(const Part& p, int group, int n) {
-  if (p.count == 1) return n;
-  const unsigned i = (unsigned)((p.index + group) % kXcds);
-  return (int)((unsigned)n * (i + 1) / kXcds - (unsigned)n * i / kXcds);
-}
-
 // Sums of G values over the 16 lanes of a DPP row, one head's sum in 16 / G lanes: two heads share a step by passing each
 // other's half on, so eight heads take 8 exchanges instead of 32, and what follows is done once instead of per head.
 // The pairs added are those of row16_sum, so the sums are its to the last bit.  The mirrors of the third and fourth step turn

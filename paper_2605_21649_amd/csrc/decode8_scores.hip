@@ -3,19 +3,13 @@
 
 namespace ekv {
 
-struct Score8Args {
-  ScoreArgs s;                      // k_pool: the codes
-  const float* k_scale;
-};
-
 // An item is one group of page slots (up to 64 tokens) of one unit, as in decode.hip, and a wavefront takes a contiguous range
 // of them.  The page-list, block-table and scale entries of up to 64 page slots are fetched at once, one slot per lane.
-// TILED: pages of 16, 32, 48 or 64 tokens, where a tile lies in one page and its place is wave-uniform.  Otherwise a tile may span
-// pages and every lane looks up its own token's (the four tokens of a result lane are of one page).
-// Columns of the MFMA beyond the G heads repeat them, so the lanes of copy t of the heads hold every tile's scores and store
-// tile t's: 16 bytes a lane, 1 KB for four heads' 64 tokens with one instruction.
-template <typename T, int G, int MODE, bool TILED, bool STREAM>
-__global__ __launch_bounds__(kScoreThreads) void decode8_scores_kernel(const Score8Args A8) {
+// OCTETS: pages of a multiple of 8 tokens, where eight tokens lie in one page and their place is wave-uniform.  Otherwise they may
+// span pages and every lane looks up its own token's (the two tokens of a result lane are of one page).
+template <typename T, int G, int MODE, bool OCTETS, bool STREAM>
+__global__ __launch_bounds__(kScoreThreads) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 && OCTETS ? 4 : 3)))
+void decode8_scores_kernel(const Score8Args A8) {
   const ScoreArgs& A = A8.s;
   constexpr bool DENSE = MODE == kAllPages, GROUPED = MODE != kPerHead;
   extern __shared__ int pre_lds[];
@@ -26,17 +20,28 @@ __global__ __launch_bounds__(kScoreThreads) void decode8_scores_kernel(const Sco
   const e4m3_t* k_pool = (const e4m3_t*)A.k_pool;
   const T* q = (const T*)A.q;
   const bool in_lds = A.pre_g == nullptr;
-  if (in_lds) block_exclusive_prefix<kScoreThreads>(A.U, [&](int u) { return (unit_slots<MODE>(A, u) + gp - 1) / gp; }, pre_lds, wsum);
-  const WaveItems wi = in_lds ? wave_item_range((const int*)pre_lds, A.U, w, Part{0, 1}) : wave_item_range(A.pre_g, A.U, w, Part{0, 1});
+  const int ratio = A.Hq / A.Hkv;
+  const Part part = MODE == kPerHead ? unit_part(A) : Part{0, 1};
+  if (in_lds)
+    block_exclusive_prefix<kScoreThreads>(A.U, [&](int u) {
+      return part_length(part, u / ratio, (unit_slots<MODE>(A, u) + gp - 1) / gp); }, pre_lds, wsum);
+  const WaveItems wi = in_lds ? wave_item_range((const int*)pre_lds, A.U, w, part) : wave_item_range(A.pre_g, A.U, w, part);
   const int last = (DENSE ? A.Mmax : A.cap) - 1;
-  // the lane's token as a row of tile t and the first of its four tokens as results: page slot of the item and place in the page
-  int k_slot[4], k_tok[4], z_slot[4], z_tok[4];
+  // Octet o of an item: page slot and token of its keys (of the lane's one, without OCTETS), and of the lane's first result
+  int k_slot[8], k_tok[8], z_slot[8], z_tok[8];
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const int pk = TILED ? 16 * t : min(16 * t + c, GT - 1), pz = TILED ? 16 * t : min(16 * t + 4 * g, GT - 4);
-    k_slot[t] = pk / P; k_tok[t] = pk - k_slot[t] * P + (TILED ? c : 0);
-    z_slot[t] = pz / P; z_tok[t] = pz - z_slot[t] * P + (TILED ? 4 * g : 0);
+  for (int o = 0; o < 8; ++o) {
+    if constexpr (OCTETS) {
+      const int p = min(8 * o, GT - 8);
+      k_slot[o] = z_slot[o] = uniform(p / P); k_tok[o] = z_tok[o] = p - k_slot[o] * P;
+    } else {
+      const int pk = min(8 * o + key_token(c), GT - 1), pz = min(8 * o + 2 * g, GT - 2);
+      k_slot[o] = pk / P; k_tok[o] = pk - k_slot[o] * P;
+      z_slot[o] = pz / P; z_tok[o] = pz - z_slot[o] * P;
+    }
   }
+  const uint32_t lane_off = (OCTETS ? key_token(c) * kD : 0) + key_offset(c, g);
+  const int head = column_head(c, G), copy = column_copy(c, G);
   Query8<T, G> qb;
   int unit_now = -1, n = 0, n_slots = 0;
   size_t row0 = 0;
@@ -51,6 +56,7 @@ __global__ __launch_bounds__(kScoreThreads) void decode8_scores_kernel(const Sco
       if (in_lds) {
         l_unit = lane_last_at_most((const int*)pre_lds, A.U, unit0, my_it, it1 - 1);
         l_grp = my_it - pre_lds[l_unit];
+        if (MODE == kPerHead && part.count != 1) l_grp += part_first(part, l_unit / ratio, (unit_slots<MODE>(A, l_unit) + gp - 1) / gp);
       } else {
         l_unit = lane_last_at_most(A.pre_g, A.U, unit0, my_it, it1 - 1);
         l_grp = my_it - A.pre_g[l_unit];
@@ -65,19 +71,22 @@ __global__ __launch_bounds__(kScoreThreads) void decode8_scores_kernel(const Sco
       l_scale = A8.k_scale[l_page];
     }
     auto of_slot = [&](int v, int in, int slot) {
-      return TILED ? __builtin_amdgcn_readlane(v, in * gp + slot) : __shfl(v, in * gp + slot);
+      return OCTETS ? __builtin_amdgcn_readlane(v, in * gp + slot) : __shfl(v, in * gp + slot);
     };
-    for (int it = it0; it < it1; ++it) {
-      const int in = it - it0;
-      const int unit = __builtin_amdgcn_readlane(l_unit, in * gp), grp = __builtin_amdgcn_readlane(l_grp, in * gp);
-      KeyTile k[4];
-      float scale[4];
+    // chunk ck of the batch: octets 4 (ck % 2) .. 4 (ck % 2) + 3 of item ck / 2
+    const int n_ck = (it1 - it0) * 2;
+    auto request = [&](int ck, auto half, uint4 (&k)[4]) {
+      constexpr int h = decltype(half)::value;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int page = of_slot(l_page, in, k_slot[t]);
-        scale[t] = __int_as_float(of_slot(__float_as_int(l_scale), in, k_slot[t]));
-        load_keys<STREAM>(k_pool + ((size_t)page * P + k_tok[t]) * kD + 16 * g, k[t]);
+      for (int o = 0; o < 4; ++o) {
+        const int page = of_slot(l_page, ck >> 1, k_slot[4 * h + o]);
+        k[o] = load16<STREAM>(k_pool + ((size_t)page * P + k_tok[4 * h + o]) * kD + lane_off);
       }
+    };
+    int grp = 0, stored = 0;
+    auto open_item = [&](int in) {
+      const int unit = __builtin_amdgcn_readlane(l_unit, in * gp);
+      grp = __builtin_amdgcn_readlane(l_grp, in * gp);
       if (unit != unit_now) {
         unit_now = unit;
         const int b = GROUPED ? unit / A.Hkv : unit / A.Hq;
@@ -86,50 +95,70 @@ __global__ __launch_bounds__(kScoreThreads) void decode8_scores_kernel(const Sco
         n_slots = DENSE ? clampi((n + P - 1) / P, 0, A.Mmax) : clampi(uniform_load(A.n_sel + unit), 0, A.cap);
         qb.load(q + row0 * kD);
       }
-      f32x4_t z[4];
-      float top = -INFINITY;
-      const int stored = min(GT, (n_slots - grp * gp) * P);             // tokens of the group that the row has
+      stored = min(GT, (n_slots - grp * gp) * P);                       // tokens of the group that the row has
+    };
+    float top = -INFINITY;
+    auto consume = [&](int ck, auto half, const uint4 (&k)[4]) {
+      constexpr int h = decltype(half)::value;
+      const int in = ck >> 1;
+      float2 z[4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        z[t] = tile_scores<T, G>(k[t], scale[t], qb);
-        const int left = 16 * t + 4 * g < stored ? n - (of_slot(l_lp, in, z_slot[t]) * P + z_tok[t]) : 0;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          z[t][r] = r < left ? A.zscale * z[t][r] : -INFINITY;
-          top = fmaxf(top, z[t][r]);
-        }
+      for (int o = 0; o < 4; ++o) {
+        octet_scores<T, G>(k[o], __int_as_float(of_slot(__float_as_int(l_scale), in, k_slot[4 * h + o])), qb, z[o].x, z[o].y);
+        const int p = 32 * h + 8 * o + 2 * g;
+        const int left = p < stored ? n - (of_slot(l_lp, in, z_slot[4 * h + o]) * P + z_tok[4 * h + o] + (OCTETS ? 2 * g : 0)) : 0;
+        z[o].x = left > 0 ? A.zscale * z[o].x : -INFINITY;
+        z[o].y = left > 1 ? A.zscale * z[o].y : -INFINITY;
+        top = fmaxf(top, fmaxf(z[o].x, z[o].y));
       }
-      float* zrow = A.zbuf + (row0 + c % G) * A.zstride + (size_t)grp * GT + 4 * g;
-      const int copy = c / G;
+      // copy i of a head stores octet i: a whole line per head where there are four copies
+      float* zrow = A.zbuf + (row0 + head) * A.zstride + (size_t)grp * GT + 32 * h + 2 * g;
 #pragma unroll
-      for (int round = 0; round < (G == 8 ? 2 : 1); ++round) {
-        const int t = G == 8 ? 2 * round + copy : copy;
-        f32x4_t v;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float a = copy & 1 ? z[2 * round + 1][r] : z[2 * round][r], d = copy & 1 ? z[3][r] : z[2][r];
-          v[r] = G != 8 && (copy & 2) ? d : a;
-        }
-        if (t < 4 && 16 * t + 4 * g < stored) *reinterpret_cast<f32x4_t*>(zrow + 16 * t) = v;
+      for (int o = 0; o < 4; o += G == 8 ? 2 : 4) {
+        const float2 v = copy_pair<G>(z[o], z[o + 1], z[2], z[3], copy);
+        if (copy < 4 && 32 * h + 8 * (o + copy) + 2 * g < stored) *reinterpret_cast<float2*>(zrow + 8 * (o + copy)) = v;
       }
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      if (lane < G) A.pmax[(row0 + lane) * A.n_chunks_max + grp] = top;
+      if (h == 1) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (g == 0 && copy == 0) A.pmax[(row0 + head) * A.n_chunks_max + grp] = top;
+        top = -INFINITY;
+      }
+    };
+    // two chunks (4 KB each) in flight, in alternating registers; every request of the loop is unconditional, so that no wait
+    // at a join drains them, and the last pair is taken after it
+    uint4 k0[4], k1[4];
+    request(0, IntC<0>{}, k0);
+    int ck = 0;
+    for (; ck + 2 < n_ck; ck += 2) {
+      open_item(ck >> 1);
+      __builtin_amdgcn_sched_barrier(0);
+      request(ck + 1, IntC<1>{}, k1);
+      __builtin_amdgcn_sched_barrier(0);
+      consume(ck, IntC<0>{}, k0);
+      request(ck + 2, IntC<0>{}, k0);
+      __builtin_amdgcn_sched_barrier(0);
+      consume(ck + 1, IntC<1>{}, k1);
     }
+    open_item(ck >> 1);
+    request(ck + 1, IntC<1>{}, k1);
+    __builtin_amdgcn_sched_barrier(0);
+    consume(ck, IntC<0>{}, k0);
+    consume(ck + 1, IntC<1>{}, k1);
   }
 }
 
 template <typename T, int G, int MODE>
 static void launch_G(const Dims& dm, const Score8Args& a, bool stream, dim3 grid, size_t lds, hipStream_t st) {
   const dim3 block(kScoreThreads);
-  const bool tiled = dm.P % 16 == 0;
+  const bool octets = dm.P % 8 == 0;
   if constexpr (MODE != kPerHead)
     if (stream) {
-      if (tiled) hipLaunchKernelGGL((decode8_scores_kernel<T, G, MODE, true, true>), grid, block, lds, st, a);
+      if (octets) hipLaunchKernelGGL((decode8_scores_kernel<T, G, MODE, true, true>), grid, block, lds, st, a);
       else hipLaunchKernelGGL((decode8_scores_kernel<T, G, MODE, false, true>), grid, block, lds, st, a);
       return;
     }
-  if (tiled) hipLaunchKernelGGL((decode8_scores_kernel<T, G, MODE, true, false>), grid, block, lds, st, a);
+  if (octets) hipLaunchKernelGGL((decode8_scores_kernel<T, G, MODE, true, false>), grid, block, lds, st, a);
   else hipLaunchKernelGGL((decode8_scores_kernel<T, G, MODE, false, false>), grid, block, lds, st, a);
 }
 template <typename T>
@@ -152,9 +181,15 @@ void launch_scores8(const Dims& dm, int mode, ScoreArgs sa, const float* k_scale
   const int gp = pmax_pages(dm.P);
   const long long items = (long long)sa.U * (((mode == kAllPages ? dm.Mmax : dm.cap) + gp - 1) / gp);
   long long wgs = (items + kScoreWaves - 1) / kScoreWaves;
-  const long long most = (long long)device_compute_units() * 16;
+  // Lists: the workgroups that a compute unit holds at a time (entmax over 2 % of a million tokens, a list per head: 18.2 us, with
+  // four times as many 21.0).  All pages: four times as many (4 x 128K tokens 102.7 us, 108 without; 32 per compute unit 107).
+  const long long most = (long long)device_compute_units() * (mode == kAllPages ? 16 : 4);
   if (wgs > most) wgs = most;
   const bool pre_global = sa.U > kUnitsLdsMax;
+  // lists of the heads of a group are split over the XCDs as in decode.hip, by the same rule
+  const bool split = mode == kPerHead && dm.G > 1 && !pre_global && 3 * wgs * kScoreWaves >= 2ll * kXcds * sa.U;
+  sa.parts = split ? kXcds : 1;
+  if (split) wgs = (wgs + kXcds - 1) / kXcds * kXcds;
   if (pre_global) {
     sa.pre_g = pre_ws;
     launch_unit_prefix(mode, sa, pre_ws, st);
@@ -162,6 +197,7 @@ void launch_scores8(const Dims& dm, int mode, ScoreArgs sa, const float* k_scale
   const long long k_bytes = (long long)sa.U * (mode == kAllPages ? dm.Mmax : dm.cap) * dm.P * kD;
   const bool stream = mode != kPerHead && k_bytes >= kStreamKBytes;
   const Score8Args a{sa, k_scale};
+  if (mode == kAllPages && launch_scores8_windows(dm, a, items, k_bytes, st)) return;
   const size_t lds = pre_global ? 0 : (size_t)(sa.U + 1) * sizeof(int);
   const dim3 grid((unsigned)wgs);
   if (dm.dtype == EKV_F32) launch_T<float>(dm, mode, a, stream, grid, lds, st);

@@ -1,12 +1,12 @@
 // Softmax attention of one query token per sequence over the 8-bit cache: every page, or a page list per query head.
 //
 // One pass over K and V with the running maximum and sum; scores and weighted values both go through the matrix cores
-// (ekv_attn8.h has the scores' tiles).  Steps of 32 tokens, two tiles: lane (c, g) then holds the scores of head c % G for tokens
-// 4g..4g+3 of either tile, and that is the layout in which the next product wants its rows (row c, eight tokens of group g),
-// so the weights go from one product to the next without leaving the lane.  Float32 weights are three bf16 terms that
-// sum to them exactly (8 + 8 + 8 bits); the columns that repeat the heads hold them: copy 0 of the heads contributes the first
-// term, copy 1 the second, copy 2 the third, as rows of one product (with eight heads there are two copies and a second
-// product).  Values are 8 bytes of each token's row per lane, transposed in pairs of tokens by byte permutes and widened with
+// (ekv_attn8.h has the scores).  Steps of 32 tokens, four octets: lane (c, g) then holds the scores of its head for tokens 2g and
+// 2g + 1 of each, and that is the layout in which the next product wants its rows (row c, eight tokens of group g), so the weights
+// go from one product to the next without leaving the lane.  Float32 weights are three bf16 terms that sum to them exactly
+// (8 + 8 + 8 bits); the columns that repeat the heads hold them: copy 0 of a head contributes the first term, copy 1 the
+// second, copy 2 the third, as rows of one product (eight heads have two copies and take a second product).  Values are 8
+// bytes of each token's row per lane, whole lines per load, transposed in pairs of tokens by byte permutes and widened with
 // their page's scale (exact), so that sums are float32 sums of exact products.
 // The maximum only has to keep exp in range: it is brought up to date, with the exchange and the rescaling that takes, when a
 // score passes it by more than 2^kSlack, not at every step.
@@ -41,24 +41,31 @@ __global__ __launch_bounds__(1024) void attn8_prefix_kernel(const Attn8Args A) {
   block_exclusive_prefix<1024>(A.s.U, [&](int u) { return unit_steps<DENSE>(A.s, u); }, A.pre, wsum);
 }
 
-// A step's data as loaded.  K: token c of either tile; V: channels 8c..8c+7 of tokens 4g..4g+3 of either tile.
+// A step's data as loaded.  K: the lane's codes of each octet; V: channels 8c..8c+7 of tokens 2g, 2g + 1 of each.
 struct Step8 {
-  KeyTile k[2];
+  uint4 k[4];
   uint2 v[8];
-  float ks[2], vs[2];
-  int left[2];                                   // valid tokens from the lane's first on (4 or more: all)
+  float ks[4], vs[4];
+  int left[4];                                   // valid tokens from the lane's first of an octet on (2 or more: both)
 };
+template <bool STREAM> __device__ __forceinline__ uint2 load8b(const e4m3_t* p) {
+  typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+  if constexpr (STREAM) return __builtin_bit_cast(uint2, __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(p)));
+  else return *reinterpret_cast<const uint2*>(p);
+}
 
-template <typename T, int G, bool DENSE, bool TILED>
-__global__ __launch_bounds__(kAttnThreads) void attn8_kernel(const Attn8Args AA) {
+template <typename T, int G, bool DENSE, bool OCTETS, bool STREAM>
+__global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2)))
+void attn8_kernel(const Attn8Args AA) {
   const ScoreArgs& A = AA.s;
   extern __shared__ int pre_lds[];
   __shared__ int wsum[kAttnWaves];
   __shared__ float s_o[kAttnWaves][G][kD];
   __shared__ float s_m[kAttnWaves][G], s_l[kAttnWaves][G];
   const int P = A.P, lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const e4m3_t* k_pool = (const e4m3_t*)A.k_pool + 16 * g;
-  const e4m3_t* v_pool = AA.v_pool + 8 * c;
+  const e4m3_t* k_pool = (const e4m3_t*)A.k_pool;
+  const uint32_t k_off = (OCTETS ? key_token(c) * kD : 0) + key_offset(c, g), v_off = (OCTETS ? 2 * g * kD : 0) + 8 * c;
+  const int head = column_head(c, G), copy = column_copy(c, G);
   const bool in_lds = A.pre_g == nullptr;
   int first_unit, begin, end;
   auto range = [&](auto pre) {                   // this workgroup's steps
@@ -76,8 +83,8 @@ __global__ __launch_bounds__(kAttnThreads) void attn8_kernel(const Attn8Args AA)
     range(A.pre_g);
   }
   const int last = (DENSE ? A.Mmax : A.cap) - 1;
-  const uint32_t take1 = c / G >= 1 ? 0xffff0000u : 0u, take2 = c / G >= 2 ? 0xffff0000u : 0u;
-  const uint32_t keep = c / G < 3 ? ~0u : 0u, first = c / G == 0 ? ~0u : 0u;
+  const uint32_t take1 = copy >= 1 ? 0xffff0000u : 0u, take2 = copy >= 2 ? 0xffff0000u : 0u;
+  const uint32_t keep = copy < 3 ? ~0u : 0u, first = copy == 0 ? ~0u : 0u;
 
   int unit = first_unit;
   for (int at = begin; at < end;) {
@@ -118,52 +125,48 @@ __global__ __launch_bounds__(kAttnThreads) void attn8_kernel(const Attn8Args AA)
         const int p0 = st * kStep;
         if ((int)page_div((uint32_t)(p0 + kStep - 1), AA.page_div) >= slot_base + 64) look_up(p0);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if constexpr (TILED) {
-            const int slot = uniform((int)page_div((uint32_t)(p0 + 16 * t), AA.page_div)), tok = p0 + 16 * t - slot * P, sl = slot - slot_base;
+        for (int o = 0; o < 4; ++o) {
+          if constexpr (OCTETS) {
+            const int p = p0 + 8 * o, slot = uniform((int)page_div((uint32_t)p, AA.page_div)), tok = p - slot * P, sl = slot - slot_base;
             const int page = __builtin_amdgcn_readlane(l_page, sl);
-            x.ks[t] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l_ks), sl));
-            x.vs[t] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l_vs), sl));
-            const size_t row = (size_t)page * P + tok;
-            load_keys<false>(k_pool + (row + c) * kD, x.k[t]);
+            const size_t at = ((size_t)page * P + tok) * kD;
+            x.k[o] = load16<STREAM>(k_pool + at + k_off);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x.v[4 * t + j] = *reinterpret_cast<const uint2*>(v_pool + (row + 4 * g + j) * kD);
-            const int lp = __builtin_amdgcn_readlane(l_lp, sl);
-            x.left[t] = p0 + 16 * t < n_pos ? n - (lp * P + tok) - 4 * g : 0;
+            for (int e = 0; e < 2; ++e) x.v[2 * o + e] = load8b<STREAM>(AA.v_pool + at + v_off + e * kD);
+            x.ks[o] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l_ks), sl));
+            x.vs[o] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l_vs), sl));
+            x.left[o] = p < n_pos ? n - (__builtin_amdgcn_readlane(l_lp, sl) * P + tok) - 2 * g : 0;
           } else {
-            const int pk = p0 + 16 * t + c, pv = p0 + 16 * t + 4 * g;
+            const int pk = p0 + 8 * o + key_token(c), pv = p0 + 8 * o + 2 * g;
             const int sk = (int)page_div((uint32_t)pk, AA.page_div), sv = (int)page_div((uint32_t)pv, AA.page_div);
-            const int page_k = __shfl(l_page, sk - slot_base), page_v = __shfl(l_page, sv - slot_base);
-            x.ks[t] = __shfl(l_ks, sk - slot_base);
-            x.vs[t] = __shfl(l_vs, sv - slot_base);
-            load_keys<false>(k_pool + ((size_t)page_k * P + (pk - sk * P)) * kD, x.k[t]);
-            const size_t row = (size_t)page_v * P + (pv - sv * P);
+            x.k[o] = load16<STREAM>(k_pool + ((size_t)__shfl(l_page, sk - slot_base) * P + (pk - sk * P)) * kD + k_off);
+            const size_t at = ((size_t)__shfl(l_page, sv - slot_base) * P + (pv - sv * P)) * kD;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x.v[4 * t + j] = *reinterpret_cast<const uint2*>(v_pool + (row + j) * kD);
-            const int lp = __shfl(l_lp, sv - slot_base);
-            x.left[t] = pv < n_pos ? n - (lp * P + (pv - sv * P)) : 0;
+            for (int e = 0; e < 2; ++e) x.v[2 * o + e] = load8b<STREAM>(AA.v_pool + at + v_off + e * kD);
+            x.ks[o] = __shfl(l_ks, sk - slot_base);
+            x.vs[o] = __shfl(l_vs, sv - slot_base);
+            x.left[o] = pv < n_pos ? n - (__shfl(l_lp, sv - slot_base) * P + (pv - sv * P)) : 0;
           }
         }
       };
       auto consume = [&](Step8& x) {
-        f32x4_t z[2];
+        float2 z[4];
         float top = -INFINITY;
+        bool some_out = false;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          z[t] = tile_scores<T, G>(x.k[t], x.ks[t], qb);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            z[t][r] = r < x.left[t] ? A.zscale * z[t][r] : -INFINITY;
-            top = fmaxf(top, z[t][r]);
-          }
+        for (int o = 0; o < 4; ++o) {
+          octet_scores<T, G>(x.k[o], x.ks[o], qb, z[o].x, z[o].y);
+          z[o].x = x.left[o] > 0 ? A.zscale * z[o].x : -INFINITY;
+          z[o].y = x.left[o] > 1 ? A.zscale * z[o].y : -INFINITY;
+          top = fmaxf(top, fmaxf(z[o].x, z[o].y));
+          some_out |= x.left[o] < 2;
         }
-        if (__any(x.left[0] < 4 || x.left[1] < 4)) {           // what a page holds behind the last token counts for nothing, NaN too
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (j % 4 >= x.left[j / 4]) x.v[j] = make_uint2(0u, 0u);
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-            if (x.left[t] <= 0) x.vs[t] = 1.f;               // ... nor does the scale of a page that nobody has
+        if (__any(some_out)) {                               // what a page holds behind the last token counts for nothing, NaN too,
+#pragma unroll                                               // nor does the scale of a page that nobody has
+          for (int o = 0; o < 4; ++o) {
+            if (x.left[o] < 2) x.v[2 * o + 1] = make_uint2(0u, 0u);
+            if (x.left[o] < 1) { x.v[2 * o] = make_uint2(0u, 0u); x.vs[o] = 1.f; }
+          }
         }
         if (__any(top > m + kSlack)) {
           top = fmaxf(top, __shfl_xor(top, 16));
@@ -184,26 +187,23 @@ __global__ __launch_bounds__(kAttnThreads) void attn8_kernel(const Attn8Args AA)
         const float m_use = m > -INFINITY ? m : 0.f;
         u32x4_t pa, pb;                                      // rows of the second product: this lane's term of its head's weights
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int o = 0; o < 4; ++o) {
+          uint32_t bits[2], low[2];
 #pragma unroll
-          for (int r = 0; r < 4; r += 2) {
-            uint32_t bits[2], low[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float p = __builtin_amdgcn_exp2f(z[t][r + e] - m_use);
-              l += p;
-              float y = p - __uint_as_float(__float_as_uint(p) & take1);
-              if constexpr (G == 8) {
-                const float rest = p - __uint_as_float(__float_as_uint(p) & 0xffff0000u);
-                low[e] = __float_as_uint(rest - __uint_as_float(__float_as_uint(rest) & 0xffff0000u));
-              } else {
-                y -= __uint_as_float(__float_as_uint(y) & take2);
-              }
-              bits[e] = __float_as_uint(y) & keep;
+          for (int e = 0; e < 2; ++e) {
+            const float p = __builtin_amdgcn_exp2f((e ? z[o].y : z[o].x) - m_use);
+            l += p;
+            float y = p - __uint_as_float(__float_as_uint(p) & take1);
+            if constexpr (G == 8) {
+              const float rest = p - __uint_as_float(__float_as_uint(p) & 0xffff0000u);
+              low[e] = __float_as_uint(rest - __uint_as_float(__float_as_uint(rest) & 0xffff0000u));
+            } else {
+              y -= __uint_as_float(__float_as_uint(y) & take2);
             }
-            pa[2 * t + r / 2] = __builtin_amdgcn_perm(bits[1], bits[0], 0x07060302u);
-            if constexpr (G == 8) pb[2 * t + r / 2] = __builtin_amdgcn_perm(low[1], low[0], 0x07060302u) & first;
+            bits[e] = __float_as_uint(y) & keep;
           }
+          pa[o] = __builtin_amdgcn_perm(bits[1], bits[0], 0x07060302u);
+          if constexpr (G == 8) pb[o] = __builtin_amdgcn_perm(low[1], low[0], 0x07060302u) & first;
         }
         // channel 8c + i of tokens 0..7 of the lane, i = 0..7: pairs of tokens side by side, then widened
 #pragma unroll
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn8_kernel(const Attn8Args AA)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const uint32_t src = i < 2 ? lo[j] : hi[j];
-              vb[j] = i & 1 ? widen2<true>(src, x.vs[j / 2]) : widen2<false>(src, x.vs[j / 2]);
+              vb[j] = i & 1 ? widen2<true>(src, x.vs[j]) : widen2<false>(src, x.vs[j]);
             }
             const bf16x8_t vv = __builtin_bit_cast(bf16x8_t, vb);
             f32x4_t& d = acc[4 * half + i];
@@ -240,24 +240,23 @@ __global__ __launch_bounds__(kAttnThreads) void attn8_kernel(const Attn8Args AA)
         consume(x1);
       }
     }
-    // the wavefront's sums: rows h + G * term of the second product belong to head h
+    // the wavefront's sums: row r of the second product is of head column_head(r), whose rows are pairs (the copies c % 2)
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     __syncthreads();                                         // the previous segment's partial results have been read
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      f32x4_t s = acc[i];
-      if constexpr (G == 1) { s[0] += s[1]; s[2] += s[3]; s[0] += s[2]; }
-      if constexpr (G == 2) { s[0] += s[2]; s[1] += s[3]; }
-      constexpr int R = G < 4 ? G : 4;
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        if constexpr (G < 8) s[r] += __shfl_xor(s[r], 16);
-        s[r] += __shfl_xor(s[r], 32);
-        if (g < (G == 8 ? 2 : 1)) s_o[w][4 * g + r][8 * c + i] = s[r];
+      float even = acc[i][0] + acc[i][1], odd = acc[i][2] + acc[i][3];
+      if constexpr (G == 1) even += odd;
+      if constexpr (G <= 2) { even += __shfl_xor(even, 16); odd += __shfl_xor(odd, 16); }
+      if constexpr (G <= 4) { even += __shfl_xor(even, 32); odd += __shfl_xor(odd, 32); }
+      constexpr int kGroups = G >= 2 ? G / 2 : 1;
+      if (g < kGroups) {
+        s_o[w][G >= 2 ? 2 * g : 0][8 * c + i] = even;
+        if constexpr (G >= 2) s_o[w][2 * g + 1][8 * c + i] = odd;
       }
     }
-    if (lane < G) { s_m[w][lane] = m; s_l[w][lane] = l; }
+    if (g == 0 && copy == 0) { s_m[w][head] = m; s_l[w][head] = l; }
     __syncthreads();
     const bool whole = at == u_begin && seg_end == u_end;    // the unit is this workgroup's alone: no record, no join
     float* rec = AA.part + (size_t)(blockIdx.x + unit) * G * kRec;
@@ -334,8 +333,11 @@ __global__ __launch_bounds__(kJoinGroups * kD) void attn8_join_kernel(const Attn
   }
 }
 
-// Workgroups: four per compute unit, no more than there can be steps for their wavefronts.  Workspaces are sized for kMostWgs.
-constexpr int kMostWgs = 1024;
+// Workgroups: the two that a compute unit holds, no more than there can be steps for their wavefronts.  With four a compute unit,
+// half of which wait for the others to end, 8 x 128K tokens for 64 heads take 315 us for 299, lists of 4 x 128K 42.6 for 37.1;
+// compiled for three or four wavefronts per SIMD (and as many workgroups) 306 / 39.9 and, with spills, 513 / 67.
+// Workspaces are sized for kMostWgs.
+constexpr int kMostWgs = 512;
 static long long attn8_units(const Dims& dm, bool dense) { return (long long)dm.B * (dense ? dm.Hkv : dm.Hq); }
 static int attn8_grid(const Dims& dm, bool dense, int most) {
   const long long steps = attn8_units(dm, dense) * (((long long)(dense ? dm.Mmax : dm.cap) * dm.P + kStep - 1) / kStep);
@@ -349,17 +351,28 @@ size_t softmax8_ws_bytes(const Dims& dm, bool dense) {
   return attn8_pre_bytes(dm, dense) + recs * (dense ? dm.G : 1) * kRec * sizeof(float);
 }
 
+static void launch_join(const Attn8Args& a, int G, int W, hipStream_t st) {
+  hipLaunchKernelGGL(attn8_join_kernel, dim3(a.s.U * G), dim3(kJoinGroups * kD), 0, st, a, G, W);
+}
 template <typename T, int G, bool DENSE>
 static void launch_attn8(const Dims& dm, Attn8Args a, hipStream_t st) {
-  const int cus = device_compute_units(), W = attn8_grid(dm, DENSE, 4 * cus < kMostWgs ? 4 * cus : kMostWgs);
+  const int cus = device_compute_units(), W = attn8_grid(dm, DENSE, 2 * cus < kMostWgs ? 2 * cus : kMostWgs);
   if (a.s.U > kUnitsLdsMax) {
     hipLaunchKernelGGL(attn8_prefix_kernel<DENSE>, dim3(1), dim3(1024), 0, st, a);
     a.s.pre_g = a.pre;
   }
   const size_t lds = a.s.pre_g != nullptr ? 0 : (size_t)(a.s.U + 1) * sizeof(int);
-  if (dm.P % 16 == 0) hipLaunchKernelGGL((attn8_kernel<T, G, DENSE, true>), dim3(W), dim3(kAttnThreads), lds, st, a);
-  else hipLaunchKernelGGL((attn8_kernel<T, G, DENSE, false>), dim3(W), dim3(kAttnThreads), lds, st, a);
-  hipLaunchKernelGGL(attn8_join_kernel, dim3(a.s.U * G), dim3(kJoinGroups * kD), 0, st, a, G, W);
+  const dim3 grid(W), block(kAttnThreads);
+  if constexpr (DENSE)
+    if (2ll * a.s.U * dm.Mmax * dm.P * kD >= kStreamKBytes) {
+      if (dm.P % 8 == 0) hipLaunchKernelGGL((attn8_kernel<T, G, true, true, true>), grid, block, lds, st, a);
+      else hipLaunchKernelGGL((attn8_kernel<T, G, true, false, true>), grid, block, lds, st, a);
+      launch_join(a, G, W, st);
+      return;
+    }
+  if (dm.P % 8 == 0) hipLaunchKernelGGL((attn8_kernel<T, G, DENSE, true, false>), grid, block, lds, st, a);
+  else hipLaunchKernelGGL((attn8_kernel<T, G, DENSE, false, false>), grid, block, lds, st, a);
+  launch_join(a, G, W, st);
 }
 template <typename T>
 static void launch_attn8_T(const Dims& dm, bool dense, const Attn8Args& a, hipStream_t st) {

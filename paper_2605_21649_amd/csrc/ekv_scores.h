@@ -65,6 +65,15 @@ struct Part { int index, count; };             // this workgroup's part, parts p
 __device__ __forceinline__ Part unit_part(const ScoreArgs& A) {
   return {A.parts == kXcds ? (int)(blockIdx.x % kXcds) : 0, A.parts};
 }
+// first item of a unit of n items that belongs to the part
+__device__ __forceinline__ int part_first(const Part& p, int group, int n) {
+  return p.count == 1 ? 0 : (int)(((unsigned)n * (unsigned)((p.index + group) % kXcds)) / kXcds);
+}
+__device__ __forceinline__ int part_length(const Part& p, int group, int n) {
+  if (p.count == 1) return n;
+  const unsigned i = (unsigned)((p.index + group) % kXcds);
+  return (int)((unsigned)n * (i + 1) / kXcds - (unsigned)n * i / kXcds);
+}
 // The item range of this wavefront and the unit its first item lies in.
 struct WaveItems { int begin, end, unit; };
 template <typename P>

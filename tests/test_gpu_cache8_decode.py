@@ -269,3 +269,42 @@ def test_same_inputs_same_bits():
             run_full(c, kind)
             seen.append((c.out.clone(), c.tau.clone()))
         assert all(torch.equal(a.view(torch.int32), b.view(torch.int32)) for s in seen[1:] for a, b in zip(seen[0], s))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", [(8, 8), (16, 8), (32, 8), (64, 8)])
+@pytest.mark.parametrize("page", [8, 16, 32, 64])
+def test_large_calls_are_those_of_their_sequences_alone(page, heads, dtype):
+    """A batch whose K (over 64 MiB) takes the score pass that holds its stores back, with a sequence that begins and ends anywhere
+    in a wavefront's range, an empty one and single tokens, against the sequences one by one: the same sums, to the last bit."""
+    lens = [40011, 1, 0, 33, 25000 + page, 3 * page - 1, 8192]
+    B, Hq, Hkv = len(lens), *heads
+    M = -(-max(lens) // page)
+    g = torch.Generator(device="cuda").manual_seed(page)
+    n_phys = B * M
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    q = torch.randn(B, Hq, D, generator=g, device="cuda").to(dt)
+    kp, vp = (torch.randint(0, 127, (n_phys, Hkv, page, D), generator=g, device="cuda", dtype=torch.uint8) % 0x60 | (
+        torch.randint(0, 2, (n_phys, Hkv, page, D), generator=g, device="cuda", dtype=torch.uint8) << 7) for _ in range(2))
+    ks, vs = (2.0 ** torch.randint(-6, -2, (n_phys, Hkv), generator=g, device="cuda").float() for _ in range(2))
+    table = torch.randperm(n_phys, generator=g, device="cuda").view(B, M).to(torch.int32)
+    assert B * Hkv * M * page * D >= 64 << 20
+
+    def run(rows, m):
+        cfg = ekv.make_config(len(rows), Hq, Hkv, D, page, dtype, 1.5, 0.02, m, m)
+        out, tau, supp = torch.zeros(len(rows), Hq, D, device="cuda"), torch.zeros(len(rows), Hq, device="cuda"), torch.zeros(len(rows), Hq, dtype=torch.int32, device="cuda")
+        ws = torch.empty(ekv.ekv_workspace_bytes(cfg, ekv.EKV_OP_DECODE_FULL), dtype=torch.uint8, device="cuda")
+        t, n = table[rows][:, :m].contiguous(), torch.tensor([lens[b] for b in rows], dtype=torch.int32, device="cuda")
+        ekv.ekv_decode8_full(cfg, q[rows].contiguous(), ekv.cache8_view(kp, vp, ks, vs, t, n), out, tau, supp, ws)
+        torch.cuda.synchronize()
+        return out, tau, supp
+
+    whole = run(list(range(B)), M)
+    for b in range(B):
+        m = max(1, min(M, -(-lens[b] // page)))
+        if Hkv * m * page * D >= 64 << 20:
+            m = M
+        one = run([b], m)
+        for x, y in zip(whole[1:], one[1:]):
+            assert torch.equal(x[b:b + 1].view(torch.int32), y.view(torch.int32)), b
+        assert torch.allclose(whole[0][b], one[0][0], rtol=0, atol=2e-6 * float(one[0].abs().max()) + 1e-12)
