@@ -166,7 +166,9 @@ __global__ __launch_bounds__(kMapThreads) void release_pages_kernel(const Releas
 // of the whole run before the first code can be written.  Lane (r, c) has channels 8c..8c+7 of the page's rows r, r + 4, ..:
 // whole lines with every load and store, and the rows' order of ekv_stats_build in the sums of the statistics, which are taken
 // from the stored values and equal that call's to the last bit.  A lane reads and writes the same rows of the page, so older
-// tokens that a grown scale rounds again need no exchange.  Bound by the new rows' bytes.
+// tokens that a grown scale rounds again need no exchange.  Rows of a chunk that the run does not have are read as one that
+// it has, which no maximum or minimum minds.  The bytes are the new rows'; the conversions with a scale leave about ten
+// instructions to an element of K with its statistics and three to one of V, without which the arithmetic was what bounded it.
 constexpr int kAppendThreads = 256, kAppendWaves = kAppendThreads / 64;
 
 struct AppendArgs {
@@ -178,7 +180,30 @@ struct AppendArgs {
   int64_t n_slots;                               // slots of the pool
 };
 
-template <typename T>
+// Sum, minimum or maximum over the four rows of lanes of 8 values each: lane (r, c) gets entries e and e + 1, e = 2 (r / 2) + 4 (r % 2).
+// The pairs are those of exchanges over 16 and then 32 lanes; each step passes on the half of the entries that the other needs.
+template <typename F> __device__ __forceinline__ float2 rows_reduce(const float (&x)[8], F&& f) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[i]), __float_as_uint(x[i + 4]), false, false);
+    y[i] = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
+  float z[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(y[i]), __float_as_uint(y[i + 2]), false, false);
+    z[i] = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
+  return make_float2(z[0], z[1]);
+}
+__device__ __forceinline__ void store2(float* p, float2 v) { *reinterpret_cast<float2*>(p) = v; }
+__device__ __forceinline__ void store2(bf16_t* p, float2 v) {
+  *reinterpret_cast<uint32_t*>(p) = float_to_bf16_bits(v.x) | ((uint32_t)float_to_bf16_bits(v.y) << 16);
+}
+
+// ONE: pages of up to 16 tokens, one chunk (its registers let four wavefronts share a SIMD).
+template <typename T, bool ONE>
 __device__ __forceinline__ void append_run(const AppendArgs& A, int side, int h, int row0, int len, uint32_t slot) {
   const int lane = threadIdx.x & 63, r = lane >> 4, c = lane & 15;
   const int P = A.P, t0 = (int)(slot % (uint32_t)P), cnt = t0 + len;
@@ -187,102 +212,149 @@ __device__ __forceinline__ void append_run(const AppendArgs& A, int side, int h,
   float* scale = A.scale[side] + page;
   const T* x = (const T*)A.x[side] + (int64_t)row0 * A.stride[side] + h * kD + 8 * c;
   const bool stats = side == 0 && A.box != nullptr;
-  const float s_was = t0 > 0 ? *scale : 0.f;
-  // sixteen rows of the page at a time; rows that are not the run's read one that is
+  // sixteen rows of the page at a time
   Raw8<T> raw[4];
+  Raw8<e4m3_t> old[4];
+  // whether four rows of a chunk hold one of the run's, or one of the page's at all (wave-uniform: a step's single token has one
+  // such four, and what the page does not hold yet costs nothing)
+  auto any_new = [&](int chunk, int s) { return 16 * chunk + 4 * s + 3 >= t0 && 16 * chunk + 4 * s < cnt; };
+  auto any_old = [&](int chunk, int s) { return 16 * chunk + 4 * s < t0; };
   auto request = [&](int chunk) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) load_raw8(x + (int64_t)min(max(16 * chunk + 4 * s + r - t0, 0), len - 1) * A.stride[side], raw[s]);
+    for (int s = 0; s < 4; ++s)
+      if (any_new(chunk, s)) load_raw8(x + (int64_t)min(max(16 * chunk + 4 * s + r - t0, 0), len - 1) * A.stride[side], raw[s]);
   };
-  const int first = t0 / 16, last = (cnt - 1) / 16;
-  float top = 0.f;
+  auto request_old = [&](int chunk) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      if (any_old(chunk, s)) load_raw8(codes + (size_t)min(16 * chunk + 4 * s + r, t0 - 1) * kD, old[s]);
+  };
+  const int first = ONE ? 0 : t0 / 16, last = ONE ? 0 : (cnt - 1) / 16;
+  const float s_was = t0 > 0 ? *scale : 0.f;
+  int b = -1, lp = -1;
+  if (stats) { b = A.seq[row0]; lp = A.pos[row0]; }
+  uint32_t top = 0;
   for (int chunk = last; chunk >= first; --chunk) {        // downwards: the first chunk's rows stay in the registers
     request(chunk);
+    if (chunk == first && stats && t0 > 0) request_old(0);
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      float v[8];
-      widen8(raw[s], v);
+    for (int s = 0; s < 4; ++s)
+      if (any_new(chunk, s)) top = max_bits(raw[s], top);
+  }
+  top = wave_max_u(max_as_float_bits<T>(top));
+  if (top >= 0x7f800000u) {                                // infinities or NaN among them: once more without
+    float m = 0.f;
+    for (int chunk = last; chunk >= first; --chunk) {
+      if constexpr (!ONE) request(chunk);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float m = __builtin_fabsf(v[i]);
-        top = fmaxf(top, m < INFINITY ? m : 0.f);
+      for (int s = 0; s < 4; ++s) {
+        if (!any_new(chunk, s)) continue;
+        float v[8];
+        widen8(raw[s], v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float f = __builtin_fabsf(v[i]);
+          m = fmaxf(m, f < INFINITY ? f : 0.f);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+    top = __float_as_uint(wave_max(m));
   }
-  int e = scale_exponent(wave_max(top));
-  const float s_new = two_to(e);
+  const float s_new = two_to(scale_exponent(__uint_as_float(top)));
   const bool grown = t0 > 0 && s_new > s_was;
   const float s = t0 == 0 || grown ? s_new : s_was;
+  const bool beyond = !(__uint_as_float(top) <= kMaxCode * s);     // the largest scale is too small
   if (lane == 0 && (t0 == 0 || grown)) *scale = s;
-  const float inv = 1.0f / s;                              // exact: a power of two
   float k0[8], mn[8], mx[8], s1[8], s2[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) { mn[i] = INFINITY; mx[i] = -INFINITY; s1[i] = s2[i] = k0[i] = 0.f; }
   for (int chunk = stats || grown ? 0 : first; chunk <= last; ++chunk) {
+    const bool has_old = 16 * chunk < t0 && (stats || grown);      // the same for the whole wavefront, as all but `fresh`
     if (chunk > first) request(chunk);
-    Raw8<e4m3_t> old[4];
-    if (16 * chunk < t0 && (stats || grown)) {             // the same for the whole wavefront
+    if (has_old && (chunk > 0 || !stats)) request_old(chunk);
+    uint2 now[4];
+    if (beyond) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) load_raw8(codes + (size_t)min(16 * chunk + 4 * q + r, t0 - 1) * kD, old[q]);
+      for (int q = 0; q < 4; ++q) {
+        if (!any_new(chunk, q)) continue;
+        float v[8];
+        widen8(raw[q], v);
+        now[q] = codes8_clamped(v, s);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     } else {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) old[q].a = make_uint2(0u, 0u);
+      for (int q = 0; q < 4; ++q)
+        if (any_new(chunk, q)) now[q] = codes8(raw[q], s);
     }
+    if (has_old) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (!any_old(chunk, q)) continue;
+        if (grown) {
+          float v[8];
+          values8(old[q].a, s_was, v);
+          old[q].a = make_uint2(codes4(v[0], v[1], v[2], v[3], s), codes4(v[4], v[5], v[6], v[7], s));
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (16 * chunk + 4 * q + r < t0) now[q] = old[q].a;
+      }
+    }
+    const int from = grown ? 0 : t0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int t = 16 * chunk + 4 * q + r;
-      const bool fresh = t >= t0;
-      float v[8], w[8];
-      widen8(raw[q], v);
-      widen8(old[q], w);
+      if (t >= from && t < cnt) *reinterpret_cast<uint2*>(codes + (size_t)t * kD) = now[q];
+    }
+    if (stats) {
+      auto add = [&](auto whole) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = fresh ? v[i] * inv : (grown ? w[i] * s_was * inv : w[i]);
-      Raw8<e4m3_t> now;
-      now.a = codes8(v);
-      if (!fresh && !grown) now = old[q];
-      if (t < cnt && (fresh || grown)) *reinterpret_cast<uint2*>(codes + (size_t)t * kD) = now.a;
-      if (stats) {
-        widen8(now, v);
+        for (int q = 0; q < 4; ++q) {
+          if (!decltype(whole)::value && 16 * chunk + 4 * q >= cnt) break;
+          float y[8];
+          values8(now[q], s, y);
+          const bool in = decltype(whole)::value || 16 * chunk + 4 * q + r < cnt;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float y = v[i] * s;
-          if (chunk == 0 && q == 0) k0[i] = __shfl(y, c);  // token 0
-          mn[i] = fminf(mn[i], t < cnt ? y : INFINITY);
-          mx[i] = fmaxf(mx[i], t < cnt ? y : -INFINITY);
-          const float dx = t < cnt ? y - k0[i] : 0.f;
-          s1[i] += dx;
-          s2[i] = fmaf(dx, dx, s2[i]);
+          for (int i = 0; i < 8; ++i) {
+            if (chunk == 0 && q == 0) k0[i] = __shfl(y[i], c);     // token 0
+            mn[i] = fminf(mn[i], y[i]);
+            mx[i] = fmaxf(mx[i], y[i]);
+            const float dx = in ? y[i] - k0[i] : 0.f;
+            s1[i] += dx;
+            s2[i] = fmaf(dx, dx, s2[i]);
+          }
+          __builtin_amdgcn_sched_barrier(0);               // a row at a time: four at once cost registers and hide nothing more
         }
-      }
+      };
+      if (16 * chunk + 16 <= cnt) add(IntC<1>{}); else add(IntC<0>{});
     }
   }
-  if (!stats) return;
-  const int b = A.seq[row0], lp = A.pos[row0] >= 0 ? A.pos[row0] / P : -1;
-  if (b < 0 || b >= A.B || lp < 0 || lp >= A.Mmax) return;
+  if (!stats || b < 0 || b >= A.B || lp < 0 || lp / P >= A.Mmax) return;
   const float inv_n = 1.0f / (float)cnt;
-  float avg[8], var[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    mn[i] = fminf(mn[i], __shfl_xor(mn[i], 16)); mn[i] = fminf(mn[i], __shfl_xor(mn[i], 32));
-    mx[i] = fmaxf(mx[i], __shfl_xor(mx[i], 16)); mx[i] = fmaxf(mx[i], __shfl_xor(mx[i], 32));
-    s1[i] += __shfl_xor(s1[i], 16); s1[i] += __shfl_xor(s1[i], 32);
-    s2[i] += __shfl_xor(s2[i], 16); s2[i] += __shfl_xor(s2[i], 32);
-    const float m1 = s1[i] * inv_n;
-    var[i] = fmaxf(fmaf(-m1, m1, s2[i] * inv_n), 0.f);
-    avg[i] = k0[i] + m1;
+  const float2 lo = rows_reduce(mn, [](float a, float b) { return fminf(a, b); }), hi = rows_reduce(mx, [](float a, float b) { return fmaxf(a, b); });
+  const float2 d1 = rows_reduce(s1, [](float a, float b) { return a + b; }), d2 = rows_reduce(s2, [](float a, float b) { return a + b; });
+  const bool up = r >> 1, far = r & 1;                     // channels 2 up + 4 far + 0, 1
+  auto mine = [&](int i) { return far ? (up ? k0[i + 6] : k0[i + 4]) : (up ? k0[i + 2] : k0[i]); };
+  auto variance = [&](float m1, float m2) { return fmaxf(fmaf(-m1, m1, m2 * inv_n), 0.f); };
+  const float m1x = d1.x * inv_n, m1y = d1.y * inv_n;
+  const size_t rec = (((size_t)b * A.Hkv + h) * A.Mmax + lp / P) * 2 * kD;
+  const int e = 2 * up + 4 * far;
+  T* box = (T*)A.box + rec + 8 * c + e; T* gauss = (T*)A.gauss + rec + 8 * c + e;
+  store2(box, lo);
+  store2(box + kD, hi);
+  store2(gauss, make_float2(mine(0) + m1x, mine(1) + m1y));
+  store2(gauss + kD, make_float2(variance(m1x, d2.x), variance(m1y, d2.y)));
+  if (A.box8 != nullptr) {
+    uint8_t* u = A.box8 + rec + 16 * c + e;
+    *reinterpret_cast<uint16_t*>(u) = (uint16_t)(f32_to_e4m3_directed<false>(lo.x) | (f32_to_e4m3_directed<false>(lo.y) << 8));
+    *reinterpret_cast<uint16_t*>(u + 8) = (uint16_t)(f32_to_e4m3_directed<true>(hi.x) | (f32_to_e4m3_directed<true>(hi.y) << 8));
   }
-  if (r != 0) return;
-  const size_t rec = (((size_t)b * A.Hkv + h) * A.Mmax + lp) * 2 * kD;
-  T* box = (T*)A.box + rec; T* gauss = (T*)A.gauss + rec;
-  store8(box + 8 * c, mn);
-  store8(box + kD + 8 * c, mx);
-  store8(gauss + 8 * c, avg);
-  store8(gauss + kD + 8 * c, var);
-  if (A.box8 != nullptr) store_box8_unit(A.box8 + rec + 16 * c, mn, mx);
 }
 
-template <typename T>
-__global__ __launch_bounds__(kAppendThreads) void append8_kernel(const AppendArgs A) {
+template <typename T, bool ONE>
+__global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 4 : 3)))
+void append8_kernel(const AppendArgs A) {
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int id = blockIdx.x * kAppendWaves + w, side = id & 1, h = (id >> 1) % A.Hkv, i0 = (id >> 1) / A.Hkv * A.block;
   if (i0 >= A.T) return;
@@ -305,7 +377,7 @@ __global__ __launch_bounds__(kAppendThreads) void append8_kernel(const AppendArg
     // rows behind l that go on: ones from bit l + 1 of the two masks
     const uint64_t m = l == 63 ? goes_on2 : (goes_on >> (l + 1)) | (goes_on2 << (63 - l));
     const int len = 1 + (m == ~0ull ? 64 : __builtin_ctzll(~m));
-    append_run<T>(A, side, h, i0 + l, len, (uint32_t)__builtin_amdgcn_readlane(sa, l));
+    append_run<T, ONE>(A, side, h, i0 + l, len, (uint32_t)__builtin_amdgcn_readlane(sa, l));
   }
 }
 
@@ -340,14 +412,22 @@ void launch_cache8_append(const Dims& dm, const ekv_cache8_view& c, const ekv_st
   a.slots = tok.slots; a.seq = tok.seq; a.pos = tok.pos;
   a.T = tok.max_tokens; a.B = dm.B; a.Hkv = dm.Hkv; a.HkvPool = dm.HkvPool; a.P = dm.P; a.Mmax = dm.Mmax;
   a.n_slots = (int64_t)c.n_phys_pages * dm.P;
-  // Rows per wavefront: one where there are few, so that a step's rows go on at once; up to 64 where most rows are prompts',
-  // of which one in P begins a run and the others' wavefronts would only find that out.
+  // Rows per wavefront: one where there are few, so that a step's rows go on at once; up to 32 where most rows are prompts', of
+  // which one in P begins a run and the others' wavefronts would only find that out.  us, 4096 wavefronts / 16384 where there
+  // are rows enough: 4096 tokens of prompts 11.9 / 17.3, 1024 single tokens 19.4 / 22.5, 32768 of prompts, which have 16384
+  // with 32 rows each, 50.6 (54.2 with 64; pages of 32 76 with 32 rows, 57 with 64).
+  const bool one = dm.P <= 16;
   a.block = 1;
-  while (a.block < 64 && (long long)a.T * dm.Hkv * 2 / a.block > 8192) a.block *= 2;
+  while (a.block < (one ? 32 : 64) && (long long)a.T * dm.Hkv * 2 / a.block > 4096) a.block *= 2;
   const long long waves = (long long)((a.T + a.block - 1) / a.block) * dm.Hkv * 2;
   const dim3 grid((unsigned)((waves + kAppendWaves - 1) / kAppendWaves)), block(kAppendThreads);
-  if (dm.dtype == EKV_F32) hipLaunchKernelGGL(append8_kernel<float>, grid, block, 0, st, a);
-  else hipLaunchKernelGGL(append8_kernel<bf16_t>, grid, block, 0, st, a);
+  if (dm.dtype == EKV_F32) {
+    if (one) hipLaunchKernelGGL((append8_kernel<float, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((append8_kernel<float, false>), grid, block, 0, st, a);
+  } else {
+    if (one) hipLaunchKernelGGL((append8_kernel<bf16_t, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((append8_kernel<bf16_t, false>), grid, block, 0, st, a);
+  }
 }
 
 }  // namespace ekv

@@ -2158,6 +2158,86 @@ void decode_row_kernel(const ScoreArgs S, const SolveArgs A) {
 }
 
 // ------------------------------------------------------------------------------------------
+// the same over an 8-bit cache
+// ------------------------------------------------------------------------------------------
+// Pages of 8, 16, 32 or 64 tokens (groups of 64; an octet lies in one page).  The scores are those of decode8_scores.hip to the
+// last bit.
+template <typename TQ, bool DENSE, int NW, int TOKENS>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(4)))
+void decode8_row_kernel(const Score8Args S8, const SolveArgs A) {
+  const ScoreArgs& S = S8.s;
+  __shared__ RowShared<NW, TOKENS, 64> sh;
+  const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+  const int heads = S.Hq / S.Hkv, P = S.P, gp = 64 / P;
+  const int bh = group_on_one_xcd(blockIdx.x, gridDim.x, heads), b = bh / S.Hq, hkv = (bh - b * S.Hq) / heads;
+  const int n = uniform_load(S.seq_lens + b);
+  const int n_slots = DENSE ? clampi((n + P - 1) / P, 0, S.Mmax) : clampi(uniform_load(S.n_sel + bh), 0, S.cap);
+  const float seed_z = A.ex.tau_seed != nullptr ? A.ex.tau_seed[bh] : NAN;
+  const int n_groups = (n_slots + gp - 1) / gp, per_batch = 64 / gp;
+  const e4m3_t* k_pool = (const e4m3_t*)S.k_pool;
+  const uint32_t lane_off = key_token(c) * kD + key_offset(c, g);
+  const int copy = column_copy(c, 1);
+  Query8<TQ, 1> qb;
+  qb.load((const TQ*)S.q + (size_t)bh * kD);
+  // lane l: page slot l % gp of this wavefront's item l / gp (groups w, w + NW, ...)
+  for (int g0 = w; g0 < n_groups; g0 += per_batch * NW) {
+    const int mine = min((n_groups - g0 + NW - 1) / NW, per_batch);
+    const int slot = min((g0 + NW * min(lane / gp, mine - 1)) * gp + lane % gp, n_slots - 1);
+    const int l_lp = clampi(DENSE ? slot : S.page_idx[(size_t)bh * S.cap + slot], 0, S.Mmax - 1);
+    const int l_page = clampi(S.block_table[(size_t)b * S.Mmax + l_lp], 0, S.n_phys - 1) * S.HkvPool + hkv;
+    const float l_scale = S8.k_scale[l_page];
+    // octet o of item i: its page's lane and first token there
+    auto lane_of = [&](int i, int o) { return i * gp + uniform(8 * o / P); };
+    auto token_in_page = [&](int o) { return 8 * o & (P - 1); };
+    auto request = [&](int i, int h, uint4 (&k)[4]) {                       // octets 4h .. 4h + 3; past the end: the last item again
+#pragma unroll
+      for (int o = 0; o < 4; ++o) {
+        const int page = __builtin_amdgcn_readlane(l_page, lane_of(min(i, mine - 1), 4 * h + o));
+        k[o] = load16(k_pool + ((size_t)page * P + token_in_page(4 * h + o)) * kD + lane_off);
+      }
+    };
+    float top = -INFINITY;
+    auto consume = [&](int i, int h, const uint4 (&k)[4]) {
+      const int grp = g0 + NW * i, stored = min(64, (n_slots - grp * gp) * P);
+      float2 z[4];
+#pragma unroll
+      for (int o = 0; o < 4; ++o) {
+        const int from = lane_of(i, 4 * h + o), p = 32 * h + 8 * o + 2 * g;
+        octet_scores<TQ, 1>(k[o], __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l_scale), from)), qb, z[o].x, z[o].y);
+        const int left = p < stored ? n - (__builtin_amdgcn_readlane(l_lp, from) * P + token_in_page(4 * h + o) + 2 * g) : 0;
+        z[o].x = left > 0 ? S.zscale * z[o].x : -INFINITY;
+        z[o].y = left > 1 ? S.zscale * z[o].y : -INFINITY;
+        top = fmaxf(top, fmaxf(z[o].x, z[o].y));
+      }
+      const float2 v = copy_pair<1>(z[0], z[1], z[2], z[3], copy);
+      if (copy < 4 && 32 * h + 8 * copy + 2 * g < stored) *reinterpret_cast<float2*>(&sh.z[grp * 64 + 32 * h + 8 * copy + 2 * g]) = v;
+      if (h == 1) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (lane == 0) sh.umax[grp] = top;
+        top = -INFINITY;
+      }
+    };
+    uint4 k0[4], k1[4];
+    request(0, 0, k0);
+    for (int i = 0; i < mine; ++i) {
+      request(i, 1, k1);
+      __builtin_amdgcn_sched_barrier(0);
+      consume(i, 0, k0);
+      request(i + 1, 0, k0);
+      __builtin_amdgcn_sched_barrier(0);
+      consume(i, 1, k1);
+    }
+  }
+  __syncthreads();
+  const RowRef R{b, bh, bh, hkv, n_slots * P, 64, n_groups};
+  if (w == 0)
+    bound_groups<(decltype(sh)::kGroups + 63) / 64, true>([&](int i) { return i < n_groups ? sh.umax[i] : -INFINITY; }, n_groups, A.beta, A.ibeta, sh);
+  __syncthreads();
+  solve_bounded_row<e4m3_t, DENSE>(A, R, sh.z, seed_z, wants_side_outputs<DENSE>(A), sh);
+}
+
+// ------------------------------------------------------------------------------------------
 // launchers
 // ------------------------------------------------------------------------------------------
 // Workgroups per compute unit in a pass-1 launch; never more than the lists can hold items for, and independent of how full
@@ -2297,6 +2377,33 @@ static void launch_rows(const Dims& dm, const ScoreArgs& sa, const SolveArgs& so
   else launch_rows_T<bf16_t, 0>(dm, sa, so, st);
 }
 
+// Rows of an 8-bit cache by one workgroup each; false where two launches are the faster way.  Whole calls, us, two launches / one:
+// lists per head, 2048 rows of 11 / 32 / 128 pages of 16 27.9 / 24.2, 46.6 / 37.5, 116.6 / 80.3, 512 rows of eight pages of 64
+// 21.9 / 15.8, 256 rows of 246 pages of 16 41.5 / 32.7, 128 rows 26.9 / 22.9, 64 rows 21.6 / 21.7, of 82 pages 17.7 / 14.5, 32 rows of
+// 17 / 33 / 66 / 164 pages 14.4 / 10.2, 15.1 / 11.6, 15.4 / 13.2, 17.6 / 17.0.  Every page of 256 / 1024 / 2048 / 4096 tokens, 32
+// rows 13.6 / 9.5, 14.2 / 12.6, 14.2 / 15.1, 14.5 / 20.0, 256 rows of 1024 15.5 / 13.8; many rows read K once per head (2048 rows
+// of 1024 58 / 72), and so do lists shared by a group (2048 of 32 pages 21.9 / 30.5): these take two.
+constexpr int kRowTokensDense = 1024;
+template <typename TQ>
+static void launch_rows8(const Dims& dm, bool dense, const Score8Args& sa, const SolveArgs& so, hipStream_t st) {
+  const int rows = dm.B * dm.Hq;
+  if (dense)
+    hipLaunchKernelGGL((decode8_row_kernel<TQ, true, 16, kRowTokens>), dim3(rows), dim3(1024), 0, st, sa, so);
+  else if (rows <= device_compute_units())
+    hipLaunchKernelGGL((decode8_row_kernel<TQ, false, 16, kRowTokens>), dim3(rows), dim3(1024), 0, st, sa, so);
+  else
+    hipLaunchKernelGGL((decode8_row_kernel<TQ, false, 4, kRowTokensMany>), dim3(rows), dim3(256), 0, st, sa, so);
+}
+static bool rows8_in_one_launch(const Dims& dm, int mode, const Score8Args& sa, const SolveArgs& so, hipStream_t st) {
+  const int cus = device_compute_units(), rows = dm.B * dm.Hq;
+  if (dm.P % 8 != 0 || 64 % dm.P != 0 || mode == kGroupList) return false;
+  if (mode == kAllPages ? rows > cus || (long long)dm.Mmax * dm.P > kRowTokensDense
+                        : (long long)dm.cap * dm.P > (rows > cus ? kRowTokensMany : kRowTokens)) return false;
+  if (dm.dtype == EKV_F32) launch_rows8<float>(dm, mode == kAllPages, sa, so, st);
+  else launch_rows8<bf16_t>(dm, mode == kAllPages, sa, so, st);
+  return true;
+}
+
 void launch_unit_prefix(int mode, const ScoreArgs& sa, int32_t* pre_out, hipStream_t st) {
   if (mode == kPerHead) hipLaunchKernelGGL((unit_prefix_kernel<kPerHead>), dim3(1), dim3(1024), 0, st, sa, pre_out);
   else if (mode == kAllPages) hipLaunchKernelGGL((unit_prefix_kernel<kAllPages>), dim3(1), dim3(1024), 0, st, sa, pre_out);
@@ -2364,6 +2471,7 @@ void launch_decode(const Dims& dm, bool dense, bool grouped, const void* q, cons
     so.page_div = make_page_div(dm.P);
     const int mode = dense ? kAllPages : grouped && dm.G > 1 ? kGroupList : kPerHead;
     sa.U = mode == kPerHead ? dm.B * dm.Hq : dm.B * dm.Hkv;
+    if (!ex.score_pass_only && rows8_in_one_launch(dm, mode, Score8Args{sa, c8->k_scale}, so, st)) return;
     launch_scores8(dm, mode, sa, c8->k_scale, ws.unit_pre, st);
     if (ex.score_pass_only) return;
     if (ws.fcount != nullptr) {

@@ -106,7 +106,8 @@ void decode8_scores_kernel(const Score8Args A8) {
       for (int o = 0; o < 4; ++o) {
         octet_scores<T, G>(k[o], __int_as_float(of_slot(__float_as_int(l_scale), in, k_slot[4 * h + o])), qb, z[o].x, z[o].y);
         const int p = 32 * h + 8 * o + 2 * g;
-        const int left = p < stored ? n - (of_slot(l_lp, in, z_slot[4 * h + o]) * P + z_tok[4 * h + o] + (OCTETS ? 2 * g : 0)) : 0;
+        const int lp = of_slot(l_lp, in, z_slot[4 * h + o]);  // by all lanes: behind the condition some sources would be idle
+        const int left = p < stored ? n - (lp * P + z_tok[4 * h + o] + (OCTETS ? 2 * g : 0)) : 0;
         z[o].x = left > 0 ? A.zscale * z[o].x : -INFINITY;
         z[o].y = left > 1 ? A.zscale * z[o].y : -INFINITY;
         top = fmaxf(top, fmaxf(z[o].x, z[o].y));

@@ -14,7 +14,7 @@
 
 namespace ekv {
 
-constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / 64;
+constexpr int kAttnWaves = 4;                    // wavefronts of a workgroup, or twice as many
 constexpr int kStep = 32;                        // tokens per step of a wavefront
 constexpr int kRec = kD + 2;                     // floats per head of a partial result: o[128], maximum, sum
 constexpr float kSlack = 8.f;                    // weights stay below 2^8
@@ -27,6 +27,7 @@ struct Attn8Args {
   float* part;                                   // [grid + U][G][kRec]
   int32_t* pre;                                  // [U + 1] steps before a unit, for the join
   PageDiv page_div;
+  int per_unit;                                  // 1: workgroup i has unit i, whole
 };
 
 template <bool DENSE>
@@ -54,31 +55,35 @@ template <bool STREAM> __device__ __forceinline__ uint2 load8b(const e4m3_t* p) 
   else return *reinterpret_cast<const uint2*>(p);
 }
 
-template <typename T, int G, bool DENSE, bool OCTETS, bool STREAM>
-__global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2)))
+template <typename T, int G, bool DENSE, bool OCTETS, bool STREAM, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
 void attn8_kernel(const Attn8Args AA) {
   const ScoreArgs& A = AA.s;
   extern __shared__ int pre_lds[];
-  __shared__ int wsum[kAttnWaves];
-  __shared__ float s_o[kAttnWaves][G][kD];
-  __shared__ float s_m[kAttnWaves][G], s_l[kAttnWaves][G];
+  __shared__ int wsum[NW];
+  __shared__ float s_o[NW][G][kD];
+  __shared__ float s_m[NW][G], s_l[NW][G];
   const int P = A.P, lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
   const e4m3_t* k_pool = (const e4m3_t*)A.k_pool;
   const uint32_t k_off = (OCTETS ? key_token(c) * kD : 0) + key_offset(c, g), v_off = (OCTETS ? 2 * g * kD : 0) + 8 * c;
   const int head = column_head(c, G), copy = column_copy(c, G);
   const bool in_lds = A.pre_g == nullptr;
-  int first_unit, begin, end;
+  int first_unit = 0, begin = 0, end = 0;
   auto range = [&](auto pre) {                   // this workgroup's steps
     const int total = uniform(pre[A.U]), W = gridDim.x, i = blockIdx.x, per = total / W, rem = total - per * W;
     begin = i * per + min(i, rem);
     end = begin + per + (i < rem ? 1 : 0);
     first_unit = wave_last_at_most(pre, A.U, begin);
   };
-  if (in_lds) {
-    block_exclusive_prefix<kAttnThreads>(A.U, [&](int u) { return unit_steps<DENSE>(A, u); }, pre_lds, wsum);
+  if (AA.per_unit) {
+    first_unit = blockIdx.x;
+    begin = 0;
+    end = max(unit_steps<DENSE>(A, first_unit), 1);          // one step at least, if of nothing: it writes the row
+  } else if (in_lds) {
+    block_exclusive_prefix<(64 * NW)>(A.U, [&](int u) { return unit_steps<DENSE>(A, u); }, pre_lds, wsum);
     range((const int*)pre_lds);
     if (blockIdx.x == 0)
-      for (int u = threadIdx.x; u <= A.U; u += kAttnThreads) AA.pre[u] = pre_lds[u];
+      for (int u = threadIdx.x; u <= A.U; u += (64 * NW)) AA.pre[u] = pre_lds[u];
   } else {
     range(A.pre_g);
   }
@@ -93,14 +98,16 @@ void attn8_kernel(const Attn8Args AA) {
       while (at >= uniform(pre[unit + 1])) ++unit;
       u_begin = uniform(pre[unit]); u_end = uniform(pre[unit + 1]);
     };
-    if (in_lds) bounds((const int*)pre_lds); else bounds(A.pre_g);
+    if (AA.per_unit) u_end = end;
+    else if (in_lds) bounds((const int*)pre_lds);
+    else bounds(A.pre_g);
     const int seg_end = min(end, u_end), n_steps = seg_end - at;
     const int b = DENSE ? unit / A.Hkv : unit / A.Hq, hkv = DENSE ? unit % A.Hkv : unit % A.Hq / (A.Hq / A.Hkv);
     const size_t row0 = DENSE ? (size_t)b * A.Hq + hkv * G : (size_t)unit;
     const int n = clampi(uniform_load(A.seq_lens + b), 0, A.Mmax * P);
     const int n_pos = DENSE ? n : clampi(uniform_load(A.n_sel + unit), 0, A.cap) * P;      // positions of the unit
     // a quarter of the segment for each wavefront
-    const int st0 = at - u_begin + n_steps * w / kAttnWaves, st1 = at - u_begin + n_steps * (w + 1) / kAttnWaves;
+    const int st0 = at - u_begin + n_steps * w / NW, st1 = at - u_begin + n_steps * (w + 1) / NW;
 
     float m = -INFINITY, l = 0.f;
     f32x4_t acc[8];
@@ -145,7 +152,8 @@ void attn8_kernel(const Attn8Args AA) {
             for (int e = 0; e < 2; ++e) x.v[2 * o + e] = load8b<STREAM>(AA.v_pool + at + v_off + e * kD);
             x.ks[o] = __shfl(l_ks, sk - slot_base);
             x.vs[o] = __shfl(l_vs, sv - slot_base);
-            x.left[o] = pv < n_pos ? n - (__shfl(l_lp, sv - slot_base) * P + (pv - sv * P)) : 0;
+            const int lp = __shfl(l_lp, sv - slot_base);     // by all lanes: behind the condition some sources would be idle
+            x.left[o] = pv < n_pos ? n - (lp * P + (pv - sv * P)) : 0;
           }
         }
       };
@@ -260,14 +268,14 @@ void attn8_kernel(const Attn8Args AA) {
     __syncthreads();
     const bool whole = at == u_begin && seg_end == u_end;    // the unit is this workgroup's alone: no record, no join
     float* rec = AA.part + (size_t)(blockIdx.x + unit) * G * kRec;
-    for (int e = threadIdx.x; e < G * kD; e += kAttnThreads) {
+    for (int e = threadIdx.x; e < G * kD; e += (64 * NW)) {
       const int h = e / kD, ch = e % kD;
       float M = s_m[0][h];
 #pragma unroll
-      for (int i = 1; i < kAttnWaves; ++i) M = fmaxf(M, s_m[i][h]);
+      for (int i = 1; i < NW; ++i) M = fmaxf(M, s_m[i][h]);
       float L = 0.f, o = 0.f;
 #pragma unroll
-      for (int i = 0; i < kAttnWaves; ++i) {
+      for (int i = 0; i < NW; ++i) {
         const float f = s_m[i][h] > -INFINITY ? __builtin_amdgcn_exp2f(s_m[i][h] - M) : 0.f;
         L = fmaf(s_l[i][h], f, L);
         o = fmaf(s_o[i][h][ch], f, o);
@@ -351,28 +359,46 @@ size_t softmax8_ws_bytes(const Dims& dm, bool dense) {
   return attn8_pre_bytes(dm, dense) + recs * (dense ? dm.G : 1) * kRec * sizeof(float);
 }
 
-static void launch_join(const Attn8Args& a, int G, int W, hipStream_t st) {
-  hipLaunchKernelGGL(attn8_join_kernel, dim3(a.s.U * G), dim3(kJoinGroups * kD), 0, st, a, G, W);
+// One workgroup per unit, without the prefix sums and the join, where no unit can be long and there are enough for the GPU, or
+// they are so short that two launches take longer.  Calls, us, split / one workgroup per unit (of eight wavefronts where there are
+// fewer than compute units): 512 units of 1024 tokens 37.4 / 28.6, of 2048 uneven ones 73 / 34.5, of 4096 110 / 76, of 8192 185 /
+// 176, 256 of 1024 26.6 / 16.0, of 8192 103 / 91, 2048 lists of 512 tokens 70 / 59; 128 units of 2048 tokens 23.3 / 19.6, of 4096
+// 35.1 / 38.8, 128 lists of 2622 28.2 / 25.2; 8 units of 256 tokens 11.0 / 8.7, of 1024 11.5 / 11.9, of 2048 11.6 / 17.8, 32 lists of
+// 524 tokens 14.4 / 9.9, of 1049 15.9 / 13.2, of 2622 18.7 / 23.0.  The line is the capacity's: a long sequence among short ones
+// is one workgroup's, at about 75 GB/s (8192 tokens: 28 us).
+static bool attn8_per_unit(const Dims& dm, bool dense, int cus) {
+  const long long tokens = (long long)(dense ? dm.Mmax : dm.cap) * dm.P, units = attn8_units(dm, dense);
+  return tokens <= (units >= cus ? 8192 : units >= cus / 2 ? 2560 : 1024);
+}
+
+template <typename T, int G, bool DENSE, bool STREAM, int NW>
+static void launch_attn8_NW(const Dims& dm, const Attn8Args& a, int W, size_t lds, hipStream_t st) {
+  if (dm.P % 8 == 0) hipLaunchKernelGGL((attn8_kernel<T, G, DENSE, true, STREAM, NW>), dim3(W), dim3(64 * NW), lds, st, a);
+  else hipLaunchKernelGGL((attn8_kernel<T, G, DENSE, false, STREAM, NW>), dim3(W), dim3(64 * NW), lds, st, a);
 }
 template <typename T, int G, bool DENSE>
 static void launch_attn8(const Dims& dm, Attn8Args a, hipStream_t st) {
-  const int cus = device_compute_units(), W = attn8_grid(dm, DENSE, 2 * cus < kMostWgs ? 2 * cus : kMostWgs);
+  const int cus = device_compute_units();
+  const bool stream = DENSE && 2ll * a.s.U * dm.Mmax * dm.P * kD >= kStreamKBytes;
+  if (attn8_per_unit(dm, DENSE, cus)) {
+    a.per_unit = 1;
+    if (a.s.U < cus) { launch_attn8_NW<T, G, DENSE, false, 2 * kAttnWaves>(dm, a, a.s.U, 0, st); return; }
+    if constexpr (DENSE)
+      if (stream) { launch_attn8_NW<T, G, true, true, kAttnWaves>(dm, a, a.s.U, 0, st); return; }
+    launch_attn8_NW<T, G, DENSE, false, kAttnWaves>(dm, a, a.s.U, 0, st);
+    return;
+  }
+  const int W = attn8_grid(dm, DENSE, 2 * cus < kMostWgs ? 2 * cus : kMostWgs);
   if (a.s.U > kUnitsLdsMax) {
     hipLaunchKernelGGL(attn8_prefix_kernel<DENSE>, dim3(1), dim3(1024), 0, st, a);
     a.s.pre_g = a.pre;
   }
   const size_t lds = a.s.pre_g != nullptr ? 0 : (size_t)(a.s.U + 1) * sizeof(int);
-  const dim3 grid(W), block(kAttnThreads);
+  bool done = false;
   if constexpr (DENSE)
-    if (2ll * a.s.U * dm.Mmax * dm.P * kD >= kStreamKBytes) {
-      if (dm.P % 8 == 0) hipLaunchKernelGGL((attn8_kernel<T, G, true, true, true>), grid, block, lds, st, a);
-      else hipLaunchKernelGGL((attn8_kernel<T, G, true, false, true>), grid, block, lds, st, a);
-      launch_join(a, G, W, st);
-      return;
-    }
-  if (dm.P % 8 == 0) hipLaunchKernelGGL((attn8_kernel<T, G, DENSE, true, false>), grid, block, lds, st, a);
-  else hipLaunchKernelGGL((attn8_kernel<T, G, DENSE, false, false>), grid, block, lds, st, a);
-  launch_join(a, G, W, st);
+    if (stream) { launch_attn8_NW<T, G, true, true, kAttnWaves>(dm, a, W, lds, st); done = true; }
+  if (!done) launch_attn8_NW<T, G, DENSE, false, kAttnWaves>(dm, a, W, lds, st);
+  hipLaunchKernelGGL(attn8_join_kernel, dim3(a.s.U * G), dim3(kJoinGroups * kD), 0, st, a, G, W);
 }
 template <typename T>
 static void launch_attn8_T(const Dims& dm, bool dense, const Attn8Args& a, hipStream_t st) {

@@ -14,8 +14,6 @@
 
 namespace ekv {
 
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
-
 struct Score8Args {
   ScoreArgs s;                      // k_pool: the codes
   const float* k_scale;

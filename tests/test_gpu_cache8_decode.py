@@ -308,3 +308,61 @@ def test_large_calls_are_those_of_their_sequences_alone(page, heads, dtype):
         for x, y in zip(whole[1:], one[1:]):
             assert torch.equal(x[b:b + 1].view(torch.int32), y.view(torch.int32)), b
         assert torch.allclose(whole[0][b], one[0][0], rtol=0, atol=2e-6 * float(one[0].abs().max()) + 1e-12)
+
+
+@pytest.mark.parametrize("kind", ["full", "sparse", "softmax", "sparse_softmax"])
+@pytest.mark.parametrize("page", [4, 12, 20, 44, 16])
+def test_wavefronts_with_many_items_are_those_with_one(page, kind):
+    """A batch so large that a wavefront has several groups or steps, whose last tokens and page slots fall on any lane, against
+    its sequences one by one.  The scores are the same to the last bit, but the kernel that solves a row goes by the number of rows, and
+    with it where the solve starts: either threshold is within 4e-6 max(1, |tau|) of the exact one, and so is every weight's base;
+    softmax has another order of its partial sums."""
+    B, Hq, Hkv, n_max = 48, 8, 8, 200 * page
+    g = torch.Generator(device="cuda").manual_seed(page)
+    M = 200
+    lens = [n_max - (b * 53) % n_max for b in range(B)]
+    kp, vp = (torch.randint(0, 0x60, (B * M, Hkv, page, D), generator=g, device="cuda", dtype=torch.uint8) for _ in range(2))
+    ks, vs = (2.0 ** torch.randint(-6, -3, (B * M, Hkv), generator=g, device="cuda").float() for _ in range(2))
+    table = torch.randperm(B * M, generator=g, device="cuda").view(B, M).to(torch.int32)
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    t = torch.arange(M * page, device="cuda").view(1, M, page) >= n[:, None, None]           # slots behind the last token: no numbers
+    kp[table.long()] = torch.where(t[:, :, None, :, None], torch.full_like(kp[:1, :1, :1, :1], 0x7F)[:, None], kp[table.long()])
+    vp[table.long()] = torch.where(t[:, :, None, :, None], torch.full_like(vp[:1, :1, :1, :1], 0x7F)[:, None], vp[table.long()])
+    q = torch.randn(B, Hq, D, generator=g, device="cuda").to(torch.bfloat16)
+    cap = 150
+    idx = torch.stack([torch.randperm(M, generator=g, device="cuda")[:cap].sort().values for _ in range(B * Hq)]).view(B, Hq, cap).to(torch.int32)
+    n_sel = torch.randint(0, cap + 1, (B, Hq), generator=g, device="cuda", dtype=torch.int32)
+
+    def run(rows):
+        cfg = ekv.make_config(len(rows), Hq, Hkv, D, page, "bf16", 1.5, 0.02, M, cap)
+        out, tau, supp = torch.zeros(len(rows), Hq, D, device="cuda"), torch.zeros(len(rows), Hq, device="cuda"), torch.zeros(len(rows), Hq, dtype=torch.int32, device="cuda")
+        op = {"full": ekv.EKV_OP_DECODE_FULL, "sparse": ekv.EKV_OP_DECODE_SPARSE, "softmax": ekv.EKV_OP_DECODE8_FULL_SOFTMAX,
+              "sparse_softmax": ekv.EKV_OP_DECODE8_SPARSE_SOFTMAX}[kind]
+        ws = torch.empty(max(256, ekv.ekv_workspace_bytes(cfg, op)), dtype=torch.uint8, device="cuda")
+        qr, tr, nr = q[rows].contiguous(), table[rows].contiguous(), n[rows].contiguous()
+        view = ekv.cache8_view(kp, vp, ks, vs, tr, nr)
+        lists = (idx[rows].contiguous(), n_sel[rows].contiguous()) if "sparse" in kind else ()
+        if "softmax" in kind:
+            getattr(ekv, "ekv_decode8_" + ("sparse_softmax" if lists else "full_softmax"))(cfg, qr, view, *lists, out, tau, ws)
+        else:
+            getattr(ekv, "ekv_decode8_" + kind)(cfg, qr, view, *lists, out, tau, supp, ws)
+        torch.cuda.synchronize()
+        return out, tau, supp
+
+    whole = run(list(range(B)))
+    assert torch.isfinite(whole[0]).all()
+    for b in range(B):
+        one = run([b])
+        assert torch.allclose(whole[1][b], one[1][0], rtol=8e-6, atol=8e-6), b
+        # weights are (z - tau)^2 <= 1: moved by 2 * 8e-6 at most for each of n tokens, and n float32 additions
+        limit = 2.4e-5 * lens[b] * 448.0 * 2.0 ** -3 if "softmax" not in kind else 1e-5 * float(one[0].abs().max())
+        assert float((whole[0][b] - one[0][0]).abs().max()) <= limit, b
+
+
+@pytest.mark.parametrize("page", [4, 12, 16, 60])
+def test_steps_of_one_workgroup(page):
+    """Sequences of every length around the ends of steps, octets and pages, each by the wavefronts of few workgroups."""
+    lens = [32 * k + d for k in (1, 5, 8, 9, 24) for d in (-1, 0, 1, 2, 7, 9)]
+    c = Cache8(len(lens), 2, 1, page, lens, seed=page)
+    run_full(c, "softmax")
+    check_all(c, "softmax")
