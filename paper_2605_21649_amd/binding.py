@@ -301,9 +301,9 @@ def ekv_release_pages(cfg, release, seq_lens, block_table, free_pages, n_free, n
 
 def _rows(t):
     """Pointer and row stride of [tokens][Hkv][d] rows that may be parts of longer ones."""
-    assert t.dim() == 3 and t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == t.shape[2]), \
-        "the heads of a row must follow each other"
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    n, st = t.shape, t.stride()                  # asked for once: an attribute of a tensor is a tenth of a microsecond
+    assert len(n) == 3 and st[2] == 1 and (n[1] == 1 or st[1] == n[2]), "the heads of a row must follow each other"
+    return t.data_ptr(), st[0] if n[0] > 1 else n[1] * n[2]
 
 
 def ekv_cache8_append(cfg, cache, stats, tokens, k_new, v_new, stream=None):

@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libentmaxkv.so")
 SOURCES = ["api.hip", "stats.hip", "score.hip", "select_topk.hip", "select_gauss.hip", "select_box.hip", "decode.hip",
-           "decode_windows.hip", "cache8.hip", "decode8_scores.hip", "decode8_windows.hip", "decode8_softmax.hip",
+           "decode_windows.hip", "cache8.hip", "decode8_scores.hip", "decode8_held.hip", "decode8_softmax.hip",
            "softmax_sparse.hip", "probe.hip"]
 # packed-FP32 instructions are switched off for all device code (hipcc-only flag; the host pass warns
 # that it does not know the feature, which is harmless)

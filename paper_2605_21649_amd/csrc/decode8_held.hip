@@ -1,32 +1,29 @@
-// Score pass over every page of a large 8-bit cache: the stores of the scores are put off and made by all of the GPU at once, as
-// in decode_windows.hip (what mixed stores cost a stream of reads is told there).  Here they are twice as many beside the bytes read.
+// Score pass over every page of a large 8-bit cache: the stores of the scores are put off, as in decode_windows.hip (what mixed
+// stores cost a stream of reads is told there; here they are twice as many beside the bytes read), until the LDS that holds them is
+// full, which the wavefronts, as fast as one another, reach at about the same time.  A clock that makes them store together does
+// not help here: 4 x 131072 tokens 115.5 us without, 115.8 with windows of 32 us, 117.9 with 16.
 #include "ekv_attn8.h"
 
 namespace ekv {
 
-// PER workgroups of four wavefronts per compute unit, one or four, share its LDS for the scores held back, and have 128 KB of
-// codes in flight: four items (8 KB) for each of four wavefronts or one for each of sixteen.
-template <int PER> struct Windows8 {
-  static constexpr int kHold = 8192 / PER;       // scores a wavefront holds back
-  static constexpr int kFlight = 4 / PER;        // items it has in flight
-  static constexpr int kUnitsMax = PER == 1 ? 4096 : 1024;    // the most units of such a launch
-};
+constexpr int kHold8 = 8192;            // scores a wavefront holds back
+constexpr int kHold8UnitsMax = 4096;    // the most units of such a launch
 
-// Pages of 8, 16, 32 or 64 tokens: items of 64.
-template <typename T, int G, int PT, int PER>
-__global__ __launch_bounds__(kScoreThreads) __attribute__((amdgpu_waves_per_eu(PER)))
-void decode8_windows_kernel(const Score8Args A8, uint32_t window) {
+// Pages of 8, 16, 32 or 64 tokens: items of 64.  One workgroup of four wavefronts per compute unit; a wavefront has one item (8 KB)
+// in flight, each octet requested anew as it is consumed.  us, one item / two / four / eight, eight wavefronts with half the LDS each,
+// sixteen with a quarter: 4 x 131072 tokens 112.9 / 112.9 / 115.2 / 124.4, 113.5, 116.2; 1 x 1048576 221 / 221 / 224 / 227, 234, 253;
+// 64 x 8192 124 / 123 / 125 / 129, 126, 130.
+template <typename T, int G, int PT>
+__global__ __launch_bounds__(kScoreThreads) void decode8_held_kernel(const Score8Args A8) {
   const ScoreArgs& A = A8.s;
   constexpr int GP = 64 / PT, kBatchItems = 64 / GP;
-  constexpr int kHold8 = Windows8<PER>::kHold, kFlight = Windows8<PER>::kFlight;
   constexpr int NB = kHold8 / (64 * G);            // items a wavefront holds
-  static_assert(kBatchItems % kFlight == 0, "a batch begins with the first item of a turn");
   extern __shared__ int pre_lds[];
   __shared__ __attribute__((aligned(16))) float hold_z[kScoreWaves][kHold8];
   __shared__ float hold_max[kScoreWaves][NB * G];
   __shared__ int4 hold_at[kScoreWaves][NB];        // first row, group, scores stored per row
   __shared__ int wsum[kScoreWaves];
-  static_assert(PER * (sizeof(hold_z) + sizeof(hold_max) + sizeof(hold_at) + sizeof(wsum) + (Windows8<PER>::kUnitsMax + 1) * sizeof(int)) <= 160 * 1024,
+  static_assert(sizeof(hold_z) + sizeof(hold_max) + sizeof(hold_at) + sizeof(wsum) + (kHold8UnitsMax + 1) * sizeof(int) <= 160 * 1024,
                 "the LDS of a compute unit");
   const T* q = (const T*)A.q;
   const e4m3_t* k_pool = (const e4m3_t*)A.k_pool;
@@ -64,7 +61,7 @@ void decode8_windows_kernel(const Score8Args A8, uint32_t window) {
   };
 
   int held = 0;
-  auto flush = [&]() __attribute__((always_inline)) {
+  auto flush = [&]() {
     wave_order();
     for (int i0 = 0; i0 < held; i0 += 4) {
 #pragma unroll
@@ -91,11 +88,9 @@ void decode8_windows_kernel(const Score8Args A8, uint32_t window) {
     wave_order();
   };
 
-  uint32_t due = (uint32_t)__builtin_amdgcn_s_memrealtime();
-  due += window - due % window;
   int unit_now = -1, n = 0, n_slots = 0, row0 = 0;
   Query8<T, G> qb;
-  auto process = [&](int it, u32x4_t (&a)[8]) __attribute__((always_inline)) {
+  auto process = [&](int it, u32x4_t (&a)[8]) {
     const int at = (it - batch0) * GP;
     const int unit = __builtin_amdgcn_readlane(now.unit, at), grp = __builtin_amdgcn_readlane(now.grp, at);
     if (unit != unit_now) {
@@ -120,7 +115,7 @@ void decode8_windows_kernel(const Score8Args A8, uint32_t window) {
         z[o].y = left > 1 ? A.zscale * z[o].y : -INFINITY;
         top = fmaxf(top, fmaxf(z[o].x, z[o].y));
         __builtin_amdgcn_sched_barrier(0);
-        request(it + kFlight, 4 * h + o, a[4 * h + o]);
+        request(it + 1, 4 * h + o, a[4 * h + o]);
         __builtin_amdgcn_sched_barrier(0);
       }
       float* hz = &hold_z[w][held * 64 * G + head * 64];
@@ -134,73 +129,55 @@ void decode8_windows_kernel(const Score8Args A8, uint32_t window) {
     top = fmaxf(top, __shfl_xor(top, 32));
     if (g == 0 && copy == 0) hold_max[w][held * G + head] = top;
     if (lane == 0) hold_at[w][held] = make_int4(row0, grp, n_slots * PT - grp * 64, 0);
-    if (it < wi.end) ++held;
-    const uint32_t t = (uint32_t)__builtin_amdgcn_s_memrealtime();
-    const bool tick = (int)(t - due) >= 0;
-    if (held == NB || tick) flush();
-    if (tick) due = t + window - t % window;
+    if (++held == NB) flush();
   };
 
-  // the first requests in the order of their use
-  u32x4_t a[kFlight][8];
+  u32x4_t a[8];
 #pragma unroll
-  for (int i = 0; i < kFlight; ++i) {
-#pragma unroll
-    for (int o = 0; o < 8; ++o) {
-      request(wi.begin + i, o, a[i][o]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+  for (int o = 0; o < 8; ++o) {                    // in the order of their use
+    request(wi.begin, o, a[o]);
+    __builtin_amdgcn_sched_barrier(0);
   }
-  for (int it = wi.begin; it < wi.end; it += kFlight) {
+  for (int it = wi.begin; it < wi.end; ++it) {
     if (it == batch0 + kBatchItems) {
       batch0 = it;
       now = next;
       next = look_up(batch0 + kBatchItems);
     }
-#pragma unroll
-    for (int i = 0; i < kFlight; ++i) process(it + i, a[i]);
+    process(it, a);
   }
   flush();
 }
 
-template <typename T, int G, int PER>
-static void launch_windows_PT(const Dims& dm, const Score8Args& a, dim3 grid, size_t lds, uint32_t window, hipStream_t st) {
+template <typename T, int G>
+static void launch_held_PT(const Dims& dm, const Score8Args& a, dim3 grid, size_t lds, hipStream_t st) {
   const dim3 block(kScoreThreads);
-  if (dm.P == 8) hipLaunchKernelGGL((decode8_windows_kernel<T, G, 8, PER>), grid, block, lds, st, a, window);
-  else if (dm.P == 16) hipLaunchKernelGGL((decode8_windows_kernel<T, G, 16, PER>), grid, block, lds, st, a, window);
-  else if (dm.P == 32) hipLaunchKernelGGL((decode8_windows_kernel<T, G, 32, PER>), grid, block, lds, st, a, window);
-  else hipLaunchKernelGGL((decode8_windows_kernel<T, G, 64, PER>), grid, block, lds, st, a, window);
+  if (dm.P == 8) hipLaunchKernelGGL((decode8_held_kernel<T, G, 8>), grid, block, lds, st, a);
+  else if (dm.P == 16) hipLaunchKernelGGL((decode8_held_kernel<T, G, 16>), grid, block, lds, st, a);
+  else if (dm.P == 32) hipLaunchKernelGGL((decode8_held_kernel<T, G, 32>), grid, block, lds, st, a);
+  else hipLaunchKernelGGL((decode8_held_kernel<T, G, 64>), grid, block, lds, st, a);
 }
-template <typename T, int PER>
-static void launch_windows_T(const Dims& dm, const Score8Args& a, dim3 grid, size_t lds, uint32_t window, hipStream_t st) {
-  if (dm.G == 1) launch_windows_PT<T, 1, PER>(dm, a, grid, lds, window, st);
-  else if (dm.G == 2) launch_windows_PT<T, 2, PER>(dm, a, grid, lds, window, st);
-  else if (dm.G == 4) launch_windows_PT<T, 4, PER>(dm, a, grid, lds, window, st);
-  else launch_windows_PT<T, 8, PER>(dm, a, grid, lds, window, st);
+template <typename T>
+static void launch_held_T(const Dims& dm, const Score8Args& a, dim3 grid, size_t lds, hipStream_t st) {
+  if (dm.G == 1) launch_held_PT<T, 1>(dm, a, grid, lds, st);
+  else if (dm.G == 2) launch_held_PT<T, 2>(dm, a, grid, lds, st);
+  else if (dm.G == 4) launch_held_PT<T, 4>(dm, a, grid, lds, st);
+  else launch_held_PT<T, 8>(dm, a, grid, lds, st);
 }
 
-// Whole calls, us, by chunks (decode8_scores.hip) / in windows by four workgroups per compute unit, heads four to a KV head: 1 x 65536
-// tokens (67 MB of K) 30.4 / 28.8, 1 x 131072 51.0 / 44.6, 4 x 131072 uneven 123.9 / 119.3, 64 x 2048 59.6 / 51.6; eight heads,
-// 1 x 32768 22.0 / 22.0, 1 x 65536 31.0 / 30.6, 1 x 524288 153 / 158; one head, 1 x 262144 69.1 / 65.5, 1 x 524288 123 / 113;
-// float32 queries, 64 x 8192 134 / 125, pages of 8 tokens, 4 x 131072 134 / 128.  One workgroup per compute unit, whose lone
-// wavefronts pay more for their start, needs a long call: 1 x 1048576 246 by chunks, 235 by four, 222 by one, 4 x 131072
-// (466 MB) 113 / 112 / 119.  A window is what fills most of a wavefront's LDS at full rate, half of decode_windows.hip's.
-bool launch_scores8_windows(const Dims& dm, const Score8Args& a, long long items, long long k_bytes, hipStream_t st) {
+// Whole calls, us, by chunks (decode8_scores.hip) / here, heads four to a KV head: 1 x 65536 tokens (67 MB of K) 30.4 / 27.1, 1 x
+// 131072 51.0 / 42.7, 4 x 131072 uneven 123.9 / 112.9, 64 x 2048 59.6 / 51.6, 1 x 1048576 246 / 221; eight heads, 1 x 65536 31.0 /
+// 30.6, 1 x 524288 153 / 145; one head, 1 x 262144 69.1 / 65.5, 1 x 524288 123 / 110.
+bool launch_scores8_held(const Dims& dm, const Score8Args& a, long long items, long long k_bytes, hipStream_t st) {
   const unsigned long long z_bytes = (unsigned long long)a.s.U * dm.G * a.s.zstride * 4;
-  if ((dm.P != 8 && dm.P != 16 && dm.P != 32 && dm.P != 64) || a.s.U > Windows8<1>::kUnitsMax || k_bytes < (64ll << 20) ||
+  if ((dm.P != 8 && dm.P != 16 && dm.P != 32 && dm.P != 64) || a.s.U > kHold8UnitsMax || k_bytes < (64ll << 20) ||
       z_bytes < (8u << 20) || (unsigned long long)a.s.zstride * dm.G * 4 > 0x7fffffffull) return false;
-  const bool one = a.s.U > Windows8<4>::kUnitsMax || k_bytes >= (768ll << 20);
-  const long long wgs = (items + kScoreWaves - 1) / kScoreWaves, most = (long long)device_compute_units() * (one ? 1 : 4);
-  const dim3 grid((unsigned)(wgs < most ? wgs : most));
+  const long long wgs = (items + kScoreWaves - 1) / kScoreWaves;
+  const int cus = device_compute_units();
+  const dim3 grid((unsigned)(wgs < cus ? wgs : cus));
   const size_t lds = (size_t)(a.s.U + 1) * sizeof(int);
-  const uint32_t window = 12800 / dm.G;
-  if (dm.dtype == EKV_F32) {
-    if (one) launch_windows_T<float, 1>(dm, a, grid, lds, window, st);
-    else launch_windows_T<float, 4>(dm, a, grid, lds, window, st);
-  } else {
-    if (one) launch_windows_T<bf16_t, 1>(dm, a, grid, lds, window, st);
-    else launch_windows_T<bf16_t, 4>(dm, a, grid, lds, window, st);
-  }
+  if (dm.dtype == EKV_F32) launch_held_T<float>(dm, a, grid, lds, st);
+  else launch_held_T<bf16_t>(dm, a, grid, lds, st);
   return true;
 }
 

@@ -198,7 +198,7 @@ void launch_scores8(const Dims& dm, int mode, ScoreArgs sa, const float* k_scale
   const long long k_bytes = (long long)sa.U * (mode == kAllPages ? dm.Mmax : dm.cap) * dm.P * kD;
   const bool stream = mode != kPerHead && k_bytes >= kStreamKBytes;
   const Score8Args a{sa, k_scale};
-  if (mode == kAllPages && launch_scores8_windows(dm, a, items, k_bytes, st)) return;
+  if (mode == kAllPages && launch_scores8_held(dm, a, items, k_bytes, st)) return;
   const size_t lds = pre_global ? 0 : (size_t)(sa.U + 1) * sizeof(int);
   const dim3 grid((unsigned)wgs);
   if (dm.dtype == EKV_F32) launch_T<float>(dm, mode, a, stream, grid, lds, st);

@@ -69,14 +69,17 @@ void attn8_kernel(const Attn8Args AA) {
   const int head = column_head(c, G), copy = column_copy(c, G);
   const bool in_lds = A.pre_g == nullptr;
   int first_unit = 0, begin = 0, end = 0;
+  // Workgroups go to the XCDs in turn: each XCD gets a stretch of the steps, so that the lists of a group's heads, which name many
+  // of the same pages, meet in one L2 (64 x 8192 tokens, lists of 32 pages, the same for a group: 51.1 -> 42.2 us a call).
+  const int wg = !DENSE && gridDim.x % kXcds == 0 ? (int)(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
   auto range = [&](auto pre) {                   // this workgroup's steps
-    const int total = uniform(pre[A.U]), W = gridDim.x, i = blockIdx.x, per = total / W, rem = total - per * W;
+    const int total = uniform(pre[A.U]), W = gridDim.x, i = wg, per = total / W, rem = total - per * W;
     begin = i * per + min(i, rem);
     end = begin + per + (i < rem ? 1 : 0);
     first_unit = wave_last_at_most(pre, A.U, begin);
   };
   if (AA.per_unit) {
-    first_unit = blockIdx.x;
+    first_unit = wg;
     begin = 0;
     end = max(unit_steps<DENSE>(A, first_unit), 1);          // one step at least, if of nothing: it writes the row
   } else if (in_lds) {
@@ -267,7 +270,7 @@ void attn8_kernel(const Attn8Args AA) {
     if (g == 0 && copy == 0) { s_m[w][head] = m; s_l[w][head] = l; }
     __syncthreads();
     const bool whole = at == u_begin && seg_end == u_end;    // the unit is this workgroup's alone: no record, no join
-    float* rec = AA.part + (size_t)(blockIdx.x + unit) * G * kRec;
+    float* rec = AA.part + (size_t)(wg + unit) * G * kRec;
     for (int e = threadIdx.x; e < G * kD; e += (64 * NW)) {
       const int h = e / kD, ch = e % kD;
       float M = s_m[0][h];

@@ -18,9 +18,9 @@ struct Score8Args {
   ScoreArgs s;                      // k_pool: the codes
   const float* k_scale;
 };
-// Score pass over every page in common windows for the stores (decode8_windows.hip); false, with nothing launched, where it is not
+// Score pass over every page with the stores put off (decode8_held.hip); false, with nothing launched, where it is not
 // the faster one or the call has a form that it does not take.
-bool launch_scores8_windows(const Dims& dm, const Score8Args& a, long long items, long long k_bytes, hipStream_t st);
+bool launch_scores8_held(const Dims& dm, const Score8Args& a, long long items, long long k_bytes, hipStream_t st);
 
 // e4m3 pairs -> bf16 times a power of two (exact); HI: the upper two codes
 template <bool HI> __device__ __forceinline__ uint32_t widen2(uint32_t codes, float scale) {
