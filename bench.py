@@ -43,7 +43,9 @@ STAGE_NAMES = {"topk": ["append_own_launch", "append+score_box", "select_topk", 
                "group": ["append_own_launch", "append+score_group_max", "select_topk", "decode_sparse_group"],
                "dense": ["-", "-", "-", "decode_full"],
                "topk8": ["append_own_launch", "append+score_box8", "select_topk", "decode_sparse"],
-               "group8": ["append_own_launch", "append+score_box8_group_max", "select_topk", "decode_sparse_group"]}
+               "group8": ["append_own_launch", "append+score_box8_group_max", "select_topk", "decode_sparse_group"],
+               "cache8": ["map+append", "score_box", "select_topk", "decode8_sparse"],
+               "dense8": ["-", "-", "-", "decode8_full"]}
 
 
 def parse():
@@ -53,7 +55,8 @@ def parse():
     ap.add_argument("--warmup", type=int, default=20)
     ap.add_argument("--workload", default="C4")
     ap.add_argument("--budget", type=float, default=0.02, help="top-k budget as a fraction of the pages")
-    ap.add_argument("--variant", default="topk", choices=["topk", "gauss", "group", "dense", "topk8", "group8"],
+    ap.add_argument("--variant", default="topk", choices=["topk", "gauss", "group", "dense", "topk8", "group8", "cache8",
+                                                                "dense8"],
                     help="step timed as the headline: top-k (default, the metric's variant), Gaussian selector, "
                          "group-shared top-k, or the dense full-cache decode alone (for profiling the other rows)")
     ap.add_argument("--copies", type=int, default=4, help="rotating copies of the cache (defeats the LLC)")
@@ -197,6 +200,31 @@ class Runner:
                                     st.ws_sparse)
         if evs: evs[4].record()
 
+    def step_cache8(self, st, evs=None):
+        """Top-k step on the cache held in 8 bits: the token's page and slot, the quantising append, scores, selection, decode."""
+        ekv = self.ekv
+        if not hasattr(st, "pools8"):
+            st.enable_cache8()
+        if evs: evs[0].record()
+        st.map_and_append8()
+        if evs: evs[1].record()
+        ekv.ekv_score_pages(st.cfg, st.inp["q"], st.stats8(), st.lens8_now, ekv.EKV_SCORE_BOX, st.box)
+        if evs: evs[2].record()
+        ekv.ekv_select_topk(st.cfg, st.box, st.lens8_now, self.k_pages, st.page_idx, st.n_sel, st.ws_topk)
+        if evs: evs[3].record()
+        ekv.ekv_decode8_sparse(st.cfg, st.inp["q"], st.cache8(), st.page_idx, st.n_sel, st.out, st.tau, st.supp, st.ws_sparse)
+        if evs: evs[4].record()
+
+    def step_dense8(self, st, evs=None):
+        if not hasattr(st, "pools8"):
+            st.enable_cache8()
+            st.map_and_append8()
+        ws = self.full_ws()
+        if evs:
+            for e in evs[:4]: e.record()
+        self.ekv.ekv_decode8_full(st.cfg, st.inp["q"], st.cache8(), st.out, st.tau, st.supp, ws)
+        if evs: evs[4].record()
+
     def step_dense(self, st, evs=None):
         if self.ws_full is None:                              # one scratch shared by the copies
             self.ws_full = self.copies[0].workspace(self.ekv.EKV_OP_DECODE_FULL)
@@ -207,7 +235,8 @@ class Runner:
 
     def step(self, variant):
         return {"topk": self.step_topk, "gauss": self.step_gauss, "group": self.step_group,
-                "dense": self.step_dense, "topk8": self.step_topk8, "group8": self.step_group8}[variant]
+                "dense": self.step_dense, "topk8": self.step_topk8, "group8": self.step_group8,
+                "cache8": self.step_cache8, "dense8": self.step_dense8}[variant]
 
     # ---- timing --------------------------------------------------------------------------------
     def run_timed(self, step_fn, steps, warmup, stages=True):
@@ -864,6 +893,24 @@ def main():
             "delta_mean": round(float((1.0 - kept_mass).mean()), 6),
             "rho_mean": round(float((kept_supp.float() / supp_f.float()).mean()), 4),
             "R_mean": round(float(((st0.out - out_f).norm(dim=-1) / out_f.norm(dim=-1)).mean()), 6)}
+        # the cache held in 8 bits (an extension): the top-k step with its pages and slots mapped on the GPU, the dense decode and
+        # softmax over the lists and over every page; quality against the 16-bit cache's dense decode
+        us_c8, stage_c8, _ = R.run_timed(R.step_cache8, side, 5)
+        us_d8, _, _ = R.run_timed(R.step_dense8, max(5, side // 2), 3, stages=False)
+        ws8 = [st0.workspace(op) for op in (ekv.EKV_OP_DECODE8_SPARSE_SOFTMAX, ekv.EKV_OP_DECODE8_FULL_SOFTMAX)]
+        lse8 = torch.zeros_like(st0.tau)
+        us_s8 = R.time_call(lambda st: ekv.ekv_decode8_sparse_softmax(st0.cfg, st0.inp["q"], st.cache8(), st0.page_idx, st0.n_sel,
+                                                                      st0.out, lse8, ws8[0]), reps=10)
+        us_f8 = R.time_call(lambda st: ekv.ekv_decode8_full_softmax(st0.cfg, st0.inp["q"], st.cache8(), st0.out, lse8, ws8[1]), reps=10)
+        R.step_dense8(st0)
+        torch.cuda.synchronize()
+        extras["cache8"] = {
+            "topk_step_us": round(us_c8, 2),
+            "topk_stage_us": {nm: round(float(v), 2) for nm, v in zip(STAGE_NAMES["cache8"], stage_c8.mean(axis=0))},
+            "dense_full_us": round(us_d8, 2),
+            "dense_full_GBps": round(B * Hkv * w.context * w.head_dim / (us_d8 * 1e-6) / 1e9, 1),
+            "softmax_over_topk_lists_us": round(us_s8, 2), "softmax_full_us": round(us_f8, 2),
+            "dense_out_error_vs_16_bit": round(float(((st0.out - out_f).norm(dim=-1) / out_f.norm(dim=-1)).mean()), 6)}
         result["other_rows"] = extras
 
     # ---------------------------------------------------------------- CPU baseline: the oracle, as it stands

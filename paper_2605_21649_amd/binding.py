@@ -184,6 +184,11 @@ def cache8_view(k_pool, v_pool, k_scale, v_scale, block_table=None, seq_lens=Non
 
 
 def token_map(slots, seq=None, pos=None, start=None, n_mapped=None):
+    assert slots.dtype == torch.int64, "slots are int64"
+    for t in (seq, pos):
+        assert t is None or (t.dtype == torch.int32 and t.numel() == slots.numel()), "seq and pos: int32, one for every slot"
+    for t in (start, n_mapped):
+        assert t is None or t.dtype == torch.int32, "start and n_mapped are int32"
     return ekv_token_map(_ptr(slots), _ptr(seq), _ptr(pos), _ptr(start), _ptr(n_mapped), slots.numel())
 
 

@@ -49,6 +49,64 @@ class DeviceState:
                                       dtype=torch.uint8)
         return self.box8_stats
 
+    def enable_cache8(self, chunk=65536):
+        """The workload's sequences on an 8-bit cache of their own, as a server fills one: pages are mapped from lengths and the
+        tokens appended in chunks, with the page statistics of the stored keys.
+        The last token of each sequence stays for the step (map_and_append8)."""
+        w, dev, i = self.w, self.box.device, self.inp
+        B, Hkv, d, P, M = w.batch, w.n_kv_heads, w.head_dim, w.page_size, self.Mmax
+        n_phys = B * M
+        i32 = dict(device=dev, dtype=torch.int32)
+        self.pools8 = [torch.zeros(n_phys, Hkv, P, d, device=dev, dtype=torch.uint8) for _ in range(2)]
+        self.scales8 = [torch.ones(n_phys, Hkv, device=dev) for _ in range(2)]
+        self.table8, self.free8 = torch.zeros(B, M, **i32), torch.randperm(n_phys, device=dev).to(torch.int32)
+        self.box_stats8, self.gauss_stats8 = torch.zeros_like(self.box_stats), torch.zeros_like(self.gauss_stats)
+        lens, n_free = torch.zeros(B, **i32), torch.full((1,), n_phys, **i32)
+        total = i["seq_lens"].tolist()
+        for at in range(0, max(total), chunk):
+            counts = [max(0, min(at + chunk, n - 1) - at) for n in total]
+            if not sum(counts):
+                break
+            t = self._tokens8(sum(counts))
+            new_lens, left = torch.zeros(B, **i32), torch.zeros(1, **i32)
+            ekv.ekv_map_tokens(self.cfg, lens, torch.tensor(counts, **i32), self.table8, self.free8, n_free, t["map"], new_lens, left)
+            rows = []
+            for name in ("k_pool", "v_pool"):
+                part = []
+                for b, c in enumerate(counts):
+                    pos = torch.arange(at, at + c, device=dev)
+                    part.append(i[name][i["block_table"][b].long()[pos // P], :, pos % P])
+                rows.append(torch.cat(part))
+            lens, n_free = new_lens, left
+            ekv.ekv_cache8_append(self.cfg, self.cache8(lens), self.stats8(), t["map"], *rows)
+            del rows
+        last = i["seq_lens"].long() - 1
+        at = (torch.arange(B, device=dev), last // P)
+        self.new8 = [i[name][i["block_table"].long()[at], :, last % P].contiguous() for name in ("k_pool", "v_pool")]
+        self.lens8, self.free_count8, self.ones8 = lens, n_free, torch.ones(B, **i32)
+        self.lens8_now, self.left8 = torch.zeros(B, **i32), torch.zeros(1, **i32)
+        self.tokens8 = self._tokens8(B)
+
+    def _tokens8(self, n):
+        i32 = dict(device=self.box.device, dtype=torch.int32)
+        t = {"slots": torch.zeros(n, device=self.box.device, dtype=torch.int64), "seq": torch.zeros(n, **i32), "pos": torch.zeros(n, **i32),
+             "start": torch.zeros(self.w.batch + 1, **i32), "n_mapped": torch.zeros(self.w.batch, **i32)}
+        t["map"] = ekv.token_map(t["slots"], t["seq"], t["pos"], t["start"], t["n_mapped"])
+        return t
+
+    def cache8(self, lens=None):
+        return ekv.cache8_view(*self.pools8, *self.scales8, self.table8, self.lens8_now if lens is None else lens)
+
+    def stats8(self):
+        return ekv.stats_view(self.box_stats8, self.gauss_stats8)
+
+    def map_and_append8(self):
+        """One token per sequence: its page and slot, its codes, its page's statistics.  The free list and the lengths before it
+        stay, so that the step can be repeated."""
+        ekv.ekv_map_tokens(self.cfg, self.lens8, self.ones8, self.table8, self.free8, self.free_count8, self.tokens8["map"],
+                           self.lens8_now, self.left8)
+        ekv.ekv_cache8_append(self.cfg, self.cache8(), self.stats8(), self.tokens8["map"], *self.new8)
+
     def workspace(self, op):
         if op not in self.ws:
             n = ekv.ekv_workspace_bytes(self.cfg, op)

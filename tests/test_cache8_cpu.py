@@ -118,3 +118,11 @@ def test_the_binding_takes_rows_of_a_longer_projection_and_no_other_strides():
             ekv._rows(bad)
     with pytest.raises(AssertionError):                      # fewer rows than the map has tokens
         ekv.ekv_cache8_append(good_cfg(), cache(), None, tokens(max_tokens=6), rows[:, 0], rows[:, 1])
+
+
+def test_the_binding_takes_maps_of_the_right_types_only():
+    slots, i32 = torch.zeros(4, dtype=torch.int64), torch.zeros(4, dtype=torch.int32)
+    assert ekv.token_map(slots, i32, i32, i32, i32).max_tokens == 4
+    for bad in ((i32,), (slots, slots, i32), (slots, i32, torch.zeros(3, dtype=torch.int32)), (slots, i32, i32, slots), (slots, i32, i32, i32, slots)):
+        with pytest.raises(AssertionError):
+            ekv.token_map(*bad)

@@ -366,3 +366,52 @@ def test_steps_of_one_workgroup(page):
     c = Cache8(len(lens), 2, 1, page, lens, seed=page)
     run_full(c, "softmax")
     check_all(c, "softmax")
+
+
+@pytest.mark.parametrize("page", [12, 16])
+@pytest.mark.parametrize("rows", [600, 40000])
+def test_a_batch_of_empty_sequences(rows, page):
+    """Nothing to look at anywhere, in short and in long capacities, with lists and without."""
+    c = Cache8(3, 8, 2, page, [0, 0, 0], row_pages=rows, seed=1, cap=min(rows, 500))
+    idx, n = torch.zeros(3, 8, c.cap, dtype=torch.int32, device="cuda"), torch.full((3, 8), c.cap, dtype=torch.int32, device="cuda")
+    n[1] = 0
+
+    def empty(first):
+        torch.cuda.synchronize()
+        ok = not c.out.any() and bool((c.tau == first).all())
+        c.out.fill_(float("nan"))
+        c.tau.fill_(float("nan"))
+        return ok
+
+    for kind, first in (("entmax", np.inf), ("softmax", -np.inf)):
+        run_full(c, kind)
+        assert empty(first)
+    ekv.ekv_decode8_sparse(c.cfg, c.q, c.view(), idx, n, c.out, c.tau, c.supp, c.workspace(ekv.EKV_OP_DECODE_SPARSE))
+    assert empty(np.inf) and not c.supp.any()
+    ekv.ekv_decode8_sparse_group(c.cfg, c.q, c.view(), idx[:, :2].contiguous(), n[:, :2].contiguous(), c.out, c.tau, c.supp,
+                                 c.workspace(ekv.EKV_OP_DECODE_SPARSE))
+    assert empty(np.inf)
+    ekv.ekv_decode8_sparse_softmax(c.cfg, c.q, c.view(), idx, n, c.out, c.tau, c.workspace(ekv.EKV_OP_DECODE8_SPARSE_SOFTMAX))
+    assert empty(-np.inf)
+
+
+@pytest.mark.parametrize("call", ["sparse", "group", "softmax"])
+@pytest.mark.parametrize("page", [12, 16, 64])
+def test_long_lists_of_grouped_heads(page, call):
+    """Lists longer than one workgroup decodes, of heads that share most of their pages, split over the GPU."""
+    rng = np.random.default_rng(page)
+    cap = 5000 // page
+    c = Cache8(2, 8, 2, page, [9000, 4100], seed=page, cap=cap)
+    lists = []
+    for b in range(2):
+        m = -(-c.lens[b] // page)
+        shared = [rng.permutation(m) for _ in range(2)]
+        lists.append([sorted(shared[i // (1 if call == "group" else 4)][:min(m, cap) - 3 * (i % 4)].tolist()) for i in range(2 if call == "group" else 8)])
+    idx, n = as_tensors(c, lists, cap, rng)
+    if call == "softmax":
+        ekv.ekv_decode8_sparse_softmax(c.cfg, c.q, c.view(), idx, n, c.out, c.tau, c.workspace(ekv.EKV_OP_DECODE8_SPARSE_SOFTMAX))
+    else:
+        fn = ekv.ekv_decode8_sparse_group if call == "group" else ekv.ekv_decode8_sparse
+        fn(c.cfg, c.q, c.view(), idx, n, c.out, c.tau, c.supp, c.workspace(ekv.EKV_OP_DECODE_SPARSE))
+    torch.cuda.synchronize()
+    check_all(c, "softmax" if call == "softmax" else "entmax", [[row[h // 4] for h in range(8)] for row in lists] if call == "group" else lists)

@@ -170,3 +170,77 @@ def test_two_servers_on_streams_of_their_own():
         for i in range(2):
             for x, y in zip(alone[i].results(), both[i].results()):
                 assert torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8))
+
+
+@pytest.mark.parametrize("name,context,page,batch", [("C2", 4100, 16, 2), ("C1", 1500, 12, 1), ("C5", 9000, 32, 3)])
+def test_a_workload_on_an_eight_bit_cache(name, context, page, batch):
+    """The benchmark's steps: a workload's cache taken over in chunks, then the step of its last token, twice."""
+    from paper_2605_21649_amd import synth
+    from tests.helpers import DeviceState, to_f64
+    w = synth.WORKLOADS[name].scaled(name="w8", context=context, page_size=page, batch=batch)
+    inp = synth.make_inputs(w, 7, device="cpu")
+    st = DeviceState(w, inp, cap=16)
+    st.enable_cache8(chunk=1000)
+    ws = st.workspace(ekv.EKV_OP_DECODE_FULL)
+    seen = []
+    for _ in range(2):
+        st.map_and_append8()
+        ekv.ekv_decode8_full(st.cfg, st.inp["q"], st.cache8(), st.out, st.tau, st.supp, ws)
+        torch.cuda.synchronize()
+        seen.append((st.out.clone(), st.tau.clone(), st.pools8[0].clone(), st.box_stats8.clone()))
+    assert all(torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8)) for a, b in zip(*seen))
+    assert st.lens8_now.tolist() == inp["seq_lens"].tolist()
+    for b, h in ((0, 0), (batch - 1, w.n_q_heads - 1)):
+        rows = st.table8[b].cpu().numpy()[:w.pages_per_seq]
+        K, V = ((VALUES[st.pools8[i][:, h // w.group].cpu().numpy()[rows]] * st.scales8[i][:, h // w.group].cpu().numpy().astype(np.float64)[rows, None, None])
+                .reshape(-1, D)[:context] for i in range(2))
+        for x, y in zip((K, V), synth.logical_kv(inp, w, b, h // w.group)):
+            y = to_f64(y)                                     # within half a step, once more where a page's scale grew meanwhile
+            assert np.all(np.abs(x - y) <= 2.0 ** -4 * np.abs(y) + 2.0 ** -9 * np.abs(y).max())
+        q = to_f64(inp["q"][b, h])
+        ref = orc.entmax_attention(q, K, V, w.alpha, w.score_scale)
+        e = score_error(q, K, w.score_scale)
+        assert abs(float(st.tau[b, h]) - ref["tau"]) <= e + 4e-6 * max(1.0, abs(ref["tau"]))
+        kmin, kmax = orc.page_stats(K, page)[:2]
+        got = st.box_stats8[b, h // w.group].float().cpu().numpy()
+        assert np.array_equal(got[:, 0], kmin) and np.array_equal(got[:, 1], kmax)
+
+
+@pytest.mark.parametrize("page", [16, 12])
+def test_pages_beyond_four_gigabytes(page):
+    """The same sequences at the end of pools of 5 GB and in small ones: the same bits of everything."""
+    B, Hq, Hkv, M = 3, 4, 2, 300 // page + 1
+    lens = [300, 17, 150]
+    results = []
+    for n_phys in (B * M, 5 * 10 ** 9 // (Hkv * page * D)):
+        g = torch.Generator(device="cuda").manual_seed(3)
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+        kp, vp = (torch.empty(n_phys, Hkv, page, D, dtype=torch.uint8, device="cuda") for _ in range(2))
+        ks, vs = (torch.empty(n_phys, Hkv, device="cuda") for _ in range(2))
+        cfg = ekv.make_config(B, Hq, Hkv, D, page, "bf16", 1.5, 0.1, M, M)
+        table, free = torch.zeros(B, M, dtype=torch.int32, device="cuda"), torch.arange(n_phys - B * M, n_phys, dtype=torch.int32, device="cuda")
+        T = sum(lens)
+        slots, seq, pos = torch.zeros(T, dtype=torch.int64, device="cuda"), i32([0] * T), i32([0] * T)
+        new_lens, left = i32([0] * B), i32([0])
+        start, mapped, before, counts, n_free = i32([0] * (B + 1)), i32([0] * B), i32([0] * B), i32(lens), i32([B * M])
+        tokens = ekv.token_map(slots, seq, pos, start, mapped)
+        ekv.ekv_map_tokens(cfg, before, counts, table, free, n_free, tokens, new_lens, left)
+        rows = torch.randn(T, 2, Hkv, D, generator=g, device="cuda").to(torch.bfloat16)
+        ekv.ekv_cache8_append(cfg, ekv.cache8_view(kp, vp, ks, vs), None, tokens, rows[:, 0], rows[:, 1])
+        assert int(slots.max()) // page >= n_phys - B * M
+        q = torch.randn(B, Hq, D, generator=g, device="cuda").to(torch.bfloat16)
+        idx = torch.arange(M, dtype=torch.int32, device="cuda").expand(B, Hq, M).contiguous()
+        n = ((new_lens + page - 1) // page)[:, None].expand(B, Hq).to(torch.int32).contiguous()
+        view = ekv.cache8_view(kp, vp, ks, vs, table, new_lens)
+        got = []
+        for name, op, lists in (("full", ekv.EKV_OP_DECODE_FULL, ()), ("sparse", ekv.EKV_OP_DECODE_SPARSE, (idx, n)),
+                                ("full_softmax", ekv.EKV_OP_DECODE8_FULL_SOFTMAX, ()), ("sparse_softmax", ekv.EKV_OP_DECODE8_SPARSE_SOFTMAX, (idx, n))):
+            out, tau, supp = torch.zeros(B, Hq, D, device="cuda"), torch.zeros(B, Hq, device="cuda"), torch.zeros(B, Hq, dtype=torch.int32, device="cuda")
+            ws = torch.empty(max(256, ekv.ekv_workspace_bytes(cfg, op)), dtype=torch.uint8, device="cuda")
+            getattr(ekv, "ekv_decode8_" + name)(cfg, q, view, *lists, out, tau, *(() if "softmax" in name else (supp,)), ws)
+            got += [out, tau, supp]
+        torch.cuda.synchronize()
+        assert torch.isfinite(got[0]).all() and torch.isfinite(got[6]).all()
+        results.append([x.cpu() for x in got])
+        del kp, vp, ks, vs, view
+    assert all(torch.equal(a, b) for a, b in zip(*results))
