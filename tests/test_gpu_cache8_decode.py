@@ -415,3 +415,14 @@ def test_long_lists_of_grouped_heads(page, call):
         fn(c.cfg, c.q, c.view(), idx, n, c.out, c.tau, c.supp, c.workspace(ekv.EKV_OP_DECODE_SPARSE))
     torch.cuda.synchronize()
     check_all(c, "softmax" if call == "softmax" else "entmax", [[row[h // 4] for h in range(8)] for row in lists] if call == "group" else lists)
+
+
+def test_many_partial_results_of_many_heads():
+    """More workgroups to a KV head than the join takes at once, of more query heads than compute units; an uneven batch."""
+    c = Cache8(6, 64, 8, 16, [3000, 2990, 2500, 3000, 100, 2000], seed=71)
+    run_full(c, "softmax")
+    out, tau = c.out.cpu().numpy().astype(np.float64), c.tau.cpu().numpy()
+    rng = np.random.default_rng(0)
+    for b in range(6):
+        for h in rng.permutation(64)[:10].tolist() + [0, 63]:
+            check_softmax(c, b, h, np.arange(c.lens[b]), out[b, h], tau[b, h])
