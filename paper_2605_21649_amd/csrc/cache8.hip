@@ -356,7 +356,12 @@ template <typename T, bool ONE>
 __global__ __launch_bounds__(kAppendThreads) __attribute__((amdgpu_waves_per_eu(ONE ? 4 : 3)))
 void append8_kernel(const AppendArgs A) {
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int id = blockIdx.x * kAppendWaves + w, side = id & 1, h = (id >> 1) % A.Hkv, i0 = (id >> 1) / A.Hkv * A.block;
+  // Workgroups go to the XCDs in turn, and with fewer rows to a wavefront than to a page only every so many of them find the
+  // beginning of a run: in stretches every XCD gets its share (16384 tokens, pages of 64: 44.7 -> 42.3 us with 64 rows to a
+  // wavefront, 76 -> 48 with 16).
+  const unsigned x = blockIdx.x % kXcds, each = gridDim.x / kXcds, rest = gridDim.x % kXcds;
+  const int wg = (int)(x * each + min(x, rest) + blockIdx.x / kXcds);
+  const int id = wg * kAppendWaves + w, side = id & 1, h = (id >> 1) % A.Hkv, i0 = (id >> 1) / A.Hkv * A.block;
   if (i0 >= A.T) return;
   // lane l: rows i0 + l and i0 + 64 + l; a row goes on the run of the one before it, or it does not
   auto slot_of = [&](int i) {
@@ -413,12 +418,13 @@ void launch_cache8_append(const Dims& dm, const ekv_cache8_view& c, const ekv_st
   a.T = tok.max_tokens; a.B = dm.B; a.Hkv = dm.Hkv; a.HkvPool = dm.HkvPool; a.P = dm.P; a.Mmax = dm.Mmax;
   a.n_slots = (int64_t)c.n_phys_pages * dm.P;
   // Rows per wavefront: one where there are few, so that a step's rows go on at once; up to 32 where most rows are prompts', of
-  // which one in P begins a run and the others' wavefronts would only find that out.  us, 4096 wavefronts / 16384 where there
-  // are rows enough: 4096 tokens of prompts 11.9 / 17.3, 1024 single tokens 19.4 / 22.5, 32768 of prompts, which have 16384
-  // with 32 rows each, 50.6 (54.2 with 64; pages of 32 76 with 32 rows, 57 with 64).
+  // which one in P begins a run and the others' wavefronts would only find that out, 64 with pages that long.  us, 4096
+  // wavefronts / 16384 where there are rows enough: 4096 tokens of prompts 11.9 / 17.3, 1024 single tokens 19.4 / 22.5.  At most
+  // 16 rows / 32 / 64, 16384 tokens of prompts: pages of 4 41 / 44 / 53 (10000 tokens), of 16 32.6 / 30.0 / 28.7 (32768: 56.0 /
+  // 52.4 / 53.2), of 32 43.5 / 40.2 / 46.1, of 48 44.5 / 39.9 / 48.8, of 64 48.1 / 45.1 / 42.3.
   const bool one = dm.P <= 16;
   a.block = 1;
-  while (a.block < (one ? 32 : 64) && (long long)a.T * dm.Hkv * 2 / a.block > 4096) a.block *= 2;
+  while (a.block < (dm.P < 64 ? 32 : 64) && (long long)a.T * dm.Hkv * 2 / a.block > 4096) a.block *= 2;
   const long long waves = (long long)((a.T + a.block - 1) / a.block) * dm.Hkv * 2;
   const dim3 grid((unsigned)((waves + kAppendWaves - 1) / kAppendWaves)), block(kAppendThreads);
   if (dm.dtype == EKV_F32) {

@@ -10,6 +10,7 @@ constexpr int kD = 128;            // head_dim the kernels are written for
 constexpr int kLanesPerRow = 16;   // 16 lanes x 8 channels cover one 128-channel row
 constexpr int kRowsPerWave = 4;    // a 64-lane wavefront covers 4 rows per step
 constexpr int kWave = 64;
+constexpr int kXcds = 8;           // L2 caches, which workgroups go to in turn
 
 struct bf16_t { uint16_t bits; };
 

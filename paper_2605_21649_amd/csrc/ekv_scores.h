@@ -60,7 +60,6 @@ __device__ __forceinline__ int unit_slots(const ScoreArgs& A, int u) {
 // are as even as the lists allow, whatever the shapes.  Whole calls, us: 32K-token Gaussian step (lists of about 40 % of
 // the pages) 52.5 -> 46.6, decode over all pages of 3 x 21K float32 tokens within the refined step 147 -> 126.5; lists that
 // hardly overlap (2 % of a million tokens) 113.4 -> 112.6.
-constexpr int kXcds = 8;
 struct Part { int index, count; };             // this workgroup's part, parts per unit (1: units are not split)
 __device__ __forceinline__ Part unit_part(const ScoreArgs& A) {
   return {A.parts == kXcds ? (int)(blockIdx.x % kXcds) : 0, A.parts};
