@@ -2160,22 +2160,31 @@ void decode_row_kernel(const ScoreArgs S, const SolveArgs A) {
 // ------------------------------------------------------------------------------------------
 // the same over an 8-bit cache
 // ------------------------------------------------------------------------------------------
-// Pages of 8, 16, 32 or 64 tokens (groups of 64; an octet lies in one page).  The scores are those of decode8_scores.hip to the
-// last bit.
-template <typename TQ, bool DENSE, int NW, int TOKENS>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(4)))
+// OCTETS: pages of 8, 16, 32 or 64 tokens (groups of 64; an octet lies in one page and its place is wave-uniform).  Of other sizes
+// an octet may span pages and every lane looks up its own tokens'.  The scores are those of decode8_scores.hip to the last bit.
+template <typename TQ, bool DENSE, bool OCTETS, int NW, int TOKENS>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8 ? 2 : 4)))
 void decode8_row_kernel(const Score8Args S8, const SolveArgs A) {
   const ScoreArgs& S = S8.s;
-  __shared__ RowShared<NW, TOKENS, 64> sh;
+  __shared__ RowShared<NW, TOKENS, OCTETS ? 64 : 36> sh;
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int heads = S.Hq / S.Hkv, P = S.P, gp = 64 / P;
+  const int heads = S.Hq / S.Hkv, P = S.P, gp = OCTETS ? 64 / P : pmax_pages(P), GT = OCTETS ? 64 : gp * P;
   const int bh = group_on_one_xcd(blockIdx.x, gridDim.x, heads), b = bh / S.Hq, hkv = (bh - b * S.Hq) / heads;
   const int n = uniform_load(S.seq_lens + b);
   const int n_slots = DENSE ? clampi((n + P - 1) / P, 0, S.Mmax) : clampi(uniform_load(S.n_sel + bh), 0, S.cap);
   const float seed_z = A.ex.tau_seed != nullptr ? A.ex.tau_seed[bh] : NAN;
   const int n_groups = (n_slots + gp - 1) / gp, per_batch = 64 / gp;
   const e4m3_t* k_pool = (const e4m3_t*)S.k_pool;
-  const uint32_t lane_off = key_token(c) * kD + key_offset(c, g);
+  const uint32_t lane_off = (OCTETS ? key_token(c) * kD : 0) + key_offset(c, g);
+  // octet o of a group: page slot (8 bits) and token there of the lane's key (OCTETS: of the first), and of its first result
+  int k_at[8], z_at[8];
+  const int per_page = 65536 / P + 1;
+#pragma unroll
+  for (int o = 0; o < 8; ++o) {
+    auto at = [&](int token) { const int slot = div64(token, per_page); return slot | (token - slot * P) << 8; };
+    k_at[o] = OCTETS ? uniform(at(8 * o)) : at(min(8 * o + key_token(c), GT - 1));
+    z_at[o] = OCTETS ? k_at[o] : at(min(8 * o + 2 * g, GT - 2));
+  }
   const int copy = column_copy(c, 1);
   Query8<TQ, 1> qb;
   qb.load((const TQ*)S.q + (size_t)bh * kD);
@@ -2186,31 +2195,30 @@ void decode8_row_kernel(const Score8Args S8, const SolveArgs A) {
     const int l_lp = clampi(DENSE ? slot : S.page_idx[(size_t)bh * S.cap + slot], 0, S.Mmax - 1);
     const int l_page = clampi(S.block_table[(size_t)b * S.Mmax + l_lp], 0, S.n_phys - 1) * S.HkvPool + hkv;
     const float l_scale = S8.k_scale[l_page];
-    // octet o of item i: its page's lane and first token there
-    auto lane_of = [&](int i, int o) { return i * gp + uniform(8 * o / P); };
-    auto token_in_page = [&](int o) { return 8 * o & (P - 1); };
+    auto of_slot = [&](int v, int i, int slot) { return OCTETS ? __builtin_amdgcn_readlane(v, i * gp + slot) : __shfl(v, i * gp + slot); };
     auto request = [&](int i, int h, uint4 (&k)[4]) {                       // octets 4h .. 4h + 3; past the end: the last item again
 #pragma unroll
       for (int o = 0; o < 4; ++o) {
-        const int page = __builtin_amdgcn_readlane(l_page, lane_of(min(i, mine - 1), 4 * h + o));
-        k[o] = load16(k_pool + ((size_t)page * P + token_in_page(4 * h + o)) * kD + lane_off);
+        const int page = of_slot(l_page, min(i, mine - 1), k_at[4 * h + o] & 255);
+        k[o] = load16(k_pool + ((size_t)page * P + (k_at[4 * h + o] >> 8)) * kD + lane_off);
       }
     };
     float top = -INFINITY;
     auto consume = [&](int i, int h, const uint4 (&k)[4]) {
-      const int grp = g0 + NW * i, stored = min(64, (n_slots - grp * gp) * P);
+      const int grp = g0 + NW * i, stored = min(GT, (n_slots - grp * gp) * P);
       float2 z[4];
 #pragma unroll
       for (int o = 0; o < 4; ++o) {
-        const int from = lane_of(i, 4 * h + o), p = 32 * h + 8 * o + 2 * g;
-        octet_scores<TQ, 1>(k[o], __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l_scale), from)), qb, z[o].x, z[o].y);
-        const int left = p < stored ? n - (__builtin_amdgcn_readlane(l_lp, from) * P + token_in_page(4 * h + o) + 2 * g) : 0;
+        octet_scores<TQ, 1>(k[o], __int_as_float(of_slot(__float_as_int(l_scale), i, k_at[4 * h + o] & 255)), qb, z[o].x, z[o].y);
+        const int p = 32 * h + 8 * o + 2 * g;
+        const int lp = of_slot(l_lp, i, z_at[4 * h + o] & 255);  // by all lanes: behind the condition some sources would be idle
+        const int left = p < stored ? n - (lp * P + (z_at[4 * h + o] >> 8) + (OCTETS ? 2 * g : 0)) : 0;
         z[o].x = left > 0 ? S.zscale * z[o].x : -INFINITY;
         z[o].y = left > 1 ? S.zscale * z[o].y : -INFINITY;
         top = fmaxf(top, fmaxf(z[o].x, z[o].y));
       }
       const float2 v = copy_pair<1>(z[0], z[1], z[2], z[3], copy);
-      if (copy < 4 && 32 * h + 8 * copy + 2 * g < stored) *reinterpret_cast<float2*>(&sh.z[grp * 64 + 32 * h + 8 * copy + 2 * g]) = v;
+      if (copy < 4 && 32 * h + 8 * copy + 2 * g < stored) *reinterpret_cast<float2*>(&sh.z[grp * GT + 32 * h + 8 * copy + 2 * g]) = v;
       if (h == 1) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
@@ -2230,7 +2238,7 @@ void decode8_row_kernel(const Score8Args S8, const SolveArgs A) {
     }
   }
   __syncthreads();
-  const RowRef R{b, bh, bh, hkv, n_slots * P, 64, n_groups};
+  const RowRef R{b, bh, bh, hkv, n_slots * P, GT, n_groups};
   if (w == 0)
     bound_groups<(decltype(sh)::kGroups + 63) / 64, true>([&](int i) { return i < n_groups ? sh.umax[i] : -INFINITY; }, n_groups, A.beta, A.ibeta, sh);
   __syncthreads();
@@ -2384,23 +2392,42 @@ static void launch_rows(const Dims& dm, const ScoreArgs& sa, const SolveArgs& so
 // rows 13.6 / 9.5, 14.2 / 12.6, 14.2 / 15.1, 14.5 / 20.0, 256 rows of 1024 15.5 / 13.8; many rows read K once per head (2048 rows
 // of 1024 58 / 72), and so do lists shared by a group (2048 of 32 pages 21.9 / 30.5): these take two.
 constexpr int kRowTokensDense = 1024;
+// Page sizes whose octets may span pages: eight wavefronts for float32, which spill as sixteen (8 rows of 777 tokens, pages of 12,
+// 14.8 / 13.0).  Two launches / one: every page of 1 sequence with 8 heads, 100 / 480 / 1020 float32 tokens 14.4 / 10.4, 14.3 / 11.2,
+// 14.6 / 13.6, 256 rows of 1020 15.6 / 14.2; lists, 32 rows of 1311 / 2624 / 3936 tokens 15.7 / 14.4, 17.9 / 18.0, 19.8 / 22.9, 64 of 3936
+// 24.7 / 23.2 (pages of 48 21.1 / 25.5), 128 30.8 / 24.3 (of 36 33.7 / 31.5), 256 47.2 / 33.2, float32 49.1 / 33.6; 2048 lists of
+// 504 tokens 57.5 / 52.1, of 48-token pages 46.6 / 49.5, float32 47.9 / 52.4.
 template <typename TQ>
-static void launch_rows8(const Dims& dm, bool dense, const Score8Args& sa, const SolveArgs& so, hipStream_t st) {
+static void launch_rows8_octets(const Dims& dm, bool dense, const Score8Args& sa, const SolveArgs& so, hipStream_t st) {
   const int rows = dm.B * dm.Hq;
   if (dense)
-    hipLaunchKernelGGL((decode8_row_kernel<TQ, true, 16, kRowTokens>), dim3(rows), dim3(1024), 0, st, sa, so);
+    hipLaunchKernelGGL((decode8_row_kernel<TQ, true, true, 16, kRowTokens>), dim3(rows), dim3(1024), 0, st, sa, so);
   else if (rows <= device_compute_units())
-    hipLaunchKernelGGL((decode8_row_kernel<TQ, false, 16, kRowTokens>), dim3(rows), dim3(1024), 0, st, sa, so);
+    hipLaunchKernelGGL((decode8_row_kernel<TQ, false, true, 16, kRowTokens>), dim3(rows), dim3(1024), 0, st, sa, so);
   else
-    hipLaunchKernelGGL((decode8_row_kernel<TQ, false, 4, kRowTokensMany>), dim3(rows), dim3(256), 0, st, sa, so);
+    hipLaunchKernelGGL((decode8_row_kernel<TQ, false, true, 4, kRowTokensMany>), dim3(rows), dim3(256), 0, st, sa, so);
+}
+template <typename TQ>
+static void launch_rows8_any(const Dims& dm, bool dense, const Score8Args& sa, const SolveArgs& so, hipStream_t st) {
+  constexpr int NW = sizeof(TQ) == 4 ? 8 : 16;
+  const dim3 grid(dm.B * dm.Hq), block(64 * NW);
+  if (dense) hipLaunchKernelGGL((decode8_row_kernel<TQ, true, false, NW, kRowTokens>), grid, block, 0, st, sa, so);
+  else hipLaunchKernelGGL((decode8_row_kernel<TQ, false, false, NW, kRowTokens>), grid, block, 0, st, sa, so);
 }
 static bool rows8_in_one_launch(const Dims& dm, int mode, const Score8Args& sa, const SolveArgs& so, hipStream_t st) {
   const int cus = device_compute_units(), rows = dm.B * dm.Hq;
-  if (dm.P % 8 != 0 || 64 % dm.P != 0 || mode == kGroupList) return false;
-  if (mode == kAllPages ? rows > cus || (long long)dm.Mmax * dm.P > kRowTokensDense
-                        : (long long)dm.cap * dm.P > (rows > cus ? kRowTokensMany : kRowTokens)) return false;
-  if (dm.dtype == EKV_F32) launch_rows8<float>(dm, mode == kAllPages, sa, so, st);
-  else launch_rows8<bf16_t>(dm, mode == kAllPages, sa, so, st);
+  const bool octets = dm.P % 8 == 0 && 64 % dm.P == 0, dense = mode == kAllPages;
+  if (mode == kGroupList) return false;
+  if (rows > cus && (dense || !octets)) return false;
+  const int most = dense ? kRowTokensDense : rows > cus ? kRowTokensMany : octets || 2 * rows >= cus ? kRowTokens : kRowTokens / 2;
+  if ((long long)(dense ? dm.Mmax : dm.cap) * dm.P > most) return false;
+  if (octets) {
+    if (dm.dtype == EKV_F32) launch_rows8_octets<float>(dm, dense, sa, so, st);
+    else launch_rows8_octets<bf16_t>(dm, dense, sa, so, st);
+  } else {
+    if (dm.dtype == EKV_F32) launch_rows8_any<float>(dm, dense, sa, so, st);
+    else launch_rows8_any<bf16_t>(dm, dense, sa, so, st);
+  }
   return true;
 }
 

@@ -29,15 +29,16 @@ void decode8_scores_kernel(const Score8Args A8) {
   const int last = (DENSE ? A.Mmax : A.cap) - 1;
   // Octet o of an item: page slot and token of its keys (of the lane's one, without OCTETS), and of the lane's first result
   int k_slot[8], k_tok[8], z_slot[8], z_tok[8];
+  const int per_page = 65536 / P + 1;
 #pragma unroll
   for (int o = 0; o < 8; ++o) {
     if constexpr (OCTETS) {
       const int p = min(8 * o, GT - 8);
-      k_slot[o] = z_slot[o] = uniform(p / P); k_tok[o] = z_tok[o] = p - k_slot[o] * P;
+      k_slot[o] = z_slot[o] = uniform(div64(p, per_page)); k_tok[o] = z_tok[o] = p - k_slot[o] * P;
     } else {
       const int pk = min(8 * o + key_token(c), GT - 1), pz = min(8 * o + 2 * g, GT - 2);
-      k_slot[o] = pk / P; k_tok[o] = pk - k_slot[o] * P;
-      z_slot[o] = pz / P; z_tok[o] = pz - z_slot[o] * P;
+      k_slot[o] = div64(pk, per_page); k_tok[o] = pk - k_slot[o] * P;
+      z_slot[o] = div64(pz, per_page); z_tok[o] = pz - z_slot[o] * P;
     }
   }
   const uint32_t lane_off = (OCTETS ? key_token(c) * kD : 0) + key_offset(c, g);

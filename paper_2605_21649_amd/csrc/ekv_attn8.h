@@ -96,6 +96,9 @@ template <int G> __device__ __forceinline__ float2 copy_pair(float2 z0, float2 z
   return make_float2(upper ? bx : ax, upper ? by : ay);
 }
 
+// n / P for 0 <= n < 64 and P <= 64, per_page = 65536 / P + 1: off by at most n / 65536 < 1 / P before the cut
+__device__ __forceinline__ int div64(int n, int per_page) { return (n * per_page) >> 16; }
+
 // Where in a page's eight tokens the lane's 16 codes are, and which token that is.
 __device__ __forceinline__ int key_token(int c) { return c >> 1; }
 __device__ __forceinline__ uint32_t key_offset(int c, int g) { return (c & 1) * 64 + g * 16; }

@@ -426,3 +426,27 @@ def test_many_partial_results_of_many_heads():
     for b in range(6):
         for h in rng.permutation(64)[:10].tolist() + [0, 63]:
             check_softmax(c, b, h, np.arange(c.lens[b]), out[b, h], tau[b, h])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [4, 12, 20, 36, 48, 60, 16])
+def test_the_longest_rows_of_one_workgroup(page, dtype):
+    """Lists and sequences about as long as one workgroup takes from scores to output, and one page beyond, whose wavefronts have
+    several groups each; few rows and many, a full list, an empty one and some of every length between."""
+    rng = np.random.default_rng(page)
+    for B, tokens in ((2, 2048), (8, 4096), (2, 2048 + page), (8, 4096 + page)):
+        cap = tokens // page
+        c = Cache8(B, 16, 2, page, [2 * tokens - 301 * b for b in range(B)], seed=page, cap=cap, dtype=dtype)
+        lists = []
+        for b in range(B):
+            m = -(-c.lens[b] // page)
+            keep = [min(m, cap) if h == 0 else 0 if h == 1 else int(rng.integers(1, min(m, cap))) for h in range(16)]
+            lists.append([sorted(rng.permutation(m)[:k].tolist()) for k in keep])
+        idx, n = as_tensors(c, lists, cap, rng)
+        ekv.ekv_decode8_sparse(c.cfg, c.q, c.view(), idx, n, c.out, c.tau, c.supp, c.workspace(ekv.EKV_OP_DECODE_SPARSE))
+        torch.cuda.synchronize()
+        check_all(c, "entmax", lists)
+    for n in (1024 // page * page, 1024 // page * page - page // 2, 1024 // page * page + 1):
+        c = Cache8(3, 16, 2, page, [n, n - 600, 1], seed=n, dtype=dtype)
+        run_full(c, "entmax")
+        check_all(c, "entmax")
