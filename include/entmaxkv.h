@@ -385,7 +385,8 @@ ekv_status ekv_decode8_full(const ekv_config* cfg, const void* q, const ekv_cach
 
 /* Softmax attention over an 8-bit cache: restricted to page lists per query head as ekv_decode_sparse_softmax, and over every
  * page.  out f32 [B][Hq][d], lse f32 [B][Hq] (log-sum-exp of scale * q.k; -inf and a zero output for an empty row).
- * Workspaces EKV_OP_DECODE8_SPARSE_SOFTMAX, EKV_OP_DECODE8_FULL_SOFTMAX. */
+ * Workspaces EKV_OP_DECODE8_SPARSE_SOFTMAX, EKV_OP_DECODE8_FULL_SOFTMAX.  Range: capacities of fewer than 2^31 steps of 32 tokens, B *
+ * Hkv * ceil(Mmax * P / 32) (lists: B * Hq * ceil(cap * P / 32)), else EKV_ERR_UNSUPPORTED. */
 ekv_status ekv_decode8_sparse_softmax(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache,
                                       const int32_t* page_idx, const int32_t* n_sel, float* out, float* lse_sel,
                                       void* workspace, size_t workspace_bytes, void* stream);

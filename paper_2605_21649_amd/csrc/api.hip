@@ -468,6 +468,7 @@ static ekv_status decode8_softmax_common(const ekv_config* cfg, bool dense, cons
   if (s != EKV_OK) return s;
   if ((s = check_cache8(cache, dm, true)) != EKV_OK) return s;
   if (!ok_ptr(q) || !ok_ptr4(out) || !ok_ptr4(lse) || (!dense && (!ok_ptr4(page_idx) || !ok_ptr4(n_sel)))) return EKV_ERR_INVALID_ARG;
+  if (!softmax8_supported(dm, dense)) return EKV_ERR_UNSUPPORTED;
   if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < softmax8_ws_bytes(dm, dense)) return EKV_ERR_WORKSPACE;
   launch_decode8_softmax(dm, dense, q, *cache, page_idx, n_sel, out, lse, workspace, (hipStream_t)stream);
   return finish((hipStream_t)stream);

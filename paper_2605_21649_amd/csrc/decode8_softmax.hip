@@ -363,6 +363,10 @@ static int attn8_grid(const Dims& dm, bool dense, int most) {
 }
 static size_t attn8_pre_bytes(const Dims& dm, bool dense) { return (((size_t)attn8_units(dm, dense) + 1) * sizeof(int32_t) + 255) & ~(size_t)255; }
 
+bool softmax8_supported(const Dims& dm, bool dense) {
+  return attn8_units(dm, dense) * (((long long)(dense ? dm.Mmax : dm.cap) * dm.P + kStep - 1) / kStep) <= 0x7fffffff;
+}
+
 size_t softmax8_ws_bytes(const Dims& dm, bool dense) {
   const size_t recs = (size_t)attn8_units(dm, dense) + (size_t)attn8_grid(dm, dense, kMostWgs);
   return attn8_pre_bytes(dm, dense) + recs * (dense ? dm.G : 1) * kRec * sizeof(float);

@@ -96,6 +96,7 @@ void launch_cache8_append(const Dims& dm, const ekv_cache8_view& c, const ekv_st
 void launch_decode8_softmax(const Dims& dm, bool dense, const void* q, const ekv_cache8_view& c, const int32_t* page_idx,
                             const int32_t* n_sel, float* out, float* lse, void* ws, hipStream_t st);
 size_t softmax8_ws_bytes(const Dims& dm, bool dense);
+bool softmax8_supported(const Dims& dm, bool dense);   // the steps of all units are counted in 31 bits
 
 size_t select_topk_ws_bytes(const Dims& dm);
 size_t select_box_ws_bytes(const Dims& dm);

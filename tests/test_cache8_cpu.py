@@ -126,3 +126,13 @@ def test_the_binding_takes_maps_of_the_right_types_only():
     for bad in ((i32,), (slots, slots, i32), (slots, i32, torch.zeros(3, dtype=torch.int32)), (slots, i32, i32, slots), (slots, i32, i32, i32, slots)):
         with pytest.raises(AssertionError):
             ekv.token_map(*bad)
+
+
+def test_softmax_refuses_capacities_of_more_steps_than_it_counts():
+    """128 units (512 lists) of 2^30 tokens: 2^32 steps and more."""
+    cfg = good_cfg(batch=128 // good_cfg().n_kv_heads, max_pages_per_seq=(1 << 30) // good_cfg().page_size,
+                   max_sel_pages=(1 << 30) // good_cfg().page_size)
+    full = dict(cfg=cfg, q=A[6], cache=cache(), out=A[9], lse=A[10], ws=A[12], nbytes=1 << 60, stream=None)
+    assert status("ekv_decode8_full_softmax", *full.values()) == UNSUPPORTED
+    lists = dict(cfg=cfg, q=A[6], cache=cache(), page_idx=A[7], n_sel=A[8], out=A[9], lse=A[10], ws=A[12], nbytes=1 << 60, stream=None)
+    assert status("ekv_decode8_sparse_softmax", *lists.values()) == UNSUPPORTED
