@@ -317,3 +317,32 @@ def test_scales_at_the_ends_of_their_range():
         torch.cuda.synchronize()
         assert float(ks[0, 0]) == 2.0 ** exponent and float(vs[0, 0]) == 2.0 ** exponent
         assert int(kp[0, 0, 0, 0]) == (0x7E if big > 1 else 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("P", [4, 16, 20, 32, 48, 64])
+def test_large_appends_are_those_of_their_parts(P, dtype):
+    """So many rows that a wavefront has up to 64, against calls of a few hundred rows each on two ranges of the KV heads: the same
+    bits, beside the touched pages too."""
+    rng = np.random.default_rng(P)
+    heads, T = 8, 20000
+    n_phys = 2 * T // P + 3
+    kp, vp, ks, vs = Pools(n_phys, heads, P, rng).device()
+    runs, slots = deal(rng, rng.permutation(n_phys), P, T)
+    dev = torch.randn(len(slots), 3, heads, D, generator=torch.Generator(device="cuda").manual_seed(P), device="cuda")
+    dev = dev * 2.0 ** torch.randint(-3, 6, (len(slots), 1, 1, 1), device="cuda")
+    dev = dev.to(torch.bfloat16) if dtype == "bf16" else dev
+    where = torch.tensor(slots, dtype=torch.int64, device="cuda")
+    parts = [x.clone() for x in (kp, vp, ks, vs)]
+    cfg = ekv.make_config(1, heads, heads, D, P, dtype, 1.5, 1.0, 4, 4)
+    ekv.ekv_cache8_append(cfg, ekv.cache8_view(kp, vp, ks, vs), None, ekv.token_map(where), dev[:, 1], dev[:, 2])
+    cuts = [0] + [r[2] for r in runs[25::25]] + [len(slots)]
+    for h0, h1 in ((0, 3), (3, 8)):
+        cfg = ekv.make_config(1, h1 - h0, h1 - h0, D, P, dtype, 1.5, 1.0, 4, 4, pool_kv_heads=heads)
+        v = ekv.cache8_view(*parts)
+        view = ekv.ekv_cache8_view(v.k_pool + h0 * P * D, v.v_pool + h0 * P * D, v.k_scale + 4 * h0, v.v_scale + 4 * h0, None, None, n_phys)
+        for a, b in zip(cuts, cuts[1:]):
+            ekv.ekv_cache8_append(cfg, view, None, ekv.token_map(where[a:b]), dev[a:b, 1, h0:h1], dev[a:b, 2, h0:h1])
+    torch.cuda.synchronize()
+    for whole, part in zip((kp, vp, ks, vs), parts):
+        assert torch.equal(whole.view(torch.uint8), part.view(torch.uint8))
