@@ -9,8 +9,9 @@ namespace ekv {
 constexpr int kHold8 = 8192;            // scores a wavefront holds back
 constexpr int kHold8UnitsMax = 4096;    // the most units of such a launch
 
-// Pages of 8, 16, 32 or 64 tokens: items of 64.  One workgroup of four wavefronts per compute unit; a wavefront has one item (8 KB)
-// in flight, each octet requested anew as it is consumed.  us, one item / two / four / eight, eight wavefronts with half the LDS each,
+// Pages of 8, 16, 32 or 64 tokens: items of 64 (with shorter ones a wavefront has less in flight: 4 x 65536 tokens in pages of 40 take
+// 71 us by chunks and 84 like this).  One workgroup of four wavefronts per compute unit; a wavefront has one item (8 KB) in flight,
+// each octet requested anew as it is consumed.  us, one item / two / four / eight, eight wavefronts with half the LDS each,
 // sixteen with a quarter: 4 x 131072 tokens 112.9 / 112.9 / 115.2 / 124.4, 113.5, 116.2; 1 x 1048576 221 / 221 / 224 / 227, 234, 253;
 // 64 x 8192 124 / 123 / 125 / 129, 126, 130.
 template <typename T, int G, int PT>
