@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libentmaxkv.so")
 
 EKV_OK = 0
 EKV_F32, EKV_BF16 = 0, 1
+_TYPES = {EKV_F32: torch.float32, EKV_BF16: torch.bfloat16}
 EKV_SCORE_BOX, EKV_SCORE_GAUSS, EKV_SCORE_BOTH, EKV_SCORE_GROUP_MAX, EKV_SCORE_BOX8 = 1, 2, 3, 4, 8
 EKV_STATIC_SCRATCH_BYTES = 32 << 20
 EKV_OP_SELECT_TOPK, EKV_OP_SELECT_GAUSS, EKV_OP_DECODE_SPARSE, EKV_OP_DECODE_FULL, \
@@ -304,16 +305,19 @@ def ekv_release_pages(cfg, release, seq_lens, block_table, free_pages, n_free, n
                                             _ptr(n_left), _stream(stream)))
 
 
-def _rows(t):
+def _rows(t, shape=None):
     """Pointer and row stride of [tokens][Hkv][d] rows that may be parts of longer ones."""
-    n, st = t.shape, t.stride()                  # asked for once: an attribute of a tensor is a tenth of a microsecond
+    n, st = shape or t.shape, t.stride()         # asked for once: an attribute of a tensor is a tenth of a microsecond
     assert len(n) == 3 and st[2] == 1 and (n[1] == 1 or st[1] == n[2]), "the heads of a row must follow each other"
     return t.data_ptr(), st[0] if n[0] > 1 else n[1] * n[2]
 
 
 def ekv_cache8_append(cfg, cache, stats, tokens, k_new, v_new, stream=None):
-    assert k_new.shape[0] >= tokens.max_tokens and v_new.shape[0] >= tokens.max_tokens, "a row for every token of the map"
-    (k, ks), (v, vs) = _rows(k_new), _rows(v_new)
+    kn, vn, rows, t = k_new.shape, v_new.shape, tokens.max_tokens, _TYPES.get(cfg.kv_dtype)
+    (k, ks), (v, vs) = _rows(k_new, kn), _rows(v_new, vn)
+    assert kn[0] >= rows and vn[0] >= rows, "a row for every token of the map"
+    assert kn[1] == vn[1] == cfg.n_kv_heads and kn[2] == vn[2] == cfg.head_dim, "rows of the config's KV heads and head size"
+    assert k_new.dtype is t and v_new.dtype is t, "rows of the config's type"
     _check(load_library().ekv_cache8_append(byref(cfg), byref(cache), byref(stats) if stats is not None else None,
                                             byref(tokens), k, ks, v, vs, _stream(stream)))
 

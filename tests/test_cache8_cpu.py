@@ -136,3 +136,28 @@ def test_softmax_refuses_capacities_of_more_steps_than_it_counts():
     assert status("ekv_decode8_full_softmax", *full.values()) == UNSUPPORTED
     lists = dict(cfg=cfg, q=A[6], cache=cache(), page_idx=A[7], n_sel=A[8], out=A[9], lse=A[10], ws=A[12], nbytes=1 << 60, stream=None)
     assert status("ekv_decode8_sparse_softmax", *lists.values()) == UNSUPPORTED
+
+
+def test_the_binding_takes_rows_of_the_configs_type_and_heads_only(monkeypatch):
+    """The library goes by the config's type and heads: rows of another are refused before it is called."""
+    called = []
+
+    class Library:
+        def ekv_cache8_append(self, *args):
+            called.append(args)
+            return 0
+
+    monkeypatch.setattr(ekv, "load_library", Library)
+    monkeypatch.setattr(ekv, "_stream", lambda stream: None)
+    cfg = good_cfg(n_kv_heads=4, n_q_heads=8, kv_dtype="bf16")
+    rows = torch.zeros(5, 3, 4, 128, dtype=torch.bfloat16)
+    k, v = rows[:, 1], rows[:, 2]
+    ekv.ekv_cache8_append(cfg, cache(), None, tokens(max_tokens=5), k, v)
+    assert len(called) == 1
+    for bad in ((k.float(), v), (k, v.float()), (k.half(), v.half()), (k[:, :2], v), (k, v[:, 1:]), (k[:, :3], v[:, :3]),
+                (k[..., :64], v[..., :64]), (torch.cat((k, k), 1), v)):
+        with pytest.raises(AssertionError):
+            ekv.ekv_cache8_append(cfg, cache(), None, tokens(max_tokens=5), *bad)
+    with pytest.raises(AssertionError):                      # bfloat16 rows where the library reads float32
+        ekv.ekv_cache8_append(good_cfg(n_kv_heads=4, n_q_heads=8, kv_dtype="f32"), cache(), None, tokens(max_tokens=5), k, v)
+    assert len(called) == 1
