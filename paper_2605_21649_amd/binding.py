@@ -180,6 +180,11 @@ def stats_view(box, gauss, box8=None):
 
 
 def cache8_view(k_pool, v_pool, k_scale, v_scale, block_table=None, seq_lens=None):
+    assert k_pool.element_size() == 1 and v_pool.element_size() == 1 and k_pool.shape == v_pool.shape, "pools of one shape, a byte per element"
+    for t in (k_scale, v_scale):
+        assert t.dtype == torch.float32 and t.shape == k_pool.shape[:2], "scales: float32, one for every page and head of the pools"
+    for t in (block_table, seq_lens):
+        assert t is None or t.dtype == torch.int32, "block_table and seq_lens are int32"
     return ekv_cache8_view(_ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale), _ptr(block_table), _ptr(seq_lens),
                            k_pool.shape[0])
 
@@ -322,17 +327,23 @@ def ekv_cache8_append(cfg, cache, stats, tokens, k_new, v_new, stream=None):
                                             byref(tokens), k, ks, v, vs, _stream(stream)))
 
 
+def _query(cfg, q):
+    assert q.dtype is _TYPES.get(cfg.kv_dtype), "queries of the config's type"
+    assert q.numel() >= cfg.batch * cfg.n_q_heads * cfg.head_dim, "a query for every sequence and head"
+    return _ptr(q)
+
+
 def ekv_decode8_sparse(cfg, q, cache, page_idx, n_sel, out, tau, supp, workspace, extras=None, stream=None):
     nbytes = workspace.numel() * workspace.element_size()
     ex = byref(extras) if extras is not None else None
-    _check(load_library().ekv_decode8_sparse(byref(cfg), _ptr(q), byref(cache), _ptr(page_idx), _ptr(n_sel), _ptr(out),
+    _check(load_library().ekv_decode8_sparse(byref(cfg), _query(cfg, q), byref(cache), _ptr(page_idx), _ptr(n_sel), _ptr(out),
                                              _ptr(tau), _ptr(supp), ex, _ptr(workspace), nbytes, _stream(stream)))
 
 
 def ekv_decode8_sparse_group(cfg, q, cache, page_idx, n_sel, out, tau, supp, workspace, extras=None, stream=None):
     nbytes = workspace.numel() * workspace.element_size()
     ex = byref(extras) if extras is not None else None
-    _check(load_library().ekv_decode8_sparse_group(byref(cfg), _ptr(q), byref(cache), _ptr(page_idx), _ptr(n_sel),
+    _check(load_library().ekv_decode8_sparse_group(byref(cfg), _query(cfg, q), byref(cache), _ptr(page_idx), _ptr(n_sel),
                                                    _ptr(out), _ptr(tau), _ptr(supp), ex, _ptr(workspace), nbytes,
                                                    _stream(stream)))
 
@@ -340,17 +351,17 @@ def ekv_decode8_sparse_group(cfg, q, cache, page_idx, n_sel, out, tau, supp, wor
 def ekv_decode8_full(cfg, q, cache, out, tau, supp, workspace, extras=None, stream=None):
     nbytes = workspace.numel() * workspace.element_size()
     ex = byref(extras) if extras is not None else None
-    _check(load_library().ekv_decode8_full(byref(cfg), _ptr(q), byref(cache), _ptr(out), _ptr(tau), _ptr(supp), ex,
+    _check(load_library().ekv_decode8_full(byref(cfg), _query(cfg, q), byref(cache), _ptr(out), _ptr(tau), _ptr(supp), ex,
                                            _ptr(workspace), nbytes, _stream(stream)))
 
 
 def ekv_decode8_sparse_softmax(cfg, q, cache, page_idx, n_sel, out, lse_sel, workspace, stream=None):
     nbytes = workspace.numel() * workspace.element_size()
-    _check(load_library().ekv_decode8_sparse_softmax(byref(cfg), _ptr(q), byref(cache), _ptr(page_idx), _ptr(n_sel),
+    _check(load_library().ekv_decode8_sparse_softmax(byref(cfg), _query(cfg, q), byref(cache), _ptr(page_idx), _ptr(n_sel),
                                                      _ptr(out), _ptr(lse_sel), _ptr(workspace), nbytes, _stream(stream)))
 
 
 def ekv_decode8_full_softmax(cfg, q, cache, out, lse, workspace, stream=None):
     nbytes = workspace.numel() * workspace.element_size()
-    _check(load_library().ekv_decode8_full_softmax(byref(cfg), _ptr(q), byref(cache), _ptr(out), _ptr(lse),
+    _check(load_library().ekv_decode8_full_softmax(byref(cfg), _query(cfg, q), byref(cache), _ptr(out), _ptr(lse),
                                                    _ptr(workspace), nbytes, _stream(stream)))

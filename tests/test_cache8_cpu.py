@@ -161,3 +161,36 @@ def test_the_binding_takes_rows_of_the_configs_type_and_heads_only(monkeypatch):
     with pytest.raises(AssertionError):                      # bfloat16 rows where the library reads float32
         ekv.ekv_cache8_append(good_cfg(n_kv_heads=4, n_q_heads=8, kv_dtype="f32"), cache(), None, tokens(max_tokens=5), k, v)
     assert len(called) == 1
+
+
+def test_the_binding_takes_queries_of_the_configs_type_and_size_only(monkeypatch):
+    called = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: called.append(name) or 0
+
+    monkeypatch.setattr(ekv, "load_library", Library)
+    monkeypatch.setattr(ekv, "_stream", lambda stream: None)
+    cfg = good_cfg(batch=2, n_kv_heads=4, n_q_heads=8, kv_dtype="f32")
+    q, x = torch.zeros(2, 8, 128), torch.zeros(4)
+    for name, n_args in (("sparse", 6), ("sparse_group", 6), ("full", 4), ("sparse_softmax", 5), ("full_softmax", 3)):
+        call = getattr(ekv, "ekv_decode8_" + name)
+        call(cfg, q, cache(), *[x] * n_args)
+        call(cfg, torch.zeros(3, 8, 128), cache(), *[x] * n_args)                # of a larger batch: its first rows
+        for bad in (q.bfloat16(), q.double(), q[:1], q[:, :4].contiguous(), q[..., :64].contiguous()):
+            with pytest.raises(AssertionError):
+                call(cfg, bad, cache(), *[x] * n_args)
+    assert len(called) == 10
+
+
+def test_the_binding_takes_pools_and_scales_that_belong_together_only():
+    k, v = (torch.zeros(6, 2, 16, 128, dtype=torch.uint8) for _ in range(2))
+    ks, vs = (torch.ones(6, 2) for _ in range(2))
+    table, lens = torch.zeros(1, 6, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    assert ekv.cache8_view(k, v, ks, vs, table, lens).n_phys_pages == 6
+    assert ekv.cache8_view(k.view(torch.float8_e4m3fn), v.view(torch.float8_e4m3fn), ks, vs).n_phys_pages == 6
+    for bad in ((k.bfloat16(), v, ks, vs), (k, v.bfloat16(), ks, vs), (k, v[:5], ks, vs), (k, v, ks.bfloat16(), vs), (k, v, ks, vs.double()),
+                (k, v, ks[:5], vs), (k, v, ks, vs[:, :1].contiguous()), (k, v, ks, vs, table.long(), lens), (k, v, ks, vs, table, lens.long())):
+        with pytest.raises(AssertionError):
+            ekv.cache8_view(*bad)
