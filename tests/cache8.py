@@ -121,3 +121,68 @@ def score_error(q, K, scale):
     if not len(K):
         return 0.0
     return float((3 * 128 + 2) * 2.0 ** -24 * scale * (np.abs(K) @ np.abs(q)).max())
+
+
+class Large:
+    """An 8-bit cache of sequences too long to make on the host, for comparisons of samples: signed values of ordinary size, pages of
+    different magnitude, NaN codes behind every last token and NaN scales where no token is."""
+
+    def __init__(self, q_heads, kv_heads, page, lens, cap=None, dtype="bf16", seed=0, row_pages=None, flat=1.0, device="cuda"):
+        g = torch.Generator(device=device).manual_seed(seed)
+        self.B, self.Hq, self.Hkv, self.P, self.G = len(lens), q_heads, kv_heads, page, q_heads // kv_heads
+        self.lens, self.alpha, self.scale = list(lens), 1.5, flat / np.sqrt(D)
+        self.M = row_pages or -(-max(lens) // page)
+        self.cap = cap or self.M
+        n_phys = self.B * self.M
+        self.table = torch.randperm(n_phys, generator=g, device=device).view(self.B, self.M).to(torch.int32)
+        self.seq_lens = torch.tensor(self.lens, dtype=torch.int32, device=device)
+        self.pools, self.scales = [], []
+        behind = torch.arange(self.M * page, device=device).view(1, self.M, page) >= self.seq_lens[:, None, None]
+        for side in range(2):
+            code = torch.empty(n_phys, kv_heads, page, D, dtype=torch.uint8, device=device)
+            step = max(1, (1 << 26) // (kv_heads * page * D))
+            for lo in range(0, n_phys, step):
+                x = torch.randn(min(step, n_phys - lo), kv_heads, page, D, generator=g, device=device)
+                code[lo:lo + x.shape[0]] = (x * 100.0).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+            scale = 2.0 ** torch.randint(-8, -5, (n_phys, kv_heads), generator=g, device=device).float()      # sizes of 0.4 to 1.6
+            for b in range(self.B):
+                rows = self.table[b].long()
+                code[rows] = torch.where(behind[b][:, None, :, None], 0x7F if side else 0xFF, code[rows])
+                scale[rows[behind[b].all(1)]] = float("nan")
+            self.pools.append(code)
+            self.scales.append(scale)
+        dt = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+        self.q = torch.randn(self.B, q_heads, D, generator=g, device=device).to(dt)
+        self.cfg = ekv.make_config(self.B, q_heads, kv_heads, D, page, dtype, self.alpha, self.scale, self.M, self.cap)
+        self.out = torch.full((self.B, q_heads, D), float("nan"), device=device)
+        self.tau = torch.full((self.B, q_heads), float("nan"), device=device)
+        self.supp = torch.full((self.B, q_heads), -1, dtype=torch.int32, device=device)
+
+    view = lambda self: ekv.cache8_view(*self.pools, *self.scales, self.table, self.seq_lens)  # noqa: E731
+    workspace = Cache8.workspace
+    query = Cache8.query
+    tokens = Cache8.tokens
+
+    def keys_values(self, b, h):
+        n, P = self.lens[b], self.P
+        rows = self.table[b, :-(-n // P)].long()
+        return tuple((VALUES[self.pools[i][rows, h].cpu().numpy()] * self.scales[i][rows, h].cpu().numpy().astype(np.float64)[:, None, None])
+                     .reshape(-1, D)[:n] for i in range(2))
+
+
+def entmax_limits(ref, q, K, V, alpha, scale):
+    """How far a threshold, and each channel of the output, may be from the oracle's `ref` (over K and V): tau moves by the scores'
+    error times alpha - 1 and the solve stops within 4e-6 max(1, |tau|); weights p = x^beta move with x by twice that, and
+    float32 sums of the support follow."""
+    a = alpha - 1.0
+    e = a * score_error(q, K, scale) + 4e-6 * max(1.0, abs(ref["tau"]))
+    x = a * ref["s"] - ref["tau"]
+    dp = np.maximum(x + 2 * e, 0.0) ** (1.0 / a) - np.maximum(x - 2 * e, 0.0) ** (1.0 / a)
+    return e, dp @ np.abs(V) + (len(ref["support"]) + 8) * 2.0 ** -24 * (ref["p"] @ np.abs(V))
+
+
+def softmax_limits(ref, q, K, V, scale):
+    """The same for a log-sum-exp and its output: weights move by the factor exp(2 e), and float32 sums follow."""
+    e = score_error(q, K, scale) + 8 * 2.0 ** -24 * max(1.0, 2.0 * np.abs(ref["s"]).max())
+    return (e + 8 * 2.0 ** -24 * max(1.0, abs(ref["lse"])) + len(K) * 2.0 ** -24,
+            (np.expm1(2 * e) + (len(K) + 64) * 2.0 ** -24) * (ref["p"] @ np.abs(V)))

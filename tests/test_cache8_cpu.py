@@ -194,3 +194,35 @@ def test_the_binding_takes_pools_and_scales_that_belong_together_only():
                 (k, v, ks[:5], vs), (k, v, ks, vs[:, :1].contiguous()), (k, v, ks, vs, table.long(), lens), (k, v, ks, vs, table, lens.long())):
         with pytest.raises(AssertionError):
             ekv.cache8_view(*bad)
+
+
+@pytest.mark.parametrize("kind", ["entmax", "softmax"])
+def test_the_limits_of_outputs_tell_right_from_wrong(kind):
+    """Mistakes planted in the oracle -- the scale of one page of values, one page's values in another's place, a head's keys with
+    its neighbour's values, one token left out -- change the output by more than the GPU tests allow, which is a small part of it."""
+    from oracle import entmaxkv_oracle as orc
+    from tests import cache8 as c8
+    import numpy as np
+
+    def attend(q, K, V):
+        return orc.entmax_attention(q, K, V, 1.5, c.scale) if kind == "entmax" else orc.softmax_attention(q, K, V, c.scale)
+
+    for n, page in ((4000, 12), (900, 16)):
+        c = c8.Large(4, 2, page, [n], seed=n, flat=0.3, device="cpu")
+        for h in range(4):
+            q, (K, V) = c.query(0, h), c.keys_values(0, h // 2)
+            ref = attend(q, K, V)
+            limit = (c8.entmax_limits(ref, q, K, V, 1.5, c.scale) if kind == "entmax" else c8.softmax_limits(ref, q, K, V, c.scale))[1]
+            assert np.linalg.norm(limit) <= 0.1 * np.linalg.norm(ref["o"])
+            top = int(np.argmax(ref["p"]))
+            at = slice(top // page * page, top // page * page + page)
+            wrong = []
+            for change in (lambda x: 2.0 * x, lambda x: 0.5 * x, lambda x: np.roll(V, page, 0)[at], lambda x: 0.0 * x):
+                W = V.copy()
+                W[at] = change(W[at])
+                wrong.append(attend(q, K, W)["o"])
+            wrong.append(attend(q, K, c.keys_values(0, 1 - h // 2)[1])["o"])
+            rest = np.arange(n) != top
+            wrong.append(attend(q, K[rest], V[rest])["o"])
+            wrong.append(np.zeros(128))
+            assert all(np.any(np.abs(o - ref["o"]) > limit) for o in wrong)

@@ -1,0 +1,83 @@
+"""Attention over the 8-bit cache where a wavefront has many items and a launch many units: outputs, value side included, of samples
+against the oracle, with limits that are a small part of the outputs."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import entmaxkv_oracle as orc
+from paper_2605_21649_amd import binding as ekv
+from tests.cache8 import Large, entmax_limits, softmax_limits
+
+pytestmark = pytest.mark.gpu
+
+CALLS = {"full": ekv.EKV_OP_DECODE_FULL, "sparse": ekv.EKV_OP_DECODE_SPARSE, "sparse_group": ekv.EKV_OP_DECODE_SPARSE,
+         "full_softmax": ekv.EKV_OP_DECODE8_FULL_SOFTMAX, "sparse_softmax": ekv.EKV_OP_DECODE8_SPARSE_SOFTMAX}
+
+
+def run(c, call, lists=()):
+    c.out.fill_(float("nan"))
+    c.tau.fill_(float("nan"))
+    ws = c.workspace(CALLS[call])
+    getattr(ekv, "ekv_decode8_" + call)(c.cfg, c.q, c.view(), *lists, c.out, c.tau, *(() if "softmax" in call else (c.supp,)), ws)
+    torch.cuda.synchronize()
+
+
+def check_sample(c, call, b, h, tok):
+    """One row against the oracle on the tokens of its list (or all)."""
+    out, first = c.out[b, h].cpu().numpy().astype(np.float64), float(c.tau[b, h])
+    soft = "softmax" in call
+    if len(tok) == 0:
+        assert not out.any() and first == (-np.inf if soft else np.inf)
+        return
+    K, V = (x[tok] for x in c.keys_values(b, h // c.G))
+    q = c.query(b, h)
+    if soft:
+        ref = orc.softmax_attention(q, K, V, c.scale)
+        e, limit = softmax_limits(ref, q, K, V, c.scale)
+    else:
+        ref = orc.entmax_attention(q, K, V, c.alpha, c.scale)
+        e, limit = entmax_limits(ref, q, K, V, c.alpha, c.scale)
+    assert len(tok) < 2 or np.linalg.norm(limit) <= 0.2 * np.linalg.norm(ref["o"])     # wrong rows, scales or weights are beyond it
+    assert abs(first - ref["lse" if soft else "tau"]) <= e, (b, h)
+    assert np.all(np.abs(out - ref["o"]) <= limit), (b, h, (np.abs(out - ref["o"]) / limit).max())
+
+
+def random_lists(c, n_lists, seed):
+    """Ascending page lists of every length up to the capacity, with anything behind their ends."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    m = ((c.seq_lens + c.P - 1) // c.P)[:, None, None]
+    score = torch.rand(c.B, n_lists, c.M, generator=g, device="cuda")
+    score = torch.where(torch.arange(c.M, device="cuda") < m, score, -1.0)
+    idx = score.topk(c.cap, dim=-1).indices
+    most = m[..., 0].clamp(max=c.cap)
+    n = (most - (torch.rand(c.B, n_lists, generator=g, device="cuda") * 0.4 * most).int()).to(torch.int32)
+    taken = torch.arange(c.cap, device="cuda") < n[..., None]
+    idx = torch.where(taken, idx, c.M + 1).sort(-1).values
+    junk = torch.randint(-3, c.M + 3, idx.shape, generator=g, device="cuda")
+    return torch.where(taken, idx, junk).to(torch.int32), n
+
+
+def tokens_of(c, call, lists, b, h):
+    if not lists:
+        return np.arange(c.lens[b])
+    i = h // c.G if call == "sparse_group" else h
+    return c.tokens(b, lists[0][b, i, :int(lists[1][b, i])].cpu().numpy())
+
+
+@pytest.mark.parametrize("page,heads,dtype", [
+    (4, (16, 8), "bf16"), (12, (16, 8), "bf16"), (16, (16, 8), "bf16"), (20, (16, 8), "bf16"), (24, (16, 8), "bf16"), (44, (16, 8), "bf16"),
+    (56, (16, 8), "bf16"), (64, (16, 8), "bf16"), (16, (8, 8), "bf16"), (12, (8, 8), "bf16"), (40, (32, 8), "bf16"), (16, (32, 4), "bf16"),
+    (12, (32, 4), "bf16"), (12, (16, 8), "f32"), (16, (16, 8), "f32"), (40, (8, 8), "f32")])
+def test_outputs_where_wavefronts_have_many_items(page, heads, dtype):
+    """24 uneven sequences of up to 12000 tokens: 18000 groups of tokens and more for 16384 wavefronts at most over all pages, three
+    to six a wavefront over lists of about 4000 tokens, whose ends fall on any lane."""
+    lens = [12000 - 487 * b for b in range(24)]
+    c = Large(*heads, page, lens, cap=4000 // page, dtype=dtype, seed=page + heads[0], flat=0.3)
+    rng = np.random.default_rng(page)
+    for call in CALLS:
+        lists = random_lists(c, c.Hkv if call == "sparse_group" else c.Hq, page) if "sparse" in call else ()
+        run(c, call, lists)
+        assert torch.isfinite(c.out).all() and torch.isfinite(c.tau).all()
+        for b in (0, 7, 13, 23):
+            for h in rng.permutation(c.Hq)[:2].tolist() + [c.Hq - 1]:
+                check_sample(c, call, b, h, tokens_of(c, call, lists, b, h))
