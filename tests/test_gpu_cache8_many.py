@@ -6,7 +6,7 @@ import torch
 
 from oracle import entmaxkv_oracle as orc
 from paper_2605_21649_amd import binding as ekv
-from tests.cache8 import Large, entmax_limits, softmax_limits
+from tests.cache8 import D, Cache8, Large, entmax_limits, softmax_limits
 
 pytestmark = pytest.mark.gpu
 
@@ -80,4 +80,34 @@ def test_outputs_where_wavefronts_have_many_items(page, heads, dtype):
         assert torch.isfinite(c.out).all() and torch.isfinite(c.tau).all()
         for b in (0, 7, 13, 23):
             for h in rng.permutation(c.Hq)[:2].tolist() + [c.Hq - 1]:
+                check_sample(c, call, b, h, tokens_of(c, call, lists, b, h))
+
+
+@pytest.mark.parametrize("page,heads,dtype", [(16, (8, 8), "bf16"), (12, (8, 8), "f32"), (16, (16, 8), "f32"), (12, (16, 8), "bf16")])
+def test_more_units_than_a_workgroup_keeps_sums_of(page, heads, dtype):
+    """1100 sequences, most of them empty, of 8 KV heads in a capacity beyond what one workgroup takes: the sums over the units before
+    come from a launch of their own, for every kind of call."""
+    lens = [0] * 1100
+    for b, n in ((0, 5000), (1, 1), (2, 8320), (500, 33), (501, 2500), (777, 64), (1098, 1), (1099, 4111)):
+        lens[b] = n
+    c = Cache8(1100, *heads, page, lens, row_pages=8400 // page, cap=8400 // page, scale=0.3 / np.sqrt(D), dtype=dtype, seed=page)
+    assert c.B * c.Hkv > 8192 and c.cap * page > 8192
+    rng = np.random.default_rng(page)
+    for call in CALLS:
+        n_lists = c.Hkv if call == "sparse_group" else c.Hq
+        idx, n = torch.zeros(c.B, n_lists, c.cap, dtype=torch.int32, device="cuda"), torch.zeros(c.B, n_lists, dtype=torch.int32, device="cuda")
+        if "sparse" in call:
+            for b, length in enumerate(lens):
+                m = -(-length // page)
+                for i in range(n_lists if m else 0):
+                    k = int(rng.integers(max(1, m // 2), m + 1))
+                    idx[b, i, :k] = torch.from_numpy(np.sort(rng.permutation(m)[:k]).astype(np.int32))
+                    n[b, i] = k
+            n[3], n[1000] = 5, c.cap                              # lists of sequences that have no token
+        lists = (idx, n) if "sparse" in call else ()
+        run(c, call, lists)
+        assert torch.isfinite(c.out).all() and not c.out[c.seq_lens == 0].any()
+        assert bool((c.tau[c.seq_lens == 0] == (-np.inf if "softmax" in call else np.inf)).all())
+        for b in [b for b, length in enumerate(lens) if length]:
+            for h in rng.permutation(c.Hq)[:3].tolist():
                 check_sample(c, call, b, h, tokens_of(c, call, lists, b, h))
