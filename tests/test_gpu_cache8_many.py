@@ -6,6 +6,7 @@ import torch
 
 from oracle import entmaxkv_oracle as orc
 from paper_2605_21649_amd import binding as ekv
+from tests import test_gpu_cache8_decode as decodes
 from tests.cache8 import D, Cache8, Large, entmax_limits, softmax_limits
 
 pytestmark = pytest.mark.gpu
@@ -111,3 +112,17 @@ def test_more_units_than_a_workgroup_keeps_sums_of(page, heads, dtype):
         for b in [b for b, length in enumerate(lens) if length]:
             for h in rng.permutation(c.Hq)[:3].tolist():
                 check_sample(c, call, b, h, tokens_of(c, call, lists, b, h))
+
+
+@pytest.mark.parametrize("heads,dtype", [((2, 2), "bf16"), ((4, 2), "f32"), ((8, 2), "bf16"), ((16, 2), "f32")])
+@pytest.mark.parametrize("page", [24, 40, 56])
+def test_pages_of_whole_octets_that_do_not_make_64(page, heads, dtype):
+    for kind in ("entmax", "softmax"):
+        decodes.test_every_page_of_ragged_sequences(page, heads, dtype, kind)
+    for call in ("sparse", "group", "softmax"):
+        decodes.test_page_lists(page, heads, dtype, call)
+    if heads == (2, 2):
+        decodes.test_steps_of_one_workgroup(page)
+        decodes.test_the_longest_rows_of_one_workgroup(page, dtype)
+        for call in ("sparse", "group", "softmax"):
+            decodes.test_long_lists_of_grouped_heads(page, call)
