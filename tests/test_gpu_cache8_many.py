@@ -1,13 +1,13 @@
 """Attention over the 8-bit cache where a wavefront has many items and a launch many units: outputs, value side included, of samples
-against the oracle, with limits that are a small part of the outputs."""
+against the oracle, with limits that are a small part of the outputs.  Statistics of large appends."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import entmaxkv_oracle as orc
 from paper_2605_21649_amd import binding as ekv
-from tests import test_gpu_cache8_decode as decodes
-from tests.cache8 import D, Cache8, Large, entmax_limits, softmax_limits
+from tests import test_gpu_cache8_append as appends, test_gpu_cache8_decode as decodes
+from tests.cache8 import D, VALUES, Cache8, Large, entmax_limits, softmax_limits
 
 pytestmark = pytest.mark.gpu
 
@@ -126,3 +126,54 @@ def test_pages_of_whole_octets_that_do_not_make_64(page, heads, dtype):
         decodes.test_the_longest_rows_of_one_workgroup(page, dtype)
         for call in ("sparse", "group", "softmax"):
             decodes.test_long_lists_of_grouped_heads(page, call)
+
+
+@pytest.mark.parametrize("dtype,with8", [("bf16", False), ("bf16", True), ("f32", False)])
+@pytest.mark.parametrize("page", [8, 20, 24, 28, 48, 60])
+def test_statistics_of_small_steps(page, dtype, with8):
+    appends.test_statistics_are_those_of_the_stored_keys(page, dtype, with8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [4, 16, 20, 28, 32, 48, 60, 64])
+def test_statistics_of_large_appends(page, dtype):
+    """Three steps of 20000 rows and more, of which a wavefront has up to 32 or 64 and with them several runs, beside partly filled pages
+    and pages that are rounded again: all statistics equal ekv_stats_build's of a cache that holds the stored keys."""
+    rng = np.random.default_rng(page)
+    g = torch.Generator(device="cuda").manual_seed(page)
+    B, H, M = 40, 8, 2400 // page + 1
+    n_phys = B * M
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    cfg = ekv.make_config(B, H, H, D, page, dtype, 1.5, 1.0, M, M)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    kp, vp = (torch.full((n_phys, H, page, D), 0x7F, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.full((n_phys, H), float("nan"), device="cuda") for _ in range(2))
+    table, free = torch.zeros(B, M, **i32), torch.from_numpy(rng.permutation(n_phys).astype(np.int32)).cuda()
+    lens, n_free = torch.zeros(B, **i32), torch.tensor([n_phys], **i32)
+    box, gauss = (torch.zeros(B, H, M, 2, D, dtype=dt, device="cuda") for _ in range(2))
+    box8 = torch.zeros(B, H, M, 16, 2, 8, dtype=torch.uint8, device="cuda") if dtype == "bf16" else None
+    for step in range(3):
+        counts = rng.integers(300, 800, B)
+        counts[step], counts[step + 5] = 0, 1
+        T = int(counts.sum())
+        assert T * H * 2 > 8 * 4096                               # more rows to a wavefront than one
+        slots, seq, pos, start, mapped = torch.zeros(T, dtype=torch.int64, device="cuda"), *(torch.zeros(k, **i32) for k in (T, T, B + 1, B))
+        new_lens, left = torch.zeros(B, **i32), torch.zeros(1, **i32)
+        tokens = ekv.token_map(slots, seq, pos, start, mapped)
+        ekv.ekv_map_tokens(cfg, lens, torch.from_numpy(counts.astype(np.int32)).cuda(), table, free, n_free, tokens, new_lens, left)
+        rows = torch.randn(T, 3, H, D, generator=g, device="cuda") * 2.0 ** torch.randint(-3, 6, (T, 1, 1, 1), generator=g, device="cuda")
+        rows = rows.to(dt)
+        ekv.ekv_cache8_append(cfg, ekv.cache8_view(kp, vp, ks, vs), ekv.stats_view(box, gauss, box8), tokens, rows[:, 1], rows[:, 2])
+        lens, n_free = new_lens, left
+        assert lens.tolist() == [int(x) for x in (counts if step == 0 else total + counts)]
+        total = lens.cpu().numpy()
+        value = torch.from_numpy(VALUES).float().cuda()
+        stored = torch.nan_to_num(value[kp.int()] * ks[:, :, None, None]).to(dt)
+        ref = [torch.zeros_like(box), torch.zeros_like(gauss)]
+        ref8 = torch.zeros_like(box8) if box8 is not None else None
+        ekv.ekv_stats_build(cfg, ekv.cache_view(stored, stored, table, lens), ekv.stats_view(*ref, ref8))
+        torch.cuda.synchronize()
+        has = torch.arange(M, device="cuda") < ((lens + page - 1) // page)[:, None]
+        for got, want in ((box, ref[0]), (gauss, ref[1])) + (((box8, ref8),) if box8 is not None else ()):
+            same = (got.view(torch.uint8) == want.view(torch.uint8)).flatten(3).all(-1)
+            assert same.transpose(1, 2)[has].all(), step
