@@ -1,5 +1,5 @@
 """Attention over the 8-bit cache where a wavefront has many items and a launch many units: outputs, value side included, of samples
-against the oracle, with limits that are a small part of the outputs.  Statistics of large appends."""
+against the oracle, with limits that are a small part of the outputs.  Statistics of large appends, and keys that are no number."""
 import numpy as np
 import pytest
 import torch
@@ -177,3 +177,53 @@ def test_statistics_of_large_appends(page, dtype):
         for got, want in ((box, ref[0]), (gauss, ref[1])) + (((box8, ref8),) if box8 is not None else ()):
             same = (got.view(torch.uint8) == want.view(torch.uint8)).flatten(3).all(-1)
             assert same.transpose(1, 2)[has].all(), step
+
+
+def poisoned(c, rng, share):
+    """NaN codes in a channel of some of each sequence's keys, a whole page's among them; which tokens stay."""
+    stay = []
+    for b in range(c.B):
+        bad = rng.random(c.lens[b]) < share
+        if c.lens[b] > 3 * c.P:
+            bad[c.P:2 * c.P] = True
+        at = torch.from_numpy(np.nonzero(bad)[0]).cuda()
+        page = torch.as_tensor(np.asarray(c.table[b].cpu() if torch.is_tensor(c.table) else c.table[b]), device="cuda").long()[at // c.P]
+        pool = c.k_pool if isinstance(c, Cache8) else c.pools[0]
+        pool[page, :, at % c.P, int(rng.integers(0, D))] = 0x7F
+        stay.append(np.nonzero(~bad)[0])
+    return stay
+
+
+@pytest.mark.parametrize("page,heads,dtype", [(16, (8, 2), "bf16"), (12, (8, 2), "bf16"), (16, (2, 2), "f32"), (44, (4, 2), "f32")])
+def test_entmax_passes_keys_over_that_are_no_number(page, heads, dtype):
+    """Short rows in one launch, longer ones in two, lists per query head and per KV head."""
+    rng = np.random.default_rng(page)
+    for lens in ([500, 77, 2], [3000, 4999, 900]):
+        c = Cache8(3, *heads, page, lens, dtype=dtype, seed=page)
+        stay = poisoned(c, rng, 0.1)
+        for call in ("full", "sparse", "sparse_group"):
+            n_lists = c.Hkv if call == "sparse_group" else c.Hq
+            m = [-(-n // page) for n in lens]
+            idx = torch.arange(c.M, dtype=torch.int32, device="cuda").expand(3, n_lists, c.M).contiguous()
+            n = torch.tensor(m, dtype=torch.int32, device="cuda")[:, None].expand(3, n_lists).contiguous()
+            run(c, call, (idx, n) if "sparse" in call else ())
+            for b in range(3):
+                for h in range(c.Hq):
+                    decodes.check_entmax(c, b, h, stay[b], c.out[b, h].cpu().numpy().astype(np.float64), float(c.tau[b, h]), int(c.supp[b, h]))
+
+
+@pytest.mark.parametrize("page", [16, 12])
+def test_entmax_passes_keys_over_that_are_no_number_in_large_calls(page):
+    """Over 64 MiB of K, where pages of 16 put the stores of the scores off."""
+    c = Large(16, 8, page, [40000 - 3001 * b for b in range(8)], seed=page, flat=0.3)
+    keys = [[c.keys_values(b, h) for h in (0, 7)] for b in (0, 7)]
+    stay = poisoned(c, np.random.default_rng(page), 0.1)
+    run(c, "full")
+    assert torch.isfinite(c.out).all()
+    for i, b in enumerate((0, 7)):
+        for j, h in enumerate((0, 15)):
+            q, (K, V) = c.query(b, h), (x[stay[b]] for x in keys[i][j])
+            ref = orc.entmax_attention(q, K, V, c.alpha, c.scale)
+            e, limit = entmax_limits(ref, q, K, V, c.alpha, c.scale)
+            assert abs(float(c.tau[b, h]) - ref["tau"]) <= e
+            assert np.all(np.abs(c.out[b, h].cpu().numpy() - ref["o"]) <= limit)
