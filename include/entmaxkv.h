@@ -387,6 +387,8 @@ ekv_status ekv_decode8_full(const ekv_config* cfg, const void* q, const ekv_cach
 
 /* Softmax attention over an 8-bit cache: restricted to page lists per query head as ekv_decode_sparse_softmax, and over every
  * page.  out f32 [B][Hq][d], lse f32 [B][Hq] (log-sum-exp of scale * q.k; -inf and a zero output for an empty row).
+ * The weighted values are summed before they are divided, with weights of up to 2^8: values below 2^90 keep the sums finite at every
+ * length, n tokens need |v| < 2^120 / n.  (The entmax decodes' weights sum to 1: no such limit.)
  * Workspaces EKV_OP_DECODE8_SPARSE_SOFTMAX, EKV_OP_DECODE8_FULL_SOFTMAX.  Range: capacities of fewer than 2^31 steps of 32 tokens, B *
  * Hkv * ceil(Mmax * P / 32) (lists: B * Hq * ceil(cap * P / 32)), else EKV_ERR_UNSUPPORTED. */
 ekv_status ekv_decode8_sparse_softmax(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache,

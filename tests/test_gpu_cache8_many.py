@@ -227,3 +227,17 @@ def test_entmax_passes_keys_over_that_are_no_number_in_large_calls(page):
             e, limit = entmax_limits(ref, q, K, V, c.alpha, c.scale)
             assert abs(float(c.tau[b, h]) - ref["tau"]) <= e
             assert np.all(np.abs(c.out[b, h].cpu().numpy() - ref["o"]) <= limit)
+
+
+@pytest.mark.parametrize("call", ["full", "full_softmax"])
+def test_values_at_the_end_of_the_softmax_range(call):
+    """Values of 448 * 2^81, just below 2^90, of both signs, in flat attention over 20011 tokens."""
+    rng = np.random.default_rng(9)
+    c = Cache8(1, 4, 1, 16, [20011], scale=0.01, seed=9)
+    c.codes[1][:] = np.where(c.valid[:, None, :, None], np.where(rng.random(c.codes[1].shape) < 0.9, 0x7E, 0xFE), 0x7F)
+    c.scales[1][c.valid.any(1)] = 2.0 ** 81
+    c.v_pool.copy_(torch.from_numpy(c.codes[1]).cuda())
+    c.v_scale.copy_(torch.from_numpy(c.scales[1].astype(np.float32)).cuda())
+    run(c, call)
+    for h in range(4):
+        check_sample(c, call, 0, h, np.arange(20011))
