@@ -154,13 +154,9 @@ template <typename T, int G, int MODE>
 static void launch_G(const Dims& dm, const Score8Args& a, bool stream, dim3 grid, size_t lds, hipStream_t st) {
   const dim3 block(kScoreThreads);
   const bool octets = dm.P % 8 == 0;
-  if constexpr (MODE != kPerHead)
-    if (stream) {
-      if (octets) hipLaunchKernelGGL((decode8_scores_kernel<T, G, MODE, true, true>), grid, block, lds, st, a);
-      else hipLaunchKernelGGL((decode8_scores_kernel<T, G, MODE, false, true>), grid, block, lds, st, a);
-      return;
-    }
-  if (octets) hipLaunchKernelGGL((decode8_scores_kernel<T, G, MODE, true, false>), grid, block, lds, st, a);
+  if (stream && octets) hipLaunchKernelGGL((decode8_scores_kernel<T, G, MODE, true, true>), grid, block, lds, st, a);
+  else if (stream) hipLaunchKernelGGL((decode8_scores_kernel<T, G, MODE, false, true>), grid, block, lds, st, a);
+  else if (octets) hipLaunchKernelGGL((decode8_scores_kernel<T, G, MODE, true, false>), grid, block, lds, st, a);
   else hipLaunchKernelGGL((decode8_scores_kernel<T, G, MODE, false, false>), grid, block, lds, st, a);
 }
 template <typename T>
@@ -197,7 +193,13 @@ void launch_scores8(const Dims& dm, int mode, ScoreArgs sa, const float* k_scale
     launch_unit_prefix(mode, sa, pre_ws, st);
   }
   const long long k_bytes = (long long)sa.U * (mode == kAllPages ? dm.Mmax : dm.cap) * dm.P * kD;
-  const bool stream = mode != kPerHead && k_bytes >= kStreamKBytes;
+  // Loads through the caches or past them, by the capacity.  Whole calls, us, kept / past, K of every page: pages of 12 17 MB 19.1 / 18.5
+  // (launched one by one 17.4 / 17.2), 34 MB 25.6 / 24.2 (23.1 / 23.7), 67 MB 38.9 / 36.8 (37.3 / 36.6), 134 MB 59.5 / 55.7, of 48 67 MB 37.9 /
+  // 36.3, float32 268 MB 85.0 / 80.7; group lists 34 MB 21.8 / 21.6 (20.3 / 21.2), 67 MB 30.3 / 28.7 and 29.3 / 28.2, 134 MB 59.2 / 54.9, 268
+  // MB 92.5 / 84.5; lists of heads without a group 34 MB 16.1 / 16.2, 67 MB 30.5 / 28.1 and 21.9 / 22.1, 134 MB 46.1 / 39.2, 268 MB
+  // 74.7 / 66.1.  Lists per head of a group meet in the caches: 16 x 16K tokens, lists of 40 %, 78.4 / 91.6 (2 % of a million, which
+  // hardly overlap, 35.4 / 31.7).
+  const bool stream = (mode != kPerHead || dm.G == 1) && k_bytes >= kStream8Bytes;
   const Score8Args a{sa, k_scale};
   if (mode == kAllPages && launch_scores8_held(dm, a, items, k_bytes, st)) return;
   const size_t lds = pre_global ? 0 : (size_t)(sa.U + 1) * sizeof(int);

@@ -392,13 +392,16 @@ static void launch_attn8_NW(const Dims& dm, const Attn8Args& a, int W, size_t ld
 template <typename T, int G, bool DENSE>
 static void launch_attn8(const Dims& dm, Attn8Args a, hipStream_t st) {
   const int cus = device_compute_units();
-  const bool stream = DENSE && 2ll * a.s.U * dm.Mmax * dm.P * kD >= kStreamKBytes;
+  // Loads through the caches or past them, by the capacity.  Whole calls, us, kept / past, K and V of every page: 34 MB 17.9 / 18.0, 67 MB 23.9 /
+  // 23.8 (launched one by one 22.1 / 22.9), 134 MB 36.7 / 34.4, in pages of 12 37.4 / 35.0, 268 MB 59.9 / 55.3, 2 GB 335 / 298; lists of heads
+  // without a group 43 MB 22.0 / 21.7 (19.9 / 20.9), 67 MB 18.8 / 18.6 (16.8 / 17.7), 134 MB 38.4 / 35.8, 268 MB 56.5 / 51.7 and 61.6 / 56.7.
+  // Lists per head of a group meet in the caches: 16 x 16K tokens, lists of 40 %, 107 / 129 (4 x 128K, 4 %, which hardly overlap, 44.0 / 41.8).
+  const bool stream = (DENSE || dm.G == 1) && (long long)a.s.U * (DENSE ? dm.Mmax : dm.cap) * dm.P * kD >= kStream8Bytes;
   if (attn8_per_unit(dm, DENSE, cus)) {
     a.per_unit = 1;
-    if (a.s.U < cus) { launch_attn8_NW<T, G, DENSE, false, 2 * kAttnWaves>(dm, a, a.s.U, 0, st); return; }
-    if constexpr (DENSE)
-      if (stream) { launch_attn8_NW<T, G, true, true, kAttnWaves>(dm, a, a.s.U, 0, st); return; }
-    launch_attn8_NW<T, G, DENSE, false, kAttnWaves>(dm, a, a.s.U, 0, st);
+    if (a.s.U < cus) launch_attn8_NW<T, G, DENSE, false, 2 * kAttnWaves>(dm, a, a.s.U, 0, st);
+    else if (stream) launch_attn8_NW<T, G, DENSE, true, kAttnWaves>(dm, a, a.s.U, 0, st);
+    else launch_attn8_NW<T, G, DENSE, false, kAttnWaves>(dm, a, a.s.U, 0, st);
     return;
   }
   const int W = attn8_grid(dm, DENSE, 2 * cus < kMostWgs ? 2 * cus : kMostWgs);
@@ -407,10 +410,8 @@ static void launch_attn8(const Dims& dm, Attn8Args a, hipStream_t st) {
     a.s.pre_g = a.pre;
   }
   const size_t lds = a.s.pre_g != nullptr ? 0 : (size_t)(a.s.U + 1) * sizeof(int);
-  bool done = false;
-  if constexpr (DENSE)
-    if (stream) { launch_attn8_NW<T, G, true, true, kAttnWaves>(dm, a, W, lds, st); done = true; }
-  if (!done) launch_attn8_NW<T, G, DENSE, false, kAttnWaves>(dm, a, W, lds, st);
+  if (stream) launch_attn8_NW<T, G, DENSE, true, kAttnWaves>(dm, a, W, lds, st);
+  else launch_attn8_NW<T, G, DENSE, false, kAttnWaves>(dm, a, W, lds, st);
   if (a.s.U * G <= cus) hipLaunchKernelGGL(attn8_join_kernel<8>, dim3(a.s.U * G), dim3(8 * kD), 0, st, a, G, W);
   else hipLaunchKernelGGL(attn8_join_kernel<2>, dim3(a.s.U * G), dim3(2 * kD), 0, st, a, G, W);
 }

@@ -22,6 +22,10 @@ struct Score8Args {
 // the faster one or the call has a form that it does not take.
 bool launch_scores8_held(const Dims& dm, const Score8Args& a, long long items, long long k_bytes, hipStream_t st);
 
+// Bytes of codes from which a call's pool passes the caches (non-temporal loads), where it is read once: every page, lists that the heads of
+// a group share, lists of heads without a group.  Both sides are measured where the loads are chosen.
+constexpr long long kStream8Bytes = 64ll << 20;
+
 // e4m3 pairs -> bf16 times a power of two (exact); HI: the upper two codes
 template <bool HI> __device__ __forceinline__ uint32_t widen2(uint32_t codes, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, HI));

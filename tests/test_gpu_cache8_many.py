@@ -67,7 +67,7 @@ def tokens_of(c, call, lists, b, h):
 
 @pytest.mark.parametrize("page,heads,dtype", [
     (4, (16, 8), "bf16"), (12, (16, 8), "bf16"), (16, (16, 8), "bf16"), (20, (16, 8), "bf16"), (24, (16, 8), "bf16"), (44, (16, 8), "bf16"),
-    (56, (16, 8), "bf16"), (64, (16, 8), "bf16"), (16, (8, 8), "bf16"), (12, (8, 8), "bf16"), (40, (32, 8), "bf16"), (16, (32, 4), "bf16"),
+    (56, (16, 8), "bf16"), (64, (16, 8), "bf16"), (16, (8, 8), "bf16"), (12, (8, 8), "bf16"), (16, (16, 16), "bf16"), (12, (16, 16), "f32"), (40, (32, 8), "bf16"), (16, (32, 4), "bf16"),
     (12, (32, 4), "bf16"), (12, (16, 8), "f32"), (16, (16, 8), "f32"), (40, (8, 8), "f32")])
 def test_outputs_where_wavefronts_have_many_items(page, heads, dtype):
     """24 uneven sequences of up to 12000 tokens: 18000 groups of tokens and more for 16384 wavefronts at most over all pages, three
