@@ -241,3 +241,18 @@ def test_values_at_the_end_of_the_softmax_range(call):
     run(c, call)
     for h in range(4):
         check_sample(c, call, 0, h, np.arange(20011))
+
+
+@pytest.mark.parametrize("batch", [512, 513])
+@pytest.mark.parametrize("heads", [(8, 8), (16, 8), (64, 8)])
+def test_as_many_units_as_the_put_off_stores_take(batch, heads):
+    """4096 units of 8 KV heads, the most that the pass takes which holds its stores back, with all of a compute unit's LDS; and more."""
+    n = 512 if heads == (8, 8) else 256                           # 8 MiB of scores too
+    lens = [n - 37 * b % (n + 1) for b in range(batch)]
+    c = Large(*heads, 16, lens, row_pages=n // 16, seed=batch, flat=0.3)
+    assert batch * 8 * n * D >= 64 << 20 and batch * c.Hq * n * 4 >= 8 << 20
+    rng = np.random.default_rng(batch)
+    run(c, "full")
+    assert torch.isfinite(c.out).all()
+    for b in rng.permutation(batch)[:30].tolist() + [0, 1, batch - 2, batch - 1]:
+        check_sample(c, "full", b, int(rng.integers(0, c.Hq)), np.arange(lens[b]))
