@@ -256,3 +256,30 @@ def test_as_many_units_as_the_put_off_stores_take(batch, heads):
     assert torch.isfinite(c.out).all()
     for b in rng.permutation(batch)[:30].tolist() + [0, 1, batch - 2, batch - 1]:
         check_sample(c, "full", b, int(rng.integers(0, c.Hq)), np.arange(lens[b]))
+
+
+@pytest.mark.parametrize("page", [16, 32])
+def test_how_far_a_stored_element_is_from_its_own(page):
+    """Tokens one by one, each up to four times as large as those before, into a page whose scale grows with them.  An element is off by half
+    a step when it is stored, 2^-4 of it or 2^-10 of the scale below the normal codes, and by at most 2^-10 of the scale again whenever
+    that grows (a code moved by whole exponents is exact unless it falls below the normal ones): at least doubled each
+    time, those sum to less than 2^-9 of the scale at the end."""
+    rng = np.random.default_rng(page)
+    H = 4
+    kp, vp = (torch.full((1, H, page, D), 0x7F, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.full((1, H), float("nan"), device="cuda") for _ in range(2))
+    cfg = ekv.make_config(1, H, H, D, page, "f32", 1.5, 1.0, 1, 1)
+    x = rng.standard_normal((page, 2, H, D)) * 2.0 ** np.cumsum(rng.integers(-1, 3, page))[:, None, None, None]
+    x = torch.from_numpy((x * 2.0 ** rng.integers(-12, 1, x.shape)).astype(np.float32))
+    grown = 0
+    for t in range(page):
+        row, before = x[t:t + 1].cuda(), ks.clone()
+        ekv.ekv_cache8_append(cfg, ekv.cache8_view(kp, vp, ks, vs), None, ekv.token_map(torch.tensor([t], device="cuda")), row[:, 0], row[:, 1])
+        grown += int((ks > before).sum())
+        for side, (pool, scale) in enumerate(((kp, ks), (vp, vs))):
+            s = scale.cpu().numpy().astype(np.float64)[0, :, None, None]
+            y = VALUES[pool.cpu().numpy()[0, :, :t + 1]] * s
+            ref = x[:t + 1, side].double().numpy().transpose(1, 0, 2)
+            assert np.all(np.abs(y - ref) <= np.maximum(2.0 ** -4 * np.abs(ref), 2.0 ** -10 * s) + 2.0 ** -9 * s)
+            assert np.all(s < np.abs(ref).max((1, 2), keepdims=True) / 224)
+    assert grown > 3 * H
