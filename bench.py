@@ -466,6 +466,9 @@ def main():
     bytes_z = B * Hq * sel_tokens * 4 * 2
     step_bytes = bytes_meta + bytes_scores + bytes_k + bytes_v + bytes_z
     dense_bytes = B * Hkv * n * 2 * d * e
+    eight = args.variant in ("cache8", "dense8")                    # a byte per element of K and V
+    if eight:
+        step_bytes -= (bytes_k + bytes_v) * (e - 1) / e
 
     # per-entry-point launch durations, measured live
     t_append = R.back_to_back(lambda st: ekv.ekv_stats_append(st.cfg, st.cache_prev, st.stats(), st.k_new, st.v_new))
@@ -549,11 +552,11 @@ def main():
         "metric": "decode-step latency", "value": round(us_wall, 2), "unit": "us", "n_gpus": 1,
         "steps": args.steps, "warmup": args.warmup, "ms_per_step": round(us_wall / 1e3, 5),
         "higher_is_better": False, "scaling": "weak", "vs_baseline": None, "dtype": "f32",
-        "data": "synthetic", "kv_dtype": w.kv_dtype,
+        "data": "synthetic", "kv_dtype": "e4m3" if eight else w.kv_dtype,
         "config": {"workload": f"{w.name}: B{B} {Hq}q/{Hkv}kv d{d} ctx{n} page{P} {w.kv_dtype}, alpha={w.alpha}, "
                                f"top-k {k_pages} pages ({args.budget:.0%}) per query head",
                    "variant": "entmaxkv-" + args.variant, "copies_rotated": args.copies,
-                   "append": "own launch" if args.two_launch_append else "inside the scoring launch"},
+                   "append": "own launch" if args.two_launch_append or eight else "inside the scoring launch"},
         "step_event_us": {"mean": round(float(whole.mean()), 2), "median": round(float(np.median(whole)), 2),
                           "p10": round(float(np.percentile(whole, 10)), 2),
                           "p90": round(float(np.percentile(whole, 90)), 2)},
