@@ -306,6 +306,7 @@ ekv_status ekv_decode_sparse_softmax(const ekv_config* cfg, const void* q,
  * undefined values, no undefined access).  A floating-point code gains nothing from a scale between two powers of two, and
  * with these code * scale is exact in bf16 and float32: scores, thresholds and page statistics are those of the stored
  * values.  cfg->kv_dtype is the type of q, of k_new / v_new and of the statistics.
+ * A config over the heads [h0, ..) of pools with more (pool_kv_heads) takes the pools advanced by h0*P*d bytes, the scales by h0 floats.
  * A key with a NaN code (what the append makes of infinities and NaN) scores NaN: the entmax decodes pass its token over, as if the
  * row did not have it, and every softmax over it is NaN.  A value with a NaN code gives NaN where its token has weight.
  * Range: n_phys_pages * pool heads * P < 2^30 (else EKV_ERR_UNSUPPORTED): 128 GiB a pool. */

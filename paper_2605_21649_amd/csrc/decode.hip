@@ -2392,11 +2392,13 @@ static void launch_rows(const Dims& dm, const ScoreArgs& sa, const SolveArgs& so
 // rows 13.6 / 9.5, 14.2 / 12.6, 14.2 / 15.1, 14.5 / 20.0, 256 rows of 1024 15.5 / 13.8; many rows read K once per head (2048 rows
 // of 1024 58 / 72), and so do lists shared by a group (2048 of 32 pages 21.9 / 30.5): these take two.
 constexpr int kRowTokensDense = 1024;
-// Page sizes whose octets may span pages: eight wavefronts for float32, which spill as sixteen (8 rows of 777 tokens, pages of 12,
-// 14.8 / 13.0).  Two launches / one: every page of 1 sequence with 8 heads, 100 / 480 / 1020 float32 tokens 14.4 / 10.4, 14.3 / 11.2,
-// 14.6 / 13.6, 256 rows of 1020 15.6 / 14.2; lists, 32 rows of 1311 / 2624 / 3936 tokens 15.7 / 14.4, 17.9 / 18.0, 19.8 / 22.9, 64 of 3936
-// 24.7 / 23.2 (pages of 48 21.1 / 25.5), 128 30.8 / 24.3 (of 36 33.7 / 31.5), 256 47.2 / 33.2, float32 49.1 / 33.6; 2048 lists of
-// 504 tokens 57.5 / 52.1, of 48-token pages 46.6 / 49.5, float32 47.9 / 52.4.
+// Page sizes whose octets may span pages: eight wavefronts for float32, which spill as sixteen.  Every page of 1 sequence with 8 heads,
+// float32, pages of 12, two launches / sixteen wavefronts / eight: alpha 1.5, 100 tokens 14.4 / 11.5 / 10.4, 480 14.4 / 13.3 / 11.4, 777
+// 14.6 / 15.4 / 13.6, 1020 14.5 / 15.8 / 13.8; alpha 1.25, whose threshold takes longer, 16.1 / 12.9 / 12.6, 17.1 / 15.7 / 14.2, 17.8 / 18.6 /
+// 16.7, 17.9 / 19.6 / 17.6 (launched one by one all are about 1 us shorter).  Two launches / one, alpha 1.5: 256 rows of 1020 15.6 / 14.2;
+// lists, 32 rows of 1311 / 2624 / 3936 tokens 15.7 / 14.4, 17.9 / 18.0, 19.8 / 22.9, 64 of 3936 24.7 / 23.2 (pages of 48 21.1 / 25.5), 128
+// 30.8 / 24.3 (of 36 33.7 / 31.5), 256 47.2 / 33.2, float32 49.1 / 33.6; 2048 lists of 504 tokens 57.5 / 52.1, of 48-token pages
+// 46.6 / 49.5, float32 47.9 / 52.4.
 template <typename TQ>
 static void launch_rows8_octets(const Dims& dm, bool dense, const Score8Args& sa, const SolveArgs& so, hipStream_t st) {
   const int rows = dm.B * dm.Hq;
