@@ -308,7 +308,7 @@ ekv_status ekv_decode_sparse_softmax(const ekv_config* cfg, const void* q,
  * values.  cfg->kv_dtype is the type of q, of k_new / v_new and of the statistics.
  * A config over the heads [h0, ..) of pools with more (pool_kv_heads) takes the pools advanced by h0*P*d bytes, the scales by h0 floats.
  * A key with a NaN code (what the append makes of infinities and NaN) scores NaN: the entmax decodes pass its token over, as if the
- * row did not have it, and every softmax over it is NaN.  A value with a NaN code gives NaN where its token has weight.
+ * row did not have it (but the side output lse is NaN), and every softmax over it is NaN.  A value with a NaN code gives NaN where its token has weight.
  * Range: n_phys_pages * pool heads * P < 2^30 (else EKV_ERR_UNSUPPORTED): 128 GiB a pool. */
 typedef struct {
   void* k_pool;

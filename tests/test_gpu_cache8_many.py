@@ -212,6 +212,17 @@ def test_entmax_passes_keys_over_that_are_no_number(page, heads, dtype):
                     decodes.check_entmax(c, b, h, stay[b], c.out[b, h].cpu().numpy().astype(np.float64), float(c.tau[b, h]), int(c.supp[b, h]))
 
 
+@pytest.mark.parametrize("n", [300, 5000])
+def test_a_key_that_is_no_number_is_in_the_log_sum_of_the_entmax_decode_alone(n):
+    c = Cache8(1, 4, 2, 16, [n], seed=n)
+    c.k_pool[c.table[0, 2], 0, 5, 3] = 0x7F                      # of the first KV head's queries
+    lse = torch.zeros(1, 4, device="cuda")
+    ekv.ekv_decode8_full(c.cfg, c.q, c.view(), c.out, c.tau, c.supp, c.workspace(ekv.EKV_OP_DECODE_FULL), extras=ekv.decode_extras(lse=lse))
+    torch.cuda.synchronize()
+    assert torch.isnan(lse[0, :2]).all() and torch.isfinite(lse[0, 2:]).all()
+    assert torch.isfinite(c.out).all() and torch.isfinite(c.tau).all()
+
+
 @pytest.mark.parametrize("page", [16, 12])
 def test_entmax_passes_keys_over_that_are_no_number_in_large_calls(page):
     """Over 64 MiB of K, where pages of 16 put the stores of the scores off."""
