@@ -104,7 +104,7 @@ def draw(rng):
     drafted, tokens, budget = _near(rng, 1, 64), _near(rng, 1, 1 << 20), rng.choice((0.01, 0.02, 0.0625, 0.25))
     share = 1.0 if over == "full" else budget
     # keys of all caches together and scores of all rows together stay below the largest listed cases'
-    keys = (1 << 20) if dtype == "f32" and cache == "same" else 3 << 20
+    keys = (3 << 20) // ((2 if dtype == "f32" and cache == "same" else 1) * (2 if form == "softmax" else 1))
     lists = heads[0] if over == "heads" else heads[1]
     cost = lambda b: max(b * tokens * max(heads[1], share * lists) / keys, b * tokens * share * heads[0] * drafted / 2.2e8)  # noqa: E731
     while cost(1) > 1:
