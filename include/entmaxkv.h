@@ -398,6 +398,38 @@ ekv_status ekv_decode8_sparse_softmax(const ekv_config* cfg, const void* q, cons
 ekv_status ekv_decode8_full_softmax(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, float* out,
                                     float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- a step of drafted tokens -----------------------------------------------------------------------------------
+ * What a program needs that looks at several new tokens of a sequence at once -- a chain or a tree of drafted tokens, a chunk
+ * of a prompt -- around the decode calls above, which take one query token per sequence.  Rows are packed as in ekv_token_map:
+ * sequence b's are rows start[b] .. start[b+1]-1. */
+
+/* Norm and rotation of the step's queries and keys, before they are scored and appended.  For every token i < n_tokens and head:
+ *   y = x / sqrt(mean_e x_e^2 + eps) * w          w = w_q for the Hq query heads, w_k for the Hkv KV heads [d]; NULL: y = x
+ *   pair (e, f) of channels, angle t = pos[i] * freq[k]:  (y_e, y_f) <- (y_e cos t - y_f sin t, y_f cos t + y_e sin t)
+ * k = 0 .. n_freq-1; pairs == 0: (e, f) = (k, k + n_freq), the two halves of the first 2 n_freq channels; pairs != 0: (2k, 2k+1),
+ * neighbours.  Channels from 2 n_freq on are not turned; n_freq == 0 (freq and pos may be NULL): none is.  Arithmetic in float32,
+ * the angle in 64 bits (a float32 position times frequency is off by 0.03 at a million), rounded once to kv_dtype.
+ * x_q, x_k: kv_dtype, heads of a token follow each other, tokens q_stride and k_stride elements apart (multiples of 8), so that
+ * parts of a fused projection need no copy.  w_q, w_k kv_dtype; freq float32 [n_freq]; pos int32 [n_tokens] (the pos of a token
+ * map, as it is): a token with pos < 0 is passed over, its rows of q_out [n_tokens][Hq][d] and k_out [n_tokens][Hkv][d] are left
+ * as they were (with pos NULL there is none).  Of cfg the head counts, head_dim and kv_dtype are used.
+ * One launch, no workspace.  Range: n_freq a multiple of 8 up to 64, n_tokens * (Hq + Hkv) < 2^31 (else EKV_ERR_UNSUPPORTED);
+ * eps finite and >= 0. */
+ekv_status ekv_norm_rotate(const ekv_config* cfg, const void* x_q, int64_t q_stride, const void* x_k, int64_t k_stride,
+                           const void* w_q, const void* w_k, float eps, const float* freq, int32_t n_freq, const int32_t* pos,
+                           int32_t n_tokens, int32_t pairs, void* q_out, void* k_out, void* stream);
+
+/* Append of several tokens per sequence to a cache in its own type, the counterpart of ekv_cache8_append: token i goes to slots[i]
+ * of the pools, its K and V are row rows[i] of k_new and v_new (int32 [max_tokens], clamped into [0, n_rows); NULL: row i) --
+ * so the accepted path of a tree is appended from where the tree's rows are.  Strides, slots, runs of consecutive slots, stats
+ * (may be NULL) and tokens->seq / pos as there; a call may name a page in one run only.  box, gauss and, if given, box8 of page pos/P are written for
+ * its tokens 0 .. t0 + run - 1 (t0: the run's first token in the page), bit for bit what ekv_stats_build computes for them.  seq_lens and
+ * block_table of `cache` are not read and may be NULL.  One launch, no workspace.
+ * Range: max_tokens < 2^30 and max_tokens * Hkv < 2^31, else EKV_ERR_UNSUPPORTED. */
+ekv_status ekv_cache_append(const ekv_config* cfg, const ekv_cache_view* cache, const ekv_stats_view* stats,
+                            const ekv_token_map* tokens, const int32_t* rows, int32_t n_rows, const void* k_new, int64_t k_stride,
+                            const void* v_new, int64_t v_stride, void* stream);
+
 /* Measurement aid, no part of the method: reads n_pages pages of page_bytes bytes (4096 or 8192) of the device
  * buffer `base` and discards the data, four pages per wavefront.  Page i of the launch is page page_ids[i] of the
  * buffer (device int32 list), or page lookup[page_ids[i]] when `lookup` (device int32 table) is given -- a second

@@ -29,8 +29,9 @@ EXPORTS = ["ekv_stats_build", "ekv_stats_append", "ekv_score_pages", "ekv_append
            "ekv_decode_sparse_softmax", "ekv_workspace_bytes", "ekv_probe_read", "ekv_decode_sparse_static",
            "ekv_probe_handoff", "ekv_map_tokens", "ekv_release_pages", "ekv_cache8_append", "ekv_decode8_sparse",
            "ekv_decode8_sparse_group", "ekv_decode8_full", "ekv_decode8_sparse_softmax", "ekv_decode8_full_softmax",
+           "ekv_norm_rotate", "ekv_cache_append",
            "ekv_status_string", "ekv_last_hip_error", "ekv_version"]
-_STATUS_CALLS = EXPORTS[:23]      # entry points that return ekv_status
+_STATUS_CALLS = EXPORTS[:-3]      # entry points that return ekv_status
 
 
 class ekv_config(ctypes.Structure):
@@ -124,6 +125,10 @@ def load_library():
                                                c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
     lib.ekv_decode8_full_softmax.argtypes = [P(ekv_config), c_void_p, P(ekv_cache8_view), c_void_p, c_void_p, c_void_p,
                                              c_size_t, c_void_p]
+    lib.ekv_norm_rotate.argtypes = [P(ekv_config), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_float, c_void_p,
+                                    c_int32, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p]
+    lib.ekv_cache_append.argtypes = [P(ekv_config), P(ekv_cache_view), P(ekv_stats_view), P(ekv_token_map), c_void_p, c_int32,
+                                     c_void_p, c_int64, c_void_p, c_int64, c_void_p]
     for name in _STATUS_CALLS:
         getattr(lib, name).restype = c_int32
     _lib = lib
@@ -365,3 +370,33 @@ def ekv_decode8_full_softmax(cfg, q, cache, out, lse, workspace, stream=None):
     nbytes = workspace.numel() * workspace.element_size()
     _check(load_library().ekv_decode8_full_softmax(byref(cfg), _query(cfg, q), byref(cache), _ptr(out), _ptr(lse),
                                                    _ptr(workspace), nbytes, _stream(stream)))
+
+
+def ekv_norm_rotate(cfg, x_q, x_k, w_q, w_k, eps, freq, pos, q_out, k_out, pairs=False, stream=None):
+    qn, kn, t = x_q.shape, x_k.shape, _TYPES.get(cfg.kv_dtype)
+    (q, qs), (k, ks) = _rows(x_q, qn), _rows(x_k, kn)
+    n = qn[0]
+    assert kn[0] == n and qn[1:] == (cfg.n_q_heads, cfg.head_dim) and kn[1:] == (cfg.n_kv_heads, cfg.head_dim), \
+        "rows of the config's heads and head size"
+    assert x_q.dtype is t and x_k.dtype is t and q_out.dtype is t and k_out.dtype is t, "rows and outputs of the config's type"
+    assert q_out.shape == qn and k_out.shape == kn, "an output row for every token"
+    for w in (w_q, w_k):
+        assert w is None or (w.dtype is t and w.numel() == cfg.head_dim), "weights of the config's type and head size"
+    assert freq is None or freq.dtype is torch.float32, "frequencies are float32"
+    assert pos is None or (pos.dtype is torch.int32 and pos.numel() >= n), "positions: int32, one for every token"
+    _check(load_library().ekv_norm_rotate(byref(cfg), q, qs, k, ks, _ptr(w_q), _ptr(w_k), eps, _ptr(freq),
+                                          freq.numel() if freq is not None else 0, _ptr(pos), n, 1 if pairs else 0, _ptr(q_out),
+                                          _ptr(k_out), _stream(stream)))
+
+
+def ekv_cache_append(cfg, cache, stats, tokens, k_new, v_new, rows=None, stream=None):
+    kn, vn, n, t = k_new.shape, v_new.shape, tokens.max_tokens, _TYPES.get(cfg.kv_dtype)
+    (k, ks), (v, vs) = _rows(k_new, kn), _rows(v_new, vn)
+    if rows is None:
+        assert kn[0] >= n and vn[0] >= n, "a row for every token of the map"
+    else:
+        assert rows.dtype is torch.int32 and rows.numel() >= n and vn[0] == kn[0], "rows: int32, one for every token of the map"
+    assert kn[1] == vn[1] == cfg.n_kv_heads and kn[2] == vn[2] == cfg.head_dim, "rows of the config's KV heads and head size"
+    assert k_new.dtype is t and v_new.dtype is t, "rows of the config's type"
+    _check(load_library().ekv_cache_append(byref(cfg), byref(cache), byref(stats) if stats is not None else None, byref(tokens),
+                                           _ptr(rows), kn[0], k, ks, v, vs, _stream(stream)))

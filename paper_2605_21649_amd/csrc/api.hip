@@ -105,7 +105,7 @@ static ekv_status check_box8(const Dims& dm, const ekv_stats_view* stats, bool r
 
 extern "C" {
 
-int32_t ekv_version(void) { return 103; }
+int32_t ekv_version(void) { return 104; }
 
 int32_t ekv_last_hip_error(void) { return g_last_hip_error; }
 
@@ -483,6 +483,45 @@ ekv_status ekv_decode8_sparse_softmax(const ekv_config* cfg, const void* q, cons
 ekv_status ekv_decode8_full_softmax(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, float* out,
                                     float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   return decode8_softmax_common(cfg, true, q, cache, nullptr, nullptr, out, lse, workspace, workspace_bytes, stream);
+}
+
+ekv_status ekv_norm_rotate(const ekv_config* cfg, const void* x_q, int64_t q_stride, const void* x_k, int64_t k_stride,
+                           const void* w_q, const void* w_k, float eps, const float* freq, int32_t n_freq, const int32_t* pos,
+                           int32_t n_tokens, int32_t pairs, void* q_out, void* k_out, void* stream) {
+  Dims dm;
+  const ekv_status s = make_dims(cfg, dm);
+  if (s != EKV_OK) return s;
+  if (!ok_ptr(x_q) || !ok_ptr(x_k) || !ok_ptr(q_out) || !ok_ptr(k_out) || n_tokens <= 0 || n_freq < 0) return EKV_ERR_INVALID_ARG;
+  if (!aligned16(w_q) || !aligned16(w_k) || !(eps >= 0.f) || !std::isfinite(eps)) return EKV_ERR_INVALID_ARG;
+  if (n_freq > 0 ? !ok_ptr4(freq) || !ok_ptr4(pos) : pos != nullptr && !ok_ptr4(pos)) return EKV_ERR_INVALID_ARG;
+  const int64_t d = cfg->head_dim;
+  if (q_stride < dm.Hq * d || k_stride < dm.Hkv * d || q_stride % 8 != 0 || k_stride % 8 != 0) return EKV_ERR_INVALID_ARG;
+  if (q_out == x_q || q_out == x_k || k_out == x_q || k_out == x_k || q_out == k_out) return EKV_ERR_INVALID_ARG;
+  if (n_freq % 8 != 0 || n_freq > d / 2 || (int64_t)n_tokens * (dm.Hq + dm.Hkv) > 0x7fffffff) return EKV_ERR_UNSUPPORTED;
+  launch_norm_rotate(dm, x_q, q_stride, x_k, k_stride, w_q, w_k, eps, freq, n_freq, pos, n_tokens, pairs != 0, q_out, k_out,
+                     (hipStream_t)stream);
+  return finish((hipStream_t)stream);
+}
+
+ekv_status ekv_cache_append(const ekv_config* cfg, const ekv_cache_view* cache, const ekv_stats_view* stats,
+                            const ekv_token_map* tokens, const int32_t* rows, int32_t n_rows, const void* k_new, int64_t k_stride,
+                            const void* v_new, int64_t v_stride, void* stream) {
+  Dims dm;
+  ekv_status s = make_dims(cfg, dm);
+  if (s != EKV_OK) return s;
+  if (cache == nullptr || !ok_ptr(cache->k_pool) || !ok_ptr(cache->v_pool) || cache->n_phys_pages <= 0) return EKV_ERR_INVALID_ARG;
+  if (tokens == nullptr || !ok_ptr8(tokens->slots) || tokens->max_tokens <= 0 || !ok_ptr(k_new) || !ok_ptr(v_new))
+    return EKV_ERR_INVALID_ARG;
+  if (rows != nullptr && (!ok_ptr4(rows) || n_rows <= 0)) return EKV_ERR_INVALID_ARG;
+  const int64_t row = (int64_t)dm.Hkv * cfg->head_dim;
+  if (k_stride < row || v_stride < row || k_stride % 8 != 0 || v_stride % 8 != 0) return EKV_ERR_INVALID_ARG;
+  if (stats != nullptr) {
+    if (!ok_ptr(stats->box) || !ok_ptr(stats->gauss) || !ok_ptr4(tokens->seq) || !ok_ptr4(tokens->pos)) return EKV_ERR_INVALID_ARG;
+    if ((s = check_box8(dm, stats, false)) != EKV_OK) return s;
+  }
+  if (tokens->max_tokens >= 1 << 30 || (int64_t)tokens->max_tokens * dm.Hkv > 0x7fffffff) return EKV_ERR_UNSUPPORTED;
+  launch_cache_append(dm, *cache, stats, *tokens, rows, n_rows, k_new, k_stride, v_new, v_stride, (hipStream_t)stream);
+  return finish((hipStream_t)stream);
 }
 
 ekv_status ekv_probe_read(const void* base, const int32_t* page_ids, const int32_t* lookup, int32_t n_pages,

@@ -98,6 +98,13 @@ void launch_decode8_softmax(const Dims& dm, bool dense, const void* q, const ekv
 size_t softmax8_ws_bytes(const Dims& dm, bool dense);
 bool softmax8_supported(const Dims& dm, bool dense);   // the steps of all units are counted in 31 bits
 
+void launch_norm_rotate(const Dims& dm, const void* x_q, int64_t q_stride, const void* x_k, int64_t k_stride, const void* w_q,
+                        const void* w_k, float eps, const float* freq, int n_freq, const int32_t* pos, int n, bool pairs, void* q_out,
+                        void* k_out, hipStream_t st);
+void launch_cache_append(const Dims& dm, const ekv_cache_view& c, const ekv_stats_view* stats, const ekv_token_map& tok,
+                         const int32_t* rows, int n_rows, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                         hipStream_t st);
+
 size_t select_topk_ws_bytes(const Dims& dm);
 size_t select_box_ws_bytes(const Dims& dm);
 bool select_box_supported(const Dims& dm);

@@ -79,6 +79,28 @@ __device__ __forceinline__ void page_stats_wave(const T* __restrict__ kpage, int
   }
 }
 
+// Sum, minimum or maximum over the four rows of lanes of 8 values each: lane (r, c) gets entries e and e + 1, e = 2 (r / 2) + 4 (r % 2).
+// The pairs are those of exchanges over 16 and then 32 lanes; each step passes on the half of the entries that the other needs.
+template <typename F> __device__ __forceinline__ float2 rows_reduce(const float (&x)[8], F&& f) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[i]), __float_as_uint(x[i + 4]), false, false);
+    y[i] = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
+  float z[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(y[i]), __float_as_uint(y[i + 2]), false, false);
+    z[i] = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
+  return make_float2(z[0], z[1]);
+}
+__device__ __forceinline__ void store2(float* p, float2 v) { *reinterpret_cast<float2*>(p) = v; }
+__device__ __forceinline__ void store2(bf16_t* p, float2 v) {
+  *reinterpret_cast<uint32_t*>(p) = float_to_bf16_bits(v.x) | ((uint32_t)float_to_bf16_bits(v.y) << 16);
+}
+
 // Appends one token to (sequence b, KV head h) with ONE wavefront (lane = threadIdx.x & 63): writes k_new
 // (and v_new) into slot `pos` of the cache and recomputes the statistics of that page over its pos%P + 1
 // tokens.  Nothing happens when the page is not mapped (pos < 0 or pos/P >= Mmax).
