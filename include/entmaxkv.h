@@ -61,7 +61,11 @@ typedef enum {
   EKV_OP_DECODE_SPARSE_SOFTMAX = 4,
   EKV_OP_SELECT_BOX_THRESHOLD = 5,
   EKV_OP_DECODE8_SPARSE_SOFTMAX = 6,
-  EKV_OP_DECODE8_FULL_SOFTMAX = 7
+  EKV_OP_DECODE8_FULL_SOFTMAX = 7,
+  EKV_OP_TREE_SPARSE = 8,          /* the ekv_tree_* and ekv_tree8_* calls: ekv_tree_workspace_bytes     */
+  EKV_OP_TREE_FULL = 9,
+  EKV_OP_TREE_SPARSE_SOFTMAX = 10,
+  EKV_OP_TREE_FULL_SOFTMAX = 11
 } ekv_op;
 
 /* Problem description (host struct).  head_dim must be 128; page_size a multiple of 4 in [4,64];
@@ -429,6 +433,69 @@ ekv_status ekv_norm_rotate(const ekv_config* cfg, const void* x_q, int64_t q_str
 ekv_status ekv_cache_append(const ekv_config* cfg, const ekv_cache_view* cache, const ekv_stats_view* stats,
                             const ekv_token_map* tokens, const int32_t* rows, int32_t n_rows, const void* k_new, int64_t k_stride,
                             const void* v_new, int64_t v_stride, void* stream);
+
+/* Drafted tokens: up to 64 new rows per sequence whose keys and values are not in the cache -- a token that is not accepted leaves no
+ * trace in page statistics, page scales or codes -- and which of them each row sees.
+ *   k_new, v_new [max_tokens][Hkv][d] kv_dtype, rows k_stride and v_stride elements apart (multiples of 8)
+ *   start   int32 [B+1]: sequence b's rows are start[b] .. start[b+1]-1, the first max_tree of them at most
+ *   visible uint64 [max_tokens]: bit i of a row's word: it sees row i of its sequence.  For a tree the row itself and the rows that
+ *           it follows, (1 << i) | visible[parent]; for a chain the rows up to it.  Any other mask is as good, none of them too.
+ * max_tree (1 .. 64) and max_tokens size grids and workspaces.  max_tokens is also the number of rows of q and of the outputs.  Entries of start
+ * are clamped into [0, max_tokens] and kept ascending; rows of no sequence, behind start[B] or beyond max_tree, are neither read nor written. */
+typedef struct {
+  const void* k_new;
+  const void* v_new;
+  int64_t k_stride;
+  int64_t v_stride;
+  const int32_t* start;
+  const uint64_t* visible;
+  int32_t max_tokens;
+  int32_t max_tree;
+} ekv_tree_view;
+
+/* Attention of every drafted row over its sequence's cache (seq_lens tokens, without the drafted ones) and over the drafted rows it sees:
+ * ekv_decode_sparse, _sparse_group, _full, _sparse_softmax and a softmax over every page, for max_tokens query tokens instead of
+ * one per sequence.  q [max_tokens][Hq][d] kv_dtype, out f32 [max_tokens][Hq][d], tau / lse f32 and supp int32 [max_tokens][Hq].  Page
+ * lists are the sequence's, shared by its rows: page_idx [B][Hq][cap] and n_sel [B][Hq], or [B][Hkv] for _group (a selection for the last
+ * committed token serves the tokens drafted after it; cfg->max_sel_pages is cap).  K and V are read once for all rows of a list.
+ * A row that sees nothing (an empty cache or list, no drafted row) has a zero output, tau = +inf, an empty support, lse = -inf.
+ * Scores, thresholds, sums and outputs are float32 sums of exact products, as in the single-token calls, in another order.
+ * What is hidden counts for nothing, infinities and NaN included.  Keys that are no number: the entmax calls pass them over, every
+ * softmax that sees one is NaN.  (Softmax sums: values below 2^120 / (n 2^8) keep them finite, n keys.)
+ * The workspace holds 4 bytes per row, query head and position for entmax (a capacity of a million tokens, 16 rows, 32 heads: 2.1 GB).
+ * Range: as the single-token calls; the steps of all lists, B * lists * blocks of rows * tiles of 16 keys or more, and max_tokens * Hq < 2^31,
+ * n_phys_pages * pool heads * P < 2^31 (8 bits: 2^30), else EKV_ERR_UNSUPPORTED. */
+ekv_status ekv_tree_sparse(const ekv_config* cfg, const void* q, const ekv_cache_view* cache, const ekv_tree_view* tree,
+                           const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau, int32_t* supp, void* workspace,
+                           size_t workspace_bytes, void* stream);
+ekv_status ekv_tree_sparse_group(const ekv_config* cfg, const void* q, const ekv_cache_view* cache, const ekv_tree_view* tree,
+                                 const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau, int32_t* supp,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+ekv_status ekv_tree_full(const ekv_config* cfg, const void* q, const ekv_cache_view* cache, const ekv_tree_view* tree, float* out,
+                         float* tau, int32_t* supp, void* workspace, size_t workspace_bytes, void* stream);
+ekv_status ekv_tree_sparse_softmax(const ekv_config* cfg, const void* q, const ekv_cache_view* cache, const ekv_tree_view* tree,
+                                   const int32_t* page_idx, const int32_t* n_sel, float* out, float* lse, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+ekv_status ekv_tree_full_softmax(const ekv_config* cfg, const void* q, const ekv_cache_view* cache, const ekv_tree_view* tree,
+                                 float* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+/* The same over an 8-bit cache; the drafted rows are in kv_dtype.  Workspaces are the same. */
+ekv_status ekv_tree8_sparse(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, const ekv_tree_view* tree,
+                            const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau, int32_t* supp, void* workspace,
+                            size_t workspace_bytes, void* stream);
+ekv_status ekv_tree8_sparse_group(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, const ekv_tree_view* tree,
+                                  const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau, int32_t* supp,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+ekv_status ekv_tree8_full(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, const ekv_tree_view* tree, float* out,
+                          float* tau, int32_t* supp, void* workspace, size_t workspace_bytes, void* stream);
+ekv_status ekv_tree8_sparse_softmax(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, const ekv_tree_view* tree,
+                                    const int32_t* page_idx, const int32_t* n_sel, float* out, float* lse, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+ekv_status ekv_tree8_full_softmax(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, const ekv_tree_view* tree,
+                                  float* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of the ekv_tree calls (EKV_OP_TREE_*; _SPARSE is that of ekv_tree_sparse and ekv_tree_sparse_group; an 8-bit cache needs
+ * the same) under cfg for the max_tokens and max_tree of the tree (host computation, no HIP calls). */
+ekv_status ekv_tree_workspace_bytes(const ekv_config* cfg, int32_t op, int32_t max_tokens, int32_t max_tree, size_t* bytes);
 
 /* Measurement aid, no part of the method: reads n_pages pages of page_bytes bytes (4096 or 8192) of the device
  * buffer `base` and discards the data, four pages per wavefront.  Page i of the launch is page page_ids[i] of the

@@ -20,7 +20,8 @@ EKV_SCORE_BOX, EKV_SCORE_GAUSS, EKV_SCORE_BOTH, EKV_SCORE_GROUP_MAX, EKV_SCORE_B
 EKV_STATIC_SCRATCH_BYTES = 32 << 20
 EKV_OP_SELECT_TOPK, EKV_OP_SELECT_GAUSS, EKV_OP_DECODE_SPARSE, EKV_OP_DECODE_FULL, \
     EKV_OP_DECODE_SPARSE_SOFTMAX, EKV_OP_SELECT_BOX_THRESHOLD, EKV_OP_DECODE8_SPARSE_SOFTMAX, \
-    EKV_OP_DECODE8_FULL_SOFTMAX = range(8)
+    EKV_OP_DECODE8_FULL_SOFTMAX, EKV_OP_TREE_SPARSE, EKV_OP_TREE_FULL, EKV_OP_TREE_SPARSE_SOFTMAX, \
+    EKV_OP_TREE_FULL_SOFTMAX = range(12)
 
 # every symbol the header declares
 EXPORTS = ["ekv_stats_build", "ekv_stats_append", "ekv_score_pages", "ekv_append_score_pages", "ekv_select_topk",
@@ -29,7 +30,9 @@ EXPORTS = ["ekv_stats_build", "ekv_stats_append", "ekv_score_pages", "ekv_append
            "ekv_decode_sparse_softmax", "ekv_workspace_bytes", "ekv_probe_read", "ekv_decode_sparse_static",
            "ekv_probe_handoff", "ekv_map_tokens", "ekv_release_pages", "ekv_cache8_append", "ekv_decode8_sparse",
            "ekv_decode8_sparse_group", "ekv_decode8_full", "ekv_decode8_sparse_softmax", "ekv_decode8_full_softmax",
-           "ekv_norm_rotate", "ekv_cache_append",
+           "ekv_norm_rotate", "ekv_cache_append", "ekv_tree_sparse", "ekv_tree_sparse_group", "ekv_tree_full",
+           "ekv_tree_sparse_softmax", "ekv_tree_full_softmax", "ekv_tree8_sparse", "ekv_tree8_sparse_group", "ekv_tree8_full",
+           "ekv_tree8_sparse_softmax", "ekv_tree8_full_softmax", "ekv_tree_workspace_bytes",
            "ekv_status_string", "ekv_last_hip_error", "ekv_version"]
 _STATUS_CALLS = EXPORTS[:-3]      # entry points that return ekv_status
 
@@ -63,6 +66,11 @@ class ekv_cache8_view(ctypes.Structure):
 class ekv_token_map(ctypes.Structure):
     _fields_ = [("slots", c_void_p), ("seq", c_void_p), ("pos", c_void_p), ("start", c_void_p), ("n_mapped", c_void_p),
                 ("max_tokens", c_int32)]
+
+
+class ekv_tree_view(ctypes.Structure):
+    _fields_ = [("k_new", c_void_p), ("v_new", c_void_p), ("k_stride", c_int64), ("v_stride", c_int64), ("start", c_void_p),
+                ("visible", c_void_p), ("max_tokens", c_int32), ("max_tree", c_int32)]
 
 
 class EkvError(RuntimeError):
@@ -129,6 +137,14 @@ def load_library():
                                     c_int32, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p]
     lib.ekv_cache_append.argtypes = [P(ekv_config), P(ekv_cache_view), P(ekv_stats_view), P(ekv_token_map), c_void_p, c_int32,
                                      c_void_p, c_int64, c_void_p, c_int64, c_void_p]
+    for name, view in (("ekv_tree_", ekv_cache_view), ("ekv_tree8_", ekv_cache8_view)):
+        head, tail = [P(ekv_config), c_void_p, P(view), P(ekv_tree_view)], [c_void_p, c_size_t, c_void_p]
+        getattr(lib, name + "sparse").argtypes = head + [c_void_p] * 5 + tail
+        getattr(lib, name + "sparse_group").argtypes = head + [c_void_p] * 5 + tail
+        getattr(lib, name + "full").argtypes = head + [c_void_p] * 3 + tail
+        getattr(lib, name + "sparse_softmax").argtypes = head + [c_void_p] * 4 + tail
+        getattr(lib, name + "full_softmax").argtypes = head + [c_void_p] * 2 + tail
+    lib.ekv_tree_workspace_bytes.argtypes = [P(ekv_config), c_int32, c_int32, c_int32, P(c_size_t)]
     for name in _STATUS_CALLS:
         getattr(lib, name).restype = c_int32
     _lib = lib
@@ -400,3 +416,80 @@ def ekv_cache_append(cfg, cache, stats, tokens, k_new, v_new, rows=None, stream=
     assert k_new.dtype is t and v_new.dtype is t, "rows of the config's type"
     _check(load_library().ekv_cache_append(byref(cfg), byref(cache), byref(stats) if stats is not None else None, byref(tokens),
                                            _ptr(rows), kn[0], k, ks, v, vs, _stream(stream)))
+
+
+def tree_view(start, visible, k_new, v_new, max_tree):
+    """Drafted rows: k_new, v_new [max_tokens][Hkv][d] (may be parts of longer rows), start int32 [B + 1], visible int64 [max_tokens],
+    the 64 bits of a row's mask."""
+    kn, vn = k_new.shape, v_new.shape
+    (k, ks), (v, vs) = _rows(k_new, kn), _rows(v_new, vn)
+    assert kn == vn and k_new.dtype is v_new.dtype, "drafted keys and values of one shape and type"
+    assert start.dtype is torch.int32 and visible.element_size() == 8 and not visible.is_floating_point(), "start int32, masks of 64 bits"
+    assert visible.numel() == kn[0], "a mask for every drafted row"
+    tree = ekv_tree_view(k, v, ks, vs, _ptr(start), _ptr(visible), kn[0], max_tree)
+    tree.of = (kn[1:], k_new.dtype, start.numel())            # what the calls check against their config
+    return tree
+
+
+def ekv_tree_workspace_bytes(cfg, op, max_tokens, max_tree):
+    n = c_size_t(0)
+    _check(load_library().ekv_tree_workspace_bytes(byref(cfg), op, max_tokens, max_tree, byref(n)))
+    return n.value
+
+
+def _tree(call, cfg, q, cache, tree, page_idx, n_sel, heads, outs, workspace, stream):
+    t = _TYPES.get(cfg.kv_dtype)
+    assert q.dtype is t and q.numel() == tree.max_tokens * cfg.n_q_heads * cfg.head_dim, "a query of the config's type for every row and head"
+    heads_of, dtype, starts = tree.of
+    assert heads_of == (cfg.n_kv_heads, cfg.head_dim) and dtype is t, "drafted rows of the config's type, KV heads and head size"
+    assert starts == cfg.batch + 1, "start has an entry for every sequence and one more"
+    rows = tree.max_tokens * cfg.n_q_heads
+    assert outs[0].dtype is torch.float32 and outs[0].numel() == rows * cfg.head_dim, "out: float32, like q"
+    for o in outs[1:]:
+        assert o.element_size() == 4 and o.numel() == rows, "tau or lse float32, supp int32: one for every row and head"
+    args = [byref(cfg), _ptr(q), byref(cache), byref(tree)]
+    if heads:
+        assert page_idx.dtype is torch.int32 and n_sel.dtype is torch.int32, "page lists are int32"
+        assert n_sel.numel() == cfg.batch * heads and page_idx.numel() == n_sel.numel() * cfg.max_sel_pages, "a list of cap pages for every sequence and head"
+        args += [_ptr(page_idx), _ptr(n_sel)]
+    _check(call(*args, *[_ptr(o) for o in outs], _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def ekv_tree_sparse(cfg, q, cache, tree, page_idx, n_sel, out, tau, supp, workspace, stream=None):
+    _tree(load_library().ekv_tree_sparse, cfg, q, cache, tree, page_idx, n_sel, cfg.n_q_heads, (out, tau, supp), workspace, stream)
+
+
+def ekv_tree_sparse_group(cfg, q, cache, tree, page_idx, n_sel, out, tau, supp, workspace, stream=None):
+    _tree(load_library().ekv_tree_sparse_group, cfg, q, cache, tree, page_idx, n_sel, cfg.n_kv_heads, (out, tau, supp), workspace, stream)
+
+
+def ekv_tree_full(cfg, q, cache, tree, out, tau, supp, workspace, stream=None):
+    _tree(load_library().ekv_tree_full, cfg, q, cache, tree, None, None, 0, (out, tau, supp), workspace, stream)
+
+
+def ekv_tree_sparse_softmax(cfg, q, cache, tree, page_idx, n_sel, out, lse, workspace, stream=None):
+    _tree(load_library().ekv_tree_sparse_softmax, cfg, q, cache, tree, page_idx, n_sel, cfg.n_q_heads, (out, lse), workspace, stream)
+
+
+def ekv_tree_full_softmax(cfg, q, cache, tree, out, lse, workspace, stream=None):
+    _tree(load_library().ekv_tree_full_softmax, cfg, q, cache, tree, None, None, 0, (out, lse), workspace, stream)
+
+
+def ekv_tree8_sparse(cfg, q, cache, tree, page_idx, n_sel, out, tau, supp, workspace, stream=None):
+    _tree(load_library().ekv_tree8_sparse, cfg, q, cache, tree, page_idx, n_sel, cfg.n_q_heads, (out, tau, supp), workspace, stream)
+
+
+def ekv_tree8_sparse_group(cfg, q, cache, tree, page_idx, n_sel, out, tau, supp, workspace, stream=None):
+    _tree(load_library().ekv_tree8_sparse_group, cfg, q, cache, tree, page_idx, n_sel, cfg.n_kv_heads, (out, tau, supp), workspace, stream)
+
+
+def ekv_tree8_full(cfg, q, cache, tree, out, tau, supp, workspace, stream=None):
+    _tree(load_library().ekv_tree8_full, cfg, q, cache, tree, None, None, 0, (out, tau, supp), workspace, stream)
+
+
+def ekv_tree8_sparse_softmax(cfg, q, cache, tree, page_idx, n_sel, out, lse, workspace, stream=None):
+    _tree(load_library().ekv_tree8_sparse_softmax, cfg, q, cache, tree, page_idx, n_sel, cfg.n_q_heads, (out, lse), workspace, stream)
+
+
+def ekv_tree8_full_softmax(cfg, q, cache, tree, out, lse, workspace, stream=None):
+    _tree(load_library().ekv_tree8_full_softmax, cfg, q, cache, tree, None, None, 0, (out, lse), workspace, stream)

@@ -13,7 +13,8 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libentmaxkv.so")
 SOURCES = ["api.hip", "stats.hip", "score.hip", "select_topk.hip", "select_gauss.hip", "select_box.hip", "decode.hip",
            "decode_windows.hip", "cache8.hip", "decode8_scores.hip", "decode8_held.hip", "decode8_softmax.hip",
-           "softmax_sparse.hip", "norm_rotate.hip", "append.hip", "probe.hip"]
+           "softmax_sparse.hip", "norm_rotate.hip", "append.hip", "tree_softmax.hip",
+           "tree_scores.hip", "tree_solve.hip", "probe.hip"]
 # packed-FP32 instructions are switched off for all device code (hipcc-only flag; the host pass warns
 # that it does not know the feature, which is harmless)
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang",

@@ -4,6 +4,7 @@
 #include <cstring>
 #include <mutex>
 #include "ekv_internal.h"
+#include "ekv_tree.h"
 
 namespace ekv {
 
@@ -522,6 +523,136 @@ ekv_status ekv_cache_append(const ekv_config* cfg, const ekv_cache_view* cache, 
   if (tokens->max_tokens >= 1 << 30 || (int64_t)tokens->max_tokens * dm.Hkv > 0x7fffffff) return EKV_ERR_UNSUPPORTED;
   launch_cache_append(dm, *cache, stats, *tokens, rows, n_rows, k_new, k_stride, v_new, v_stride, (hipStream_t)stream);
   return finish((hipStream_t)stream);
+}
+
+static ekv_status check_tree_sizes(int32_t max_tokens, int32_t max_tree) {
+  if (max_tokens <= 0 || max_tree <= 0) return EKV_ERR_INVALID_ARG;
+  return max_tree <= kTreeMost ? EKV_OK : EKV_ERR_UNSUPPORTED;
+}
+// lists: kPerHead, kAllPages or kGroupList
+static bool tree_supported(const Dims& dm, int lists, bool entmax, int n_tokens, int most) {
+  const int L = lists == kPerHead ? dm.Hq : dm.Hkv;
+  if (entmax) return tree_entmax_supported(dm, lists == kAllPages, L, n_tokens, most);
+  return tree_softmax_supported(dm, lists == kAllPages, L, most) && (int64_t)n_tokens * dm.Hq <= 0x7fffffff;
+}
+static size_t tree_ws_bytes(const Dims& dm, int lists, bool entmax, int n_tokens, int most) {
+  const int L = lists == kAllPages ? dm.Hkv : dm.Hq;         // one size for lists per query head and per KV head
+  return entmax ? tree_entmax_ws_bytes(dm, lists == kAllPages, L, n_tokens) : tree_softmax_ws_bytes(dm, L, most);
+}
+
+// one of cache and c8; entmax: norm is tau, else the log-sum-exp and supp is null
+static ekv_status tree_common(const ekv_config* cfg, int lists, bool entmax, const void* q, const ekv_cache_view* cache,
+                              const ekv_cache8_view* c8, const ekv_tree_view* tree, const int32_t* page_idx, const int32_t* n_sel,
+                              float* out, float* norm, int32_t* supp, void* workspace, size_t workspace_bytes, void* stream) {
+  Dims dm;
+  ekv_status s = make_dims(cfg, dm);
+  if (s != EKV_OK) return s;
+  TreeArgs a{};
+  if (c8 != nullptr) {
+    if ((s = check_cache8(c8, dm, true)) != EKV_OK) return s;
+    a.k_pool = c8->k_pool; a.v_pool = c8->v_pool; a.k_scale = c8->k_scale; a.v_scale = c8->v_scale;
+    a.block_table = c8->block_table; a.seq_lens = c8->seq_lens; a.n_phys = c8->n_phys_pages;
+  } else {
+    if ((s = check_cache(cache, true)) != EKV_OK) return s;
+    if ((s = check_pool_rows(cache, dm)) != EKV_OK) return s;
+    a.k_pool = cache->k_pool; a.v_pool = cache->v_pool; a.block_table = cache->block_table; a.seq_lens = cache->seq_lens;
+    a.n_phys = cache->n_phys_pages;
+  }
+  if (!ok_ptr(q) || !ok_ptr(out) || !ok_ptr4(norm) || (entmax && !ok_ptr4(supp))) return EKV_ERR_INVALID_ARG;
+  if (lists != kAllPages && (!ok_ptr4(page_idx) || !ok_ptr4(n_sel))) return EKV_ERR_INVALID_ARG;
+  if (tree == nullptr || !ok_ptr(tree->k_new) || !ok_ptr(tree->v_new) || !ok_ptr4(tree->start) || !ok_ptr8(tree->visible))
+    return EKV_ERR_INVALID_ARG;
+  const int64_t row = (int64_t)dm.Hkv * cfg->head_dim;
+  if (tree->k_stride < row || tree->v_stride < row || tree->k_stride % 8 != 0 || tree->v_stride % 8 != 0) return EKV_ERR_INVALID_ARG;
+  if ((s = check_tree_sizes(tree->max_tokens, tree->max_tree)) != EKV_OK) return s;
+  if (!tree_supported(dm, lists, entmax, tree->max_tokens, tree->max_tree)) return EKV_ERR_UNSUPPORTED;
+  if (workspace == nullptr || !aligned16(workspace) ||
+      workspace_bytes < tree_ws_bytes(dm, lists, entmax, tree->max_tokens, tree->max_tree))
+    return EKV_ERR_WORKSPACE;
+  a.q = q; a.page_idx = page_idx; a.n_sel = n_sel;
+  a.k_new = tree->k_new; a.v_new = tree->v_new; a.ks = tree->k_stride; a.vs = tree->v_stride;
+  a.start = tree->start; a.visible = tree->visible;
+  a.B = dm.B; a.Hq = dm.Hq; a.Hkv = dm.Hkv; a.HkvPool = dm.HkvPool; a.P = dm.P; a.Mmax = dm.Mmax; a.cap = dm.cap;
+  a.N = tree->max_tokens; a.most = tree->max_tree;
+  a.L = lists == kPerHead ? dm.Hq : dm.Hkv;
+  a.GL = dm.Hq / a.L;
+  a.U = dm.B * a.L;
+  a.page_div = make_page_div(dm.P);
+  a.out = out; a.norm = norm;
+  if (entmax) launch_tree_entmax(dm, a, c8 != nullptr, supp, workspace, (hipStream_t)stream);
+  else launch_tree_softmax(dm, a, c8 != nullptr, workspace, (hipStream_t)stream);
+  return finish((hipStream_t)stream);
+}
+
+ekv_status ekv_tree_sparse(const ekv_config* cfg, const void* q, const ekv_cache_view* cache, const ekv_tree_view* tree, const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau, int32_t* supp, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  return tree_common(cfg, kPerHead, true, q, cache, nullptr, tree, page_idx, n_sel, out, tau, supp, workspace, workspace_bytes, stream);
+}
+
+ekv_status ekv_tree_sparse_group(const ekv_config* cfg, const void* q, const ekv_cache_view* cache, const ekv_tree_view* tree, const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau, int32_t* supp, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  return tree_common(cfg, kGroupList, true, q, cache, nullptr, tree, page_idx, n_sel, out, tau, supp, workspace, workspace_bytes, stream);
+}
+
+ekv_status ekv_tree_full(const ekv_config* cfg, const void* q, const ekv_cache_view* cache, const ekv_tree_view* tree, float* out, float* tau, int32_t* supp, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  return tree_common(cfg, kAllPages, true, q, cache, nullptr, tree, nullptr, nullptr, out, tau, supp, workspace, workspace_bytes, stream);
+}
+
+ekv_status ekv_tree_sparse_softmax(const ekv_config* cfg, const void* q, const ekv_cache_view* cache, const ekv_tree_view* tree, const int32_t* page_idx, const int32_t* n_sel, float* out, float* lse, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  return tree_common(cfg, kPerHead, false, q, cache, nullptr, tree, page_idx, n_sel, out, lse, nullptr, workspace, workspace_bytes, stream);
+}
+
+ekv_status ekv_tree_full_softmax(const ekv_config* cfg, const void* q, const ekv_cache_view* cache, const ekv_tree_view* tree, float* out, float* lse, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  return tree_common(cfg, kAllPages, false, q, cache, nullptr, tree, nullptr, nullptr, out, lse, nullptr, workspace, workspace_bytes, stream);
+}
+
+ekv_status ekv_tree8_sparse(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, const ekv_tree_view* tree, const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau, int32_t* supp, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  if (cache == nullptr) return EKV_ERR_INVALID_ARG;
+  return tree_common(cfg, kPerHead, true, q, nullptr, cache, tree, page_idx, n_sel, out, tau, supp, workspace, workspace_bytes, stream);
+}
+
+ekv_status ekv_tree8_sparse_group(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, const ekv_tree_view* tree, const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau, int32_t* supp, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  if (cache == nullptr) return EKV_ERR_INVALID_ARG;
+  return tree_common(cfg, kGroupList, true, q, nullptr, cache, tree, page_idx, n_sel, out, tau, supp, workspace, workspace_bytes, stream);
+}
+
+ekv_status ekv_tree8_full(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, const ekv_tree_view* tree, float* out, float* tau, int32_t* supp, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  if (cache == nullptr) return EKV_ERR_INVALID_ARG;
+  return tree_common(cfg, kAllPages, true, q, nullptr, cache, tree, nullptr, nullptr, out, tau, supp, workspace, workspace_bytes, stream);
+}
+
+ekv_status ekv_tree8_sparse_softmax(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, const ekv_tree_view* tree, const int32_t* page_idx, const int32_t* n_sel, float* out, float* lse, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  if (cache == nullptr) return EKV_ERR_INVALID_ARG;
+  return tree_common(cfg, kPerHead, false, q, nullptr, cache, tree, page_idx, n_sel, out, lse, nullptr, workspace, workspace_bytes, stream);
+}
+
+ekv_status ekv_tree8_full_softmax(const ekv_config* cfg, const void* q, const ekv_cache8_view* cache, const ekv_tree_view* tree, float* out, float* lse, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  if (cache == nullptr) return EKV_ERR_INVALID_ARG;
+  return tree_common(cfg, kAllPages, false, q, nullptr, cache, tree, nullptr, nullptr, out, lse, nullptr, workspace, workspace_bytes, stream);
+}
+
+ekv_status ekv_tree_workspace_bytes(const ekv_config* cfg, int32_t op, int32_t max_tokens, int32_t max_tree, size_t* bytes) {
+  Dims dm;
+  ekv_status s = make_dims(cfg, dm);
+  if (s != EKV_OK) return s;
+  if (bytes == nullptr || op < EKV_OP_TREE_SPARSE || op > EKV_OP_TREE_FULL_SOFTMAX) return EKV_ERR_INVALID_ARG;
+  if ((s = check_tree_sizes(max_tokens, max_tree)) != EKV_OK) return s;
+  const bool entmax = op == EKV_OP_TREE_SPARSE || op == EKV_OP_TREE_FULL;
+  const int lists = op == EKV_OP_TREE_FULL || op == EKV_OP_TREE_FULL_SOFTMAX ? kAllPages : kPerHead;
+  // lists per KV head may be within range where lists per query head are not
+  if (!tree_supported(dm, lists, entmax, max_tokens, max_tree) &&
+      !(entmax && lists == kPerHead && tree_supported(dm, kGroupList, true, max_tokens, max_tree)))
+    return EKV_ERR_UNSUPPORTED;
+  *bytes = tree_ws_bytes(dm, lists, entmax, max_tokens, max_tree);
+  return EKV_OK;
 }
 
 ekv_status ekv_probe_read(const void* base, const int32_t* page_ids, const int32_t* lookup, int32_t n_pages,

@@ -1,0 +1,493 @@
+// Softmax attention of drafted rows over the cache and over the drafted keys that their masks name (ekv_tree.h has the layout).
+//
+// One pass over K and V with the running maximum and sum of every row.  The work of all lists is one sequence of steps (tiles of
+// keys; the drafted keys are a list's last), of which every workgroup takes an even, contiguous share; a list that several
+// workgroups share leaves partial results, two at most to a workgroup, which a second launch joins.
+// bf16 products take float32 weights as three terms that sum to them exactly (8 + 8 + 8 bits), so sums are float32 sums of exact
+// products, as in the single-token call.  The maximum only has to keep exp in range: it moves when a score passes it by 2^kSlack.
+// What a mask hides counts for nothing, infinities and NaN in its value among them: such drafted values are taken out of the
+// product (0 * NaN) and added by themselves to the rows that see them.
+#include "ekv_tree.h"
+
+namespace ekv {
+
+constexpr int kRec = kD + 2;
+constexpr float kSlack = 8.f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+
+// floats of a partial result: rows of outputs, then (maximum, sum) of every row
+__host__ __device__ constexpr size_t tree_rec(int rows) { return (size_t)rows * kRec; }
+
+__device__ __forceinline__ uint32_t top_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
+__device__ __forceinline__ float below(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+
+template <typename TQ, int NQ, int TILES> struct TreeSoftmax {
+  f32x4_t o[NQ][8];                              // lane (c, j): channels 16 i + 4 j + 0..3 of row c
+  float m[NQ], l[NQ];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+      m[t] = -INFINITY; l[t] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[t][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  // One LDS tile.  all: every key counts; else seen[t] has bit i for the tile's key i, of the lane's row.  bad: keys whose values are added
+  // by themselves, from v_bad.
+  __device__ __forceinline__ void add(const char* k, const char* v, const TreeQuery<TQ, NQ>& q, float zscale, bool all,
+                                      const uint64_t (&seen)[NQ], uint64_t bad, const TQ* v_bad, int64_t v_stride) {
+    const int lane = threadIdx.x & 63, c = lane & 15, j = lane >> 4;
+    f32x4_t p[TILES][NQ];
+    bool higher = false;
+    float top[NQ];
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) top[t] = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      tree_scores<TQ, NQ>(k, i, q, p[i]);
+#pragma unroll
+      for (int t = 0; t < NQ; ++t) p[i][t] *= zscale;
+    }
+    if (!all) {
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) {
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) {
+          const uint32_t bits = (uint32_t)(seen[t] >> (16 * i + 4 * j));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[i][t][e] = bits >> e & 1 ? p[i][t][e] : -INFINITY;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+#pragma unroll
+      for (int t = 0; t < NQ; ++t) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top[t] = fmaxf(top[t], p[i][t][e]);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) higher |= top[t] > m[t] + kSlack;
+    if (__any(higher)) {
+#pragma unroll
+      for (int t = 0; t < NQ; ++t) {
+        float x = fmaxf(top[t], __shfl_xor(top[t], 16));
+        x = fmaxf(x, __shfl_xor(x, 32));
+        const float now = fmaxf(m[t], x), f = now > -INFINITY ? __builtin_amdgcn_exp2f(m[t] - now) : 1.f;
+        m[t] = now;
+        l[t] *= f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[t][i] *= f;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+      const float base = m[t] > -INFINITY ? m[t] : 0.f;
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[i][t][e] = __builtin_amdgcn_exp2f(p[i][t][e] - base);
+          l[t] += p[i][t][e];
+        }
+      }
+    }
+    if (bad != 0) {
+      for (uint64_t left = bad; left != 0; left &= left - 1) {
+        const int key = __builtin_ctzll(left);
+        const TQ* row = v_bad + (int64_t)key * v_stride + 4 * j;
+        float w[NQ];
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) {
+          w[t] = 0.f;
+#pragma unroll
+          for (int i = 0; i < TILES; ++i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if ((key >> 4) == i && (key & 3) == e) {
+                w[t] = __shfl(p[i][t][e], (((key >> 2) & 3) << 4) + c);
+                p[i][t][e] = j == ((key >> 2) & 3) ? 0.f : p[i][t][e];
+              }
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float x[4];
+          if constexpr (sizeof(TQ) == 2) {
+            const uint2 u = *reinterpret_cast<const uint2*>(row + 16 * i);
+            x[0] = __uint_as_float(u.x << 16); x[1] = __uint_as_float(u.x & 0xffff0000u);
+            x[2] = __uint_as_float(u.y << 16); x[3] = __uint_as_float(u.y & 0xffff0000u);
+          } else {
+            const float4 u = *reinterpret_cast<const float4*>(row + 16 * i);
+            x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+          }
+#pragma unroll
+          for (int t = 0; t < NQ; ++t) {
+            if (seen[t] >> key & 1) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[t][i][e] = fmaf(w[t], x[e], o[t][i][e]);
+            }
+          }
+        }
+      }
+    }
+    if constexpr (sizeof(TQ) == 2) {
+#pragma unroll
+      for (int i = 0; i < TILES; i += 2) {       // 32 keys: lane group j has keys 4j..4j+3 of either tile
+        bf16x8_t w[3][NQ];
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) {
+          float x[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { x[e] = p[i][t][e]; x[4 + e] = p[i + 1][t][e]; }
+#pragma unroll
+          for (int term = 0; term < 3; ++term) {
+            u32x4_t r;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = top_halves(x[2 * e], x[2 * e + 1]);
+            w[term][t] = __builtin_bit_cast(bf16x8_t, r);
+            if (term < 2) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] = below(x[e]);
+            }
+          }
+        }
+#pragma unroll
+        for (int ch = 0; ch < 8; ++ch) {
+          const int row = 16 * i + 4 * j + (c >> 2), piece = 2 * ch + ((c & 3) >> 1), half = (c & 1) * 8;
+          const s16x4_t a0 = read_transposed(v + tree_piece<TQ>(row, piece) + half), a1 = read_transposed(v + tree_piece<TQ>(row + 16, piece) + half);
+          const bf16x8_t a = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+          for (int t = 0; t < NQ; ++t) {
+#pragma unroll
+            for (int term = 2; term >= 0; --term)          // the smallest terms first
+              o[t][ch] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[term][t], o[t][ch], 0, 0, 0);
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) {
+#pragma unroll
+        for (int ch = 0; ch < 8; ++ch) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float a = *reinterpret_cast<const float*>(v + tree_piece<TQ>(16 * i + 4 * j + e, 4 * ch + (c >> 2)) + 4 * (c & 3));
+#pragma unroll
+            for (int t = 0; t < NQ; ++t) o[t][ch] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p[i][t][e], o[t][ch], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
+};
+
+template <typename TQ> __device__ __forceinline__ bool has_no_number(const uint4& v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  bool no = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    no |= (w[i] & 0x7f800000u) == 0x7f800000u;
+    if constexpr (sizeof(TQ) == 2) no |= (w[i] & 0x7f80u) == 0x7f80u;
+  }
+  return no;
+}
+
+template <typename TQ, typename TC, int NQ, int WQ>
+__global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2)))
+void tree_softmax_kernel(const TreeArgs A) {
+  using S = TreeShape<TQ, TC, NQ, WQ, 2>;
+  extern __shared__ int pre_lds[];
+  __shared__ __attribute__((aligned(16))) char s_tile[S::kLds];
+  __shared__ uint32_t s_bad[S::kGroups][2];
+  __shared__ int wsum[kTreeWaves];
+  constexpr int RS = kD + 4;                     // floats between rows of partial outputs in LDS
+  static_assert(WQ == 4 || NQ * 16 * RS * 4 * 2 <= S::kLds, "two wavefronts' partial outputs take the tiles' place");
+  __shared__ float s_m[kTreeWaves][16 * NQ], s_l[kTreeWaves][16 * NQ];
+  const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), c = lane & 15, j = lane >> 4;
+  const int grp = WQ == 1 ? w : 0, tid = WQ == 1 ? lane : threadIdx.x;
+  char* tile = s_tile + grp * 2 * S::kSideBytes;
+  tree_work<S::kRows, S::kKeys>(A, pre_lds, wsum, [&](int wg, int unit, const TreeRows& R, int blk, int st0, int st1, int steps, bool first) {
+    const int b = unit / A.L, list = unit - b * A.L, list_head = list * A.GL, hkv = list_head / (A.Hq / A.Hkv);
+    const int tiles0 = min(st0, steps - 1), tiles1 = min(st1, steps - 1);          // the steps' tiles of the cache
+    const bool drafted = st1 == steps;
+    const int r0 = blk * S::kRows + (WQ == 4 ? w * 16 * NQ : 0);         // the wavefront's first row
+    TreeQuery<TQ, NQ> q;
+    q.load(A, R, list_head, r0);
+    TreeSoftmax<TQ, NQ, S::kTiles> acc;
+    acc.clear();
+    // a group's share of the tiles
+    const int n_t = tiles1 - tiles0, t0 = tiles0 + n_t * grp / S::kGroups, t1 = tiles0 + n_t * (grp + 1) / S::kGroups;
+    const TreeLook look(A, unit, hkv);
+    const int row = lane % S::kKeys;
+    auto pos_of = [&](int t) { return min(t, t1 - 1) * S::kKeys + row; };
+    TreeStage<TQ, TC, NQ, WQ, 2> stage;
+    uint64_t valid_next = 0;
+    auto fetch = [&](int t, int lp, int ph) {
+      const int pos = pos_of(t);
+      const uint32_t at_row = look.row(pos, ph);
+      valid_next = __ballot(look.valid(pos, lp));
+      stage.request(A, tid, [&](int i) { return (uint32_t)__shfl((int)at_row, i); });
+    };
+    int lp1 = 0, ph1 = 0, lp2 = 0;
+    if (t0 < t1) {
+      const int lp0 = look.page(pos_of(t0)), ph0 = look.phys(lp0);
+      lp1 = look.page(pos_of(t0 + 1)); lp2 = look.page(pos_of(t0 + 2));
+      ph1 = look.phys(lp1);
+      fetch(t0, lp0, ph0);
+    }
+    // after the cache's tiles the drafted keys', which the groups take in turn
+    int d0 = WQ == 1 ? grp * S::kKeys : 0;
+    for (int t = t0; t < t1 || (drafted && d0 < R.count); ++t) {
+      const bool cached = t < t1;
+      uint64_t seen[NQ], bad = 0;
+      bool all = false;
+      const TQ* v_bad = nullptr;
+      if constexpr (WQ == 4) __syncthreads(); else wave_order();           // the tile before is read
+      if (cached) {
+        const uint64_t valid = valid_next;
+        stage.commit(tile, tid, valid);
+        const int ph2 = look.phys(lp2), lp3 = look.page(pos_of(t + 3));
+        fetch(t + 1, lp1, ph1);
+        lp1 = lp2; ph1 = ph2; lp2 = lp3;
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) seen[i] = valid;
+        constexpr uint64_t full = S::kKeys == 64 ? ~0ull : (1ull << (S::kKeys & 63)) - 1;
+        all = (valid & full) == full;
+      } else {
+        if (tid < 2) s_bad[grp][tid] = 0;
+        if constexpr (WQ == 4) __syncthreads(); else wave_order();
+        constexpr int pieces = S::kRowBytes / 16;
+#pragma unroll 1
+        for (int i = tid; i < S::kKeys * pieces; i += S::kThreads) {
+          const int key_row = i / pieces, piece = i % pieces, key = d0 + key_row;
+          const bool in = key < R.count;
+          const int kc = R.first + min(key, R.count - 1);
+          uint4 kv = load16((const char*)((const TQ*)A.k_new + kc * A.ks + hkv * kD) + 16 * piece);
+          uint4 vv = load16((const char*)((const TQ*)A.v_new + kc * A.vs + hkv * kD) + 16 * piece);
+          const bool no = has_no_number<TQ>(vv);
+          if (in && no) atomicOr(&s_bad[grp][key_row >> 5], 1u << (key_row & 31));
+          if (!in) kv = make_uint4(0u, 0u, 0u, 0u);
+          if (!in || no) vv = make_uint4(0u, 0u, 0u, 0u);
+          *reinterpret_cast<uint4*>(tile + tree_piece<TQ>(key_row, piece)) = kv;
+          *reinterpret_cast<uint4*>(tile + S::kSideBytes + tree_piece<TQ>(key_row, piece)) = vv;
+        }
+        const uint64_t there = R.count - d0 >= 64 ? ~0ull : (1ull << (R.count - d0)) - 1;
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+          const int r = min(r0 + 16 * i + c, R.count * A.GL - 1);
+          seen[i] = (A.visible[R.first + r / A.GL] >> d0) & there;
+        }
+        v_bad = (const TQ*)A.v_new + (int64_t)(R.first + d0) * A.vs + hkv * kD;
+      }
+      if constexpr (WQ == 4) __syncthreads(); else wave_order();
+      if (!cached) {
+        bad = (uint64_t)(uint32_t)uniform((int)s_bad[grp][0]) | (uint64_t)(uint32_t)uniform((int)s_bad[grp][1]) << 32;
+        d0 += S::kGroups * S::kKeys;
+      }
+      acc.add(tile, tile + S::kSideBytes, q, A.zscale, all, seen, bad, v_bad, A.vs);
+    }
+    // the rows' sums
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+      acc.l[t] += __shfl_xor(acc.l[t], 16);
+      acc.l[t] += __shfl_xor(acc.l[t], 32);
+    }
+    const bool whole = st0 == 0 && st1 == steps;
+    float* rec = A.part + tree_rec(S::kRows) * (2 * (size_t)wg + (first ? 0 : 1));
+    auto put = [&](int r, int ch, float4 o, float m, float l) {            // four channels of row r of the block
+      const int row = blk * S::kRows + r;
+      if (row >= R.count * A.GL) return;
+      if (whole) {
+        const int tok = row / A.GL;
+        const size_t to = (size_t)(R.first + tok) * A.Hq + list_head + (row - tok * A.GL);
+        const float f = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);          // no key at all: a zero output; NaN stays
+        *reinterpret_cast<float4*>(A.out + to * kD + ch) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+        if (ch == 0) A.norm[to] = l == 0.f ? -INFINITY : m * kLn2 + __logf(l);
+      } else {
+        *reinterpret_cast<float4*>(rec + (size_t)r * kD + ch) = o;
+        if (ch == 0) *reinterpret_cast<float2*>(rec + (size_t)S::kRows * kD + 2 * r) = make_float2(m, l);
+      }
+    };
+    if constexpr (WQ == 4) {
+#pragma unroll
+      for (int t = 0; t < NQ; ++t) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          put(w * 16 * NQ + 16 * t + c, 16 * i + 4 * j, make_float4(acc.o[t][i][0], acc.o[t][i][1], acc.o[t][i][2], acc.o[t][i][3]), acc.m[t], acc.l[t]);
+      }
+    } else {
+      // two wavefronts hand theirs to the other two, and one of these to the first; then the first's go out
+      float* so = reinterpret_cast<float*>(s_tile);
+      if (j == 0) {
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) { s_m[w][16 * t + c] = acc.m[t]; s_l[w][16 * t + c] = acc.l[t]; }
+      }
+      float f[NQ], M[NQ], Ls[NQ];
+      __syncthreads();                                                     // the tiles are read
+#pragma unroll
+      for (int t = 0; t < NQ; ++t) {
+        M[t] = fmaxf(fmaxf(s_m[0][16 * t + c], s_m[1][16 * t + c]), fmaxf(s_m[2][16 * t + c], s_m[3][16 * t + c]));
+        f[t] = acc.m[t] > -INFINITY ? __builtin_amdgcn_exp2f(acc.m[t] - M[t]) : 0.f;
+        Ls[t] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kTreeWaves; ++i) {
+          const float mi = s_m[i][16 * t + c];
+          Ls[t] = fmaf(s_l[i][16 * t + c], mi > -INFINITY ? __builtin_amdgcn_exp2f(mi - M[t]) : 0.f, Ls[t]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc.o[t][i] *= f[t];
+      }
+#pragma unroll
+      for (int hand = 2; hand >= 1; hand >>= 1) {                          // wavefronts hand..2 hand-1 to 0..hand-1
+        if (w >= hand && w < 2 * hand) {
+#pragma unroll
+          for (int t = 0; t < NQ; ++t) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              *reinterpret_cast<f32x4_t*>(so + ((size_t)(w - hand) * 16 * NQ + 16 * t + c) * RS + 16 * i + 4 * j) = acc.o[t][i];
+          }
+        }
+        __syncthreads();
+        if (w < hand) {
+#pragma unroll
+          for (int t = 0; t < NQ; ++t) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              acc.o[t][i] += *reinterpret_cast<const f32x4_t*>(so + ((size_t)w * 16 * NQ + 16 * t + c) * RS + 16 * i + 4 * j);
+          }
+        }
+        __syncthreads();
+      }
+      if (w == 0) {
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            put(16 * t + c, 16 * i + 4 * j, make_float4(acc.o[t][i][0], acc.o[t][i][1], acc.o[t][i][2], acc.o[t][i][3]), M[t], Ls[t]);
+        }
+      }
+    }
+  });
+}
+
+// Joins the partial results of row blocks that several workgroups worked on, in their order: a wavefront per row, two channels a lane.
+__global__ __launch_bounds__(256) void tree_join_kernel(const TreeArgs A, int rows, int keys) {
+  const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
+  const int most = A.most * A.GL, per = (most + 3) / 4;
+  const int unit = (int)(blockIdx.x / (unsigned)per), r = (int)(blockIdx.x % (unsigned)per) * 4 + w, b = unit / A.L;
+  const TreeRows R = tree_rows(A, b);
+  if (r >= R.count * A.GL) return;
+  const int blk = r / rows, steps = tree_steps(A, unit, keys);
+  const int total = A.pre[A.U], share = total / A.W, rem = total - share * A.W;
+  const int begin = A.pre[unit] + blk * steps, end = begin + steps;
+  auto wg_of = [&](int s) { return s < rem * (share + 1) ? s / (share + 1) : rem + (s - rem * (share + 1)) / share; };
+  auto first_of = [&](int i) { return i * share + min(i, rem); };
+  const int w0 = wg_of(begin), w1 = wg_of(end - 1);
+  if (w0 == w1) return;                                                    // written by that workgroup
+  const int in_blk = r - blk * rows;
+  // the block is the second that workgroup w0 left if it began before the block did
+  auto rec_of = [&](int i) { return A.part + tree_rec(rows) * (2 * (size_t)i + (i == w0 && first_of(i) < begin ? 1 : 0)); };
+  float M = -INFINITY;
+  for (int i = w0 + lane; i <= w1; i += 64) M = fmaxf(M, rec_of(i)[(size_t)rows * kD + 2 * in_blk]);
+  M = wave_max(M);
+  float L = 0.f;
+  float2 o = make_float2(0.f, 0.f);
+  for (int i = w0; i <= w1; ++i) {
+    const float* rec = rec_of(i);
+    const float2 ml = *reinterpret_cast<const float2*>(rec + (size_t)rows * kD + 2 * in_blk);
+    const float2 x = *reinterpret_cast<const float2*>(rec + (size_t)in_blk * kD + 2 * lane);
+    const float f = ml.x > -INFINITY ? __builtin_amdgcn_exp2f(ml.x - M) : 0.f;
+    L = fmaf(ml.y, f, L);
+    o.x = fmaf(x.x, f, o.x);
+    o.y = fmaf(x.y, f, o.y);
+  }
+  const int list = unit - b * A.L, tok = r / A.GL;
+  const size_t to = (size_t)(R.first + tok) * A.Hq + list * A.GL + (r - tok * A.GL);
+  const float f = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+  *reinterpret_cast<float2*>(A.out + to * kD + 2 * lane) = make_float2(o.x * f, o.y * f);
+  if (lane == 0) A.norm[to] = L == 0.f ? -INFINITY : M * kLn2 + __logf(L);
+}
+
+__global__ __launch_bounds__(1024) void tree_prefix_kernel(const TreeArgs A, int keys, int rows) {
+  __shared__ int wsum[16];
+  block_exclusive_prefix<1024>(A.U, [&](int u) { return tree_unit_steps(A, u, keys, rows); }, A.pre, wsum);
+}
+void launch_tree_prefix(const TreeArgs& a, int keys, int rows, hipStream_t st) {
+  hipLaunchKernelGGL(tree_prefix_kernel, dim3(1), dim3(1024), 0, st, a, keys, rows);
+}
+
+// ------------------------------------------------------------------------------------------
+constexpr int kTreeWgs = 512;                    // workgroups of a launch at most; workspaces are sized for them
+
+struct TreeDims { int rows, keys; };             // of a workgroup, of a tile
+static TreeDims softmax_dims(const Dims& dm, int list_rows) {
+  if (dm.dtype == EKV_F32) return list_rows <= 16 ? TreeDims{16, 16} : TreeDims{64, 32};
+  return list_rows <= 16 ? TreeDims{16, 32} : list_rows <= 32 ? TreeDims{32, 32} : list_rows <= 64 ? TreeDims{64, 64} : TreeDims{128, 64};
+}
+static long long softmax_steps(const Dims& dm, bool dense, int lists, int list_rows) {
+  const TreeDims td = softmax_dims(dm, list_rows);
+  const long long tokens = (long long)(dense ? dm.Mmax : dm.cap) * dm.P;
+  return (long long)dm.B * lists * ((list_rows + td.rows - 1) / td.rows) * ((tokens + td.keys - 1) / td.keys + 1);
+}
+bool tree_softmax_supported(const Dims& dm, bool dense, int lists, int most) {
+  return softmax_steps(dm, dense, lists, most * (dm.Hq / lists)) <= 0x7fffffff;
+}
+size_t tree_softmax_ws_bytes(const Dims& dm, int lists, int most) {
+  const TreeDims td = softmax_dims(dm, most * (dm.Hq / lists));
+  return tree_pre_bytes((size_t)dm.B * lists) + 2 * kTreeWgs * tree_rec(td.rows) * sizeof(float);
+}
+
+template <typename TQ, typename TC, int NQ, int WQ>
+static void launch_softmax_shape(const TreeArgs& a, int grid, size_t lds, hipStream_t st) {
+  hipLaunchKernelGGL((tree_softmax_kernel<TQ, TC, NQ, WQ>), dim3(grid), dim3(kTreeThreads), lds, st, a);
+}
+template <typename TQ, typename TC>
+static void launch_softmax_T(const Dims& dm, TreeArgs a, hipStream_t st) {
+  const int list_rows = a.most * a.GL;
+  const TreeDims td = softmax_dims(dm, list_rows);
+  const bool dense = a.page_idx == nullptr;
+  const int cus = device_compute_units();
+  a.blocks = (list_rows + td.rows - 1) / td.rows;
+  const long long units = (long long)a.U * a.blocks, tokens = (long long)(dense ? dm.Mmax : dm.cap) * dm.P;
+  a.per_unit = tokens <= (units >= cus ? 8192 : units >= cus / 2 ? 2560 : 1024);
+  const long long steps = softmax_steps(dm, dense, a.L, list_rows);
+  const int most = 2 * cus < kTreeWgs ? 2 * cus : kTreeWgs, share = td.rows <= 32 ? kTreeWaves : 1;
+  const long long wgs = (steps + share - 1) / share;
+  a.W = (int)(wgs < most ? wgs : most);
+  size_t lds = 0;
+  if (!a.per_unit) {
+    if (a.U > kUnitsLdsMax) {
+      launch_tree_prefix(a, td.keys, td.rows, st);
+      a.pre_g = a.pre;
+    } else {
+      lds = (size_t)(a.U + 1) * sizeof(int);
+    }
+  }
+  const int grid = a.per_unit ? (int)units : a.W;
+  if (td.rows == 16) launch_softmax_shape<TQ, TC, 1, 1>(a, grid, lds, st);
+  else if (td.rows == 64) launch_softmax_shape<TQ, TC, 1, 4>(a, grid, lds, st);
+  if constexpr (sizeof(TQ) == 2) {
+    if (td.rows == 32) launch_softmax_shape<TQ, TC, 2, 1>(a, grid, lds, st);
+    else if (td.rows == 128) launch_softmax_shape<TQ, TC, 2, 4>(a, grid, lds, st);
+  }
+  if (!a.per_unit)
+    hipLaunchKernelGGL(tree_join_kernel, dim3((unsigned)a.U * ((list_rows + 3) / 4)), dim3(256), 0, st, a, td.rows, td.keys);
+}
+
+void launch_tree_softmax(const Dims& dm, TreeArgs a, bool codes, void* ws, hipStream_t st) {
+  a.pre = (int32_t*)ws;
+  a.part = (float*)((char*)ws + tree_pre_bytes(a.U));
+  a.zscale = dm.scale * kLog2e;
+  if (dm.dtype == EKV_F32) {
+    if (codes) launch_softmax_T<float, e4m3_t>(dm, a, st);
+    else launch_softmax_T<float, float>(dm, a, st);
+  } else {
+    if (codes) launch_softmax_T<bf16_t, e4m3_t>(dm, a, st);
+    else launch_softmax_T<bf16_t, bf16_t>(dm, a, st);
+  }
+}
+
+}  // namespace ekv

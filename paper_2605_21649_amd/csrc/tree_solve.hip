@@ -1,0 +1,297 @@
+// Entmax attention of drafted rows, second launch: from a row's scores and group maxima to its threshold and output.
+//
+// One workgroup per row (drafted token, query head).  The mass of the group maxima bounds the threshold from below, so only the
+// groups above that bound are read, and of them the candidates above it go to LDS, in the order of their wavefronts; one
+// wavefront iterates to the exact root, then every wavefront adds up the value rows of its part of the support (V is read
+// where a weight is not zero, nowhere else).  A row too flat for LDS is gone through in its scores instead, evaluation by evaluation.
+// A chain of latencies (maxima, scores, root, lookups, values), several rows to a compute unit.
+#include "ekv_solve.h"
+#include "ekv_tree.h"
+
+namespace ekv {
+
+constexpr int kGroup = 64;
+
+struct TreeSolveArgs {
+  TreeArgs t;
+  int32_t* supp;
+  float beta; int ibeta;
+  int rows;                                      // tokens * query heads
+};
+
+// Weighted sum of `n` value rows: weight and row of entry e are weight[e] and row[e] in LDS, rows `stride` elements apart; lane (r, c) adds
+// channels 8c..8c+7 of entries r, r + 4, ...
+template <typename T, typename W>
+__device__ __forceinline__ void add_rows(const T* v, int64_t stride, const float* weight, const uint32_t* row, int n, float (&acc)[8], W&& scaled) {
+  const int lane = threadIdx.x & 63, r = lane >> 4, c = lane & 15;
+  for (int e0 = 0; e0 < n; e0 += 32) {
+    Raw8<T> raw[8];
+    float p[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int e = e0 + 4 * k + r, ec = min(e, n - 1);
+      const uint32_t at = row[ec];
+      p[k] = e < n ? scaled(weight[ec], at) : 0.f;
+      load_raw8(v + (int64_t)at * stride + 8 * c, raw[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (e0 + 4 * k >= n) break;                // the same for the wavefront
+      float x[8];
+      widen8(raw[k], x);
+      const bool in = e0 + 4 * k + r < n;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] = in ? fmaf(p[k], x[i], acc[i]) : acc[i];
+    }
+  }
+}
+
+template <typename TQ, typename TC, int NW>
+__global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs S) {
+#pragma clang fp contract(off)
+  constexpr int NT = 64 * NW, SEG = NW == 1 ? 1024 : 512, R = 8;
+  __shared__ float s_u[NW][SEG];
+  __shared__ uint32_t s_at[NW][SEG];
+  __shared__ float s_o[NW][kD];
+  __shared__ float s_red[2][NW][3], s_one[NW];
+  __shared__ int s_n[NW], s_supp;
+  __shared__ float s_tau;
+  const TreeArgs& A = S.t;
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
+  const uint64_t lt = (1ull << lane) - 1;
+  // consecutive rows, the heads of a token, on one XCD
+  const int row = gridDim.x % kXcds == 0 ? (int)(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
+  const int n = row / A.Hq, hq = row - n * A.Hq;
+  const int b = wave_last_at_most(A.start, A.B, n);
+  const TreeRows T = tree_rows(A, b);
+  if (n < T.first || n >= T.first + T.count) return;         // of no sequence
+  const int list = hq / A.GL, unit = b * A.L + list, hkv = hq / (A.Hq / A.Hkv);
+  const int groups = (list_positions(A, unit) + kGroup - 1) / kGroup;      // of the cache; one more of drafted keys
+  const float* z = A.z + (size_t)row * A.zstride;
+  const float* zm = A.zmax + (size_t)row * A.n_groups;
+  const float zd = z[(size_t)groups * kGroup + lane];
+  // maxima, several groups to a register where there are more than registers (their mass is still no more than the row's)
+  float m[R];
+#pragma unroll
+  for (int k = 0; k < R; ++k) m[k] = k * NT + tid <= groups ? zm[k * NT + tid] : -INFINITY;
+  const bool folded = groups >= R * NT;
+  if (folded) {
+    for (int g = R * NT + tid; g <= groups; g += R * NT) {
+#pragma unroll
+      for (int k = 0; k < R; ++k) m[k] = fmaxf(m[k], zm[min(g + k * NT, groups)]);
+    }
+  }
+  float mx = m[0];
+#pragma unroll
+  for (int k = 1; k < R; ++k) mx = fmaxf(mx, m[k]);
+  const float zmax = NW == 1 ? wave_max(mx) : block_max(mx, s_one);
+  float* out = A.out + (size_t)row * kD;
+  if (!(zmax > -INFINITY)) {                                 // no key at all
+    if (tid < kD / 4) *reinterpret_cast<float4*>(out + 4 * tid) = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (tid == 0) { A.norm[row] = INFINITY; S.supp[row] = 0; }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < R; ++k) m[k] -= zmax;
+  const float eps = 4e-6f * fmaxf(1.f, fabsf(zmax));
+  int parity = 0;
+  float bound = group_bound(m, -1.0f - eps, S.beta, S.ibeta, [&](float& f, float& d) {
+    f = wave_sum(f); d = wave_sum(d);
+    if constexpr (NW > 1) {
+      if (lane == 0) { s_red[parity][w][0] = f; s_red[parity][w][1] = d; }
+      __syncthreads();
+      f = 0.f; d = 0.f;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) { f += s_red[parity][i][0]; d += s_red[parity][i][1]; }
+      parity ^= 1;
+    }
+  });
+  bound = fmaxf(bound - eps, -1.0f - eps);
+  const float thr = zmax + bound, lo_u = fminf(bound, -1e-7f), ud = zd - zmax;
+  // each(u, position) for every candidate of this wavefront's groups above `above` (relative), 64 lanes at a time
+  auto each_group = [&](uint64_t mask, int base, auto&& each) {
+    while (mask != 0) {
+      float zz[4];
+      int g[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        g[k] = mask != 0 ? base + __builtin_ctzll(mask) : -1;
+        mask &= mask - 1;
+        zz[k] = z[(size_t)max(g[k], 0) * kGroup + lane];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (g[k] < 0) break;
+        each(zz[k] - zmax, g[k] * kGroup + lane);
+      }
+    }
+  };
+  auto each_candidate = [&](float above, auto&& each) {
+    for (int base = 64 * w; base < groups; base += NT) {
+      const float x = base + lane < groups ? zm[base + lane] : -INFINITY;
+      each_group(__ballot(x - zmax > above), base, each);
+    }
+  };
+  int count = 0;
+  auto keep = [&](float u, int pos) {
+    const bool in = u > bound;
+    const uint64_t mk = __ballot(in);
+    const int o = count + __popcll(mk & lt);
+    if (in && o < SEG) { s_u[w][o] = u; s_at[w][o] = (uint32_t)pos; }
+    count += __popcll(mk);
+  };
+  if (folded) {
+    each_candidate(bound, keep);
+  } else {
+#pragma unroll
+    for (int k = 0; k < R; ++k) each_group(__ballot(m[k] > bound && k * NT + tid < groups), k * NT + 64 * w, keep);
+  }
+  (void)thr;
+  if (lane == 0) s_n[w] = count;
+  __syncthreads();
+  bool fits = true;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) fits &= s_n[i] <= SEG;
+  int supp = 0, evals = 0;
+  float tau;
+  if (fits) {
+    if (w == 0) {
+      tau = with_beta(S.ibeta, [&](auto ib) {
+        constexpr int IB = decltype(ib)::value;
+        return solve_tau_core([&](float t, float& F, float& D, int& cnt) {
+          float f = 0.f, d = 0.f;
+          const float x0 = fmaxf(ud - t, 0.f);
+          add_mass<IB>(x0, S.beta, f, d);
+          cnt = __popcll(__ballot(x0 > 0.f));
+#pragma unroll
+          for (int i = 0; i < NW; ++i) {
+            const int ni = s_n[i];
+            for (int e = 0; e < ni; e += 64) {
+              const float x = e + lane < ni ? fmaxf(s_u[i][e + lane] - t, 0.f) : 0.f;
+              add_mass<IB>(x, S.beta, f, d);
+              cnt += __popcll(__ballot(x > 0.f));
+            }
+          }
+          F = wave_sum(f); D = S.beta * wave_sum(d);
+        }, lo_u, NAN, IB, supp, evals);
+      });
+      if (lane == 0) { s_tau = tau; s_supp = supp; }
+    }
+    __syncthreads();
+    tau = s_tau; supp = s_supp;
+  } else {
+    parity = 0;
+    tau = solve_tau_core([&](float t, float& F, float& D, int& cnt) {
+      float f = 0.f, d = 0.f;
+      int c = 0;
+      auto mass = [&](float u, int) {
+        const float x = u - t;
+        if (x > 0.f) { f += pow_beta(x, S.beta, S.ibeta); d += pow_beta_m1(x, S.beta, S.ibeta); ++c; }
+      };
+      if (w == 0) mass(ud, 0);
+      each_candidate(t, mass);
+      f = wave_sum(f); d = wave_sum(d); c = wave_sum_i(c);
+      if (lane == 0) { s_red[parity][w][0] = f; s_red[parity][w][1] = d; s_red[parity][w][2] = __int_as_float(c); }
+      __syncthreads();
+      F = 0.f; D = 0.f; cnt = 0;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) { F += s_red[parity][i][0]; D += s_red[parity][i][1]; cnt += __float_as_int(s_red[parity][i][2]); }
+      D *= S.beta;
+      parity ^= 1;
+    }, lo_u, NAN, S.ibeta, supp, evals);
+    __syncthreads();
+  }
+  // weights and value rows of the support, in place
+  const TreeLook look(A, unit, hkv);
+  auto value_row = [&](int pos) { return look.row(pos, look.phys(look.page(pos))); };
+  auto scaled = [&](float p, uint32_t at) {
+    if constexpr (sizeof(TC) == 1) return p * A.v_scale[page_div(at, A.page_div)];
+    else return p;
+  };
+  float acc[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+  int n_sup = 0;
+  auto take = [&](float u, int pos, bool real) {             // a wavefront's next 64 entries, to its segment
+    const float x = u - tau;
+    const bool in = real && x > 0.f;
+    const uint64_t mk = __ballot(in);
+    const uint32_t at = value_row(in ? pos : 0);
+    wave_order();
+    if (in) {
+      const int o = n_sup + __popcll(mk & lt);
+      s_u[w][o] = pow_beta(x, S.beta, S.ibeta);
+      s_at[w][o] = at;
+    }
+    n_sup += __popcll(mk);
+    wave_order();
+  };
+  if (fits) {
+    for (int e = 0; e < count; e += 64) {
+      const int ec = min(e + lane, count - 1);
+      take(s_u[w][ec], (int)s_at[w][ec], e + lane < count);
+    }
+    add_rows((const TC*)A.v_pool, kD, s_u[w], s_at[w], n_sup, acc, scaled);
+  } else {
+    each_candidate(tau, [&](float u, int pos) {
+      take(u, pos, true);
+      if (n_sup > SEG - 64) {
+        add_rows((const TC*)A.v_pool, kD, s_u[w], s_at[w], n_sup, acc, scaled);
+        n_sup = 0;
+        wave_order();
+      }
+    });
+    add_rows((const TC*)A.v_pool, kD, s_u[w], s_at[w], n_sup, acc, scaled);
+  }
+  if (w == NW - 1) {                                         // the drafted keys' share
+    wave_order();
+    const float x = ud - tau;
+    const bool in = x > 0.f;
+    const uint64_t mk = __ballot(in);
+    if (in) {
+      const int o = __popcll(mk & lt);
+      s_u[w][o] = pow_beta(x, S.beta, S.ibeta);
+      s_at[w][o] = (uint32_t)lane;
+    }
+    wave_order();
+    add_rows((const TQ*)A.v_new + T.first * A.vs + hkv * kD, A.vs, s_u[w], s_at[w], __popcll(mk), acc, [](float p, uint32_t) { return p; });
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    acc[i] += __shfl_xor(acc[i], 16);
+    acc[i] += __shfl_xor(acc[i], 32);
+  }
+  if constexpr (NW == 1) {
+    if (lane < 16) store8(out + 8 * lane, acc);
+  } else {
+    if (lane < 16) store8(&s_o[w][8 * lane], acc);
+    __syncthreads();
+    if (tid < kD) {
+      float o = 0.f;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) o += s_o[i][tid];
+      out[tid] = o;
+    }
+  }
+  if (tid == 0) { A.norm[row] = tau + zmax; S.supp[row] = supp; }
+}
+
+template <typename TQ, typename TC>
+static void launch_solve_T(const TreeSolveArgs& s, hipStream_t st) {
+  if (s.rows > 8 * device_compute_units() && s.t.n_groups <= 512)
+    hipLaunchKernelGGL((tree_solve_kernel<TQ, TC, 1>), dim3(s.rows), dim3(64), 0, st, s);
+  else
+    hipLaunchKernelGGL((tree_solve_kernel<TQ, TC, 4>), dim3(s.rows), dim3(256), 0, st, s);
+}
+void launch_tree_solve(const Dims& dm, const TreeArgs& a, bool codes, int32_t* supp, hipStream_t st) {
+  const TreeSolveArgs s{a, supp, dm.beta, dm.ibeta, a.N * dm.Hq};
+  if (dm.dtype == EKV_F32) {
+    if (codes) launch_solve_T<float, e4m3_t>(s, st);
+    else launch_solve_T<float, float>(s, st);
+  } else {
+    if (codes) launch_solve_T<bf16_t, e4m3_t>(s, st);
+    else launch_solve_T<bf16_t, bf16_t>(s, st);
+  }
+}
+
+}  // namespace ekv
