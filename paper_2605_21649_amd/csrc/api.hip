@@ -569,7 +569,7 @@ static ekv_status tree_common(const ekv_config* cfg, int lists, bool entmax, con
   if (workspace == nullptr || !aligned16(workspace) ||
       workspace_bytes < tree_ws_bytes(dm, lists, entmax, tree->max_tokens, tree->max_tree))
     return EKV_ERR_WORKSPACE;
-  a.q = q; a.page_idx = page_idx; a.n_sel = n_sel;
+  a.q = q; a.page_idx = page_idx; a.n_sel = lists == kAllPages ? a.seq_lens : n_sel;
   a.k_new = tree->k_new; a.v_new = tree->v_new; a.ks = tree->k_stride; a.vs = tree->v_stride;
   a.start = tree->start; a.visible = tree->visible;
   a.B = dm.B; a.Hq = dm.Hq; a.Hkv = dm.Hkv; a.HkvPool = dm.HkvPool; a.P = dm.P; a.Mmax = dm.Mmax; a.cap = dm.cap;

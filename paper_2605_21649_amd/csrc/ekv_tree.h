@@ -9,19 +9,18 @@
 // Keys and values pass through LDS once for all rows of a workgroup: rows of a tile lie at their length, their 16-byte pieces in an
 // order that their number turns (piece ^ row % 16), so that neither sixteen rows' same piece nor the transposing reads of V
 // meet in a bank.  An 8-bit cache's codes become bf16 or float32 with their page's scale (exact) on the way into LDS.
-// Two shapes: few rows (32): every wavefront has all of them and keys of its own, nothing is waited for together; more: the
-// four wavefronts share the keys and have 16 or 32 rows each.
+// Two kinds of shape: few rows (32): every wavefront has all of them and keys of its own, nothing is waited for together; more: four
+// or eight wavefronts share the keys, twice a tile's in LDS so that they meet once a tile, and have 16 or 32 rows each.
 #pragma once
 #include "ekv_attn8.h"
 
 namespace ekv {
 
 constexpr int kTreeMost = 64;                    // drafted rows of a sequence: bits of a mask
-constexpr int kTreeThreads = 256, kTreeWaves = 4;
 
 struct TreeArgs {
   const void* q; const void* k_pool; const void* v_pool; const float* k_scale; const float* v_scale;
-  const int32_t* block_table; const int32_t* seq_lens; const int32_t* page_idx; const int32_t* n_sel;      // page_idx null: every page
+  const int32_t* block_table; const int32_t* seq_lens; const int32_t* page_idx; const int32_t* n_sel;      // every page: page_idx null, n_sel seq_lens
   const void* k_new; const void* v_new; int64_t ks, vs;
   const int32_t* start; const uint64_t* visible;
   int B, Hq, Hkv, HkvPool, P, Mmax, cap, n_phys, N, most;
@@ -39,22 +38,37 @@ struct TreeArgs {
 
 // Drafted rows of a sequence: [first, first + count).
 struct TreeRows { int first, count; };
-__device__ __forceinline__ TreeRows tree_rows(const TreeArgs& A, int b) {
-  const int s0 = clampi(A.start[b], 0, A.N), s1 = clampi(A.start[b + 1], s0, A.N);
+__device__ __forceinline__ TreeRows tree_rows(const TreeArgs& A, int from, int to) {
+  const int s0 = clampi(from, 0, A.N), s1 = clampi(to, s0, A.N);
   return {s0, min(s1 - s0, A.most)};
 }
-// Positions of a list that may hold keys: all of the sequence's tokens, or the tokens of the selected pages.
-__device__ __forceinline__ int list_positions(const TreeArgs& A, int u) {
-  if (A.page_idx == nullptr) return (int)min((int64_t)max(A.seq_lens[u / A.L], 0), (int64_t)A.Mmax * A.P);
-  return clampi(A.n_sel[u], 0, A.cap) * A.P;
+__device__ __forceinline__ TreeRows tree_rows(const TreeArgs& A, int b) { return tree_rows(A, uniform_load(A.start + b), uniform_load(A.start + b + 1)); }
+// Positions of a list that may hold keys: all of the sequence's tokens, or the tokens of the selected pages.  n_sel[list_entry] says how many.
+__device__ __forceinline__ int list_entry(const TreeArgs& A, int u) { return A.page_idx == nullptr ? u / A.L : u; }
+__device__ __forceinline__ int list_positions(const TreeArgs& A, int entry) {
+  if (A.page_idx == nullptr) return (int)min((int64_t)max(entry, 0), (int64_t)A.Mmax * A.P);
+  return clampi(entry, 0, A.cap) * A.P;
 }
 // Steps of a list: tiles of `keys` positions and one for the drafted keys, for every block of `rows` rows; none without rows.
 __device__ __forceinline__ int tree_blocks(const TreeArgs& A, int count, int rows) { return (count * A.GL + rows - 1) / rows; }
-__device__ __forceinline__ int tree_steps(const TreeArgs& A, int u, int keys) { return (list_positions(A, u) + keys - 1) / keys + 1; }
-
 __device__ __forceinline__ int tree_unit_steps(const TreeArgs& A, int u, int keys, int rows) {
-  const int count = tree_rows(A, u / A.L).count;
-  return count > 0 ? tree_blocks(A, count, rows) * tree_steps(A, u, keys) : 0;
+  const int b = u / A.L, s0 = A.start[b], s1 = A.start[b + 1], entry = A.n_sel[list_entry(A, u)];      // one wait for all
+  const int count = tree_rows(A, s0, s1).count;
+  return count > 0 ? tree_blocks(A, count, rows) * ((list_positions(A, entry) + keys - 1) / keys + 1) : 0;
+}
+// A list: its sequence, its first query head, its KV head, rows, the sequence's tokens and the list's positions.  Scalar loads, waited for once.
+struct TreeList { int b, head, hkv, n, n_pos; TreeRows R; };
+__device__ __forceinline__ TreeList tree_list(const TreeArgs& A, int u) {
+  TreeList l;
+  l.b = u / A.L;
+  const int s0 = uniform_load(A.start + l.b), s1 = uniform_load(A.start + l.b + 1), n = uniform_load(A.seq_lens + l.b);
+  const int entry = uniform_load(A.n_sel + list_entry(A, u));
+  l.head = (u - l.b * A.L) * A.GL;
+  l.hkv = l.head / (A.Hq / A.Hkv);
+  l.R = tree_rows(A, s0, s1);
+  l.n = (int)min((int64_t)max(n, 0), (int64_t)A.Mmax * A.P);
+  l.n_pos = list_positions(A, entry);
+  return l;
 }
 
 typedef __attribute__((address_space(3))) char lds_char;
@@ -63,17 +77,19 @@ __device__ __forceinline__ s16x4_t read_transposed(const char* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_t __attribute__((address_space(3)))*)(lds_char*)p);
 }
 
-// How a workgroup of four wavefronts divides rows and keys.  TQ: type of queries and drafted rows, which the products have; TC: of the
-// cache.  NQ: tiles of 16 rows a wavefront, WQ: wavefronts that share the keys (1 or 4).  SIDES: K alone or K and V.
+// How a workgroup divides rows and keys.  TQ: type of queries and drafted rows, which the products have; TC: of the cache.  NQ: tiles of 16
+// rows a wavefront, WQ: wavefronts that share the keys (1: none of four; 4 or 8: all).  SIDES: K alone or K and V.
 template <typename TQ, typename TC, int NQ, int WQ, int SIDES> struct TreeShape {
-  static constexpr int kGroups = kTreeWaves / WQ;                        // groups of wavefronts with keys of their own
+  static constexpr int kWaves = WQ == 1 ? 4 : WQ, kWork = 64 * kWaves;   // of the workgroup
+  static constexpr int kGroups = kWaves / WQ;                            // groups of wavefronts with keys of their own
   static constexpr int kRows = 16 * NQ * WQ;                             // rows of a workgroup
-  static constexpr int kKeys = (WQ == 1 && SIDES == 2 ? 32 : 64) * 2 / (int)sizeof(TQ);   // keys of a tile
+  static constexpr int kKeys = (WQ == 1 ? 32 : 64) * 2 / (int)sizeof(TQ);       // keys of a tile
   static constexpr int kTiles = kKeys / 16;
   static constexpr int kRowBytes = kD * (int)sizeof(TQ);
   static constexpr int kSideBytes = kKeys * kRowBytes;
   static constexpr int kThreads = 64 * WQ;                               // that stage a tile
-  static constexpr int kLds = kGroups * SIDES * kSideBytes;
+  static constexpr int kTileBytes = SIDES * kSideBytes;
+  static constexpr int kLds = WQ == 1 ? kGroups * kTileBytes : 2 * kTileBytes;
 };
 // where 16-byte piece `piece` of row `row` lies
 template <typename TQ> __device__ __forceinline__ int tree_piece(int row, int piece) { return row * kD * (int)sizeof(TQ) + ((piece ^ (row & 15)) << 4); }
@@ -113,7 +129,8 @@ template <typename TQ, typename TC, int NQ, int WQ, int SIDES> struct TreeStage 
 #pragma unroll
       for (int s = 0; s < SIDES; ++s) {
         char* side = lds + s * S::kSideBytes;
-        const uint4 v = in ? raw[s][i] : make_uint4(0u, 0u, 0u, 0u);
+        const uint32_t keep = in ? ~0u : 0u;
+        const uint4 v = make_uint4(raw[s][i].x & keep, raw[s][i].y & keep, raw[s][i].z & keep, raw[s][i].w & keep);
         if constexpr (!kCodes) {
           *reinterpret_cast<uint4*>(side + tree_piece<TQ>(row, piece)) = v;
         } else if constexpr (sizeof(TQ) == 2) {
@@ -136,22 +153,18 @@ template <typename TQ, typename TC, int NQ, int WQ, int SIDES> struct TreeStage 
 
 // Lookups of a list's positions, a row of the tile per lane, in steps that are consumed a tile later each: page of the list, its
 // physical page, and then the data.
-struct TreeLook {
+template <bool LISTS> struct TreeLook {
   const TreeArgs* A; const int32_t* list; const int32_t* table;
   int P, n, n_pos, last, hkv;
-  __device__ __forceinline__ TreeLook(const TreeArgs& a, int u, int hkv_) : A(&a), hkv(hkv_) {
-    const int b = u / a.L;
-    P = a.P;
-    n = (int)min((int64_t)max(uniform_load(a.seq_lens + b), 0), (int64_t)a.Mmax * P);
-    n_pos = a.page_idx == nullptr ? n : clampi(uniform_load(a.n_sel + u), 0, a.cap) * P;
-    list = a.page_idx == nullptr ? nullptr : a.page_idx + (size_t)u * a.cap;
-    table = a.block_table + (size_t)b * a.Mmax;
-    last = (a.page_idx == nullptr ? a.Mmax : a.cap) * P - 1;
+  __device__ __forceinline__ TreeLook(const TreeArgs& a, int u, const TreeList& l) : A(&a), P(a.P), n(l.n), n_pos(l.n_pos), hkv(l.hkv) {
+    table = a.block_table + (size_t)l.b * a.Mmax;
+    list = LISTS ? a.page_idx + (size_t)u * a.cap : nullptr;
+    last = (LISTS ? a.cap : a.Mmax) * P - 1;
   }
   __device__ __forceinline__ int slot(int pos) const { return (int)page_div((uint32_t)min(pos, last), A->page_div); }
   __device__ __forceinline__ int page(int pos) const {
-    const int s = slot(pos);
-    return list == nullptr ? s : clampi(list[s], 0, A->Mmax - 1);
+    if constexpr (LISTS) return clampi(list[slot(pos)], 0, A->Mmax - 1);
+    else return slot(pos);
   }
   __device__ __forceinline__ int phys(int lp) const { return clampi(table[lp], 0, A->n_phys - 1); }
   __device__ __forceinline__ uint32_t row(int pos, int ph) const {
@@ -160,41 +173,110 @@ struct TreeLook {
   __device__ __forceinline__ bool valid(int pos, int lp) const { return pos < n_pos && (int64_t)lp * P + (pos - slot(pos) * P) < n; }
 };
 
+// A tile of drafted keys (and values): rows [d0, d0 + kKeys) of R, zeros behind the last.  The threads that stage a tile call it;
+// found(row, v): a piece of the values, to be changed where it has to be.
+template <typename TQ, typename S, int SIDES, typename F>
+__device__ __forceinline__ void stage_drafted(const TreeArgs& A, char* lds, int tid, const TreeRows& R, int hkv, int d0, F&& found) {
+  constexpr int kPieces = S::kRowBytes / 16, kTotal = S::kKeys * kPieces, kBatch = kTotal < 4 * S::kThreads ? kTotal / S::kThreads : 4;
+  static_assert(kTotal % (kBatch * S::kThreads) == 0, "whole batches");
+#pragma unroll 1
+  for (int i0 = 0; i0 < kTotal; i0 += kBatch * S::kThreads) {
+    uint4 k[kBatch], v[kBatch];
+    const bool any = d0 + i0 / kPieces < R.count;                          // the same for the threads
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      k[q] = v[q] = make_uint4(0u, 0u, 0u, 0u);
+      if (any) {
+        const int i = i0 + q * S::kThreads + tid, row = R.first + min(d0 + i / kPieces, R.count - 1);
+        k[q] = load16((const char*)((const TQ*)A.k_new + row * A.ks + hkv * kD) + 16 * (i % kPieces));
+        if constexpr (SIDES == 2) v[q] = load16((const char*)((const TQ*)A.v_new + row * A.vs + hkv * kD) + 16 * (i % kPieces));
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      const int i = i0 + q * S::kThreads + tid, row = i / kPieces, piece = i % kPieces;
+      const uint32_t keep = d0 + row < R.count ? ~0u : 0u;
+      k[q] = make_uint4(k[q].x & keep, k[q].y & keep, k[q].z & keep, k[q].w & keep);
+      *reinterpret_cast<uint4*>(lds + tree_piece<TQ>(row, piece)) = k[q];
+      if constexpr (SIDES == 2) {
+        v[q] = make_uint4(v[q].x & keep, v[q].y & keep, v[q].z & keep, v[q].w & keep);
+        found(row, v[q]);
+        *reinterpret_cast<uint4*>(lds + S::kSideBytes + tree_piece<TQ>(row, piece)) = v[q];
+      }
+    }
+  }
+}
+
 // Query operands of a wavefront's NQ tiles of rows: lane (c, j) has of row c of a tile channels 32 s + 8 j + 0..7 (bf16), 16 s + 4 j +
-// 0..3 (float32).  Rows behind the last one repeat it.
-template <typename TQ, int NQ> struct TreeQuery {
+// 0..3 (float32).  Rows behind the last one repeat it.  LDS: kept there, 16 bytes a lane side by side: two tiles of rows beside a whole tile of
+// keys and values under way make the kernel spill, and a spilled register read back waits for every load before it (112 -> 96 us
+// for softmax over lists of 4 x 128K tokens, 32 rows).
+template <typename TQ, int NQ, bool LDS> struct TreeQuery {
   static constexpr int kSteps = sizeof(TQ) == 2 ? 4 : 8;
-  uint4 v[NQ][kSteps];
-  __device__ __forceinline__ void load(const TreeArgs& A, const TreeRows& R, int list_head, int r0) {
+  static constexpr int kLds = LDS ? NQ * kSteps * 1024 : 16;             // of a wavefront
+  uint4 v[LDS ? 1 : NQ][kSteps];
+  char* lds;
+  __device__ __forceinline__ void load(const TreeArgs& A, const TreeRows& R, int list_head, int r0, char* to) {
     const int lane = threadIdx.x & 63, c = lane & 15, j = lane >> 4;
+    lds = to + 16 * lane;
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
       const int r = min(r0 + 16 * t + c, R.count * A.GL - 1), tok = r / A.GL;
       const TQ* row = (const TQ*)A.q + ((size_t)(R.first + tok) * A.Hq + list_head + (r - tok * A.GL)) * kD;
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) v[t][s] = *reinterpret_cast<const uint4*>(row + (sizeof(TQ) == 2 ? 32 * s + 8 * j : 16 * s + 4 * j));
+      for (int s = 0; s < kSteps; ++s) {
+        const uint4 x = *reinterpret_cast<const uint4*>(row + (sizeof(TQ) == 2 ? 32 * s + 8 * j : 16 * s + 4 * j));
+        if constexpr (LDS) *reinterpret_cast<uint4*>(lds + (t * kSteps + s) * 1024) = x;
+        else v[t][s] = x;
+      }
     }
+  }
+  __device__ __forceinline__ uint4 get(int t, int s) const {
+    if constexpr (LDS) return *reinterpret_cast<const uint4*>(lds + (t * kSteps + s) * 1024);
+    else return v[t][s];
   }
 };
 
-// S^T of sixteen keys (tile m of the LDS tile) and a wavefront's rows: lane (c, j) gets keys 4j..4j+3 of row c.
-template <typename TQ, int NQ>
-__device__ __forceinline__ void tree_scores(const char* k, int m, const TreeQuery<TQ, NQ>& q, f32x4_t (&d)[NQ]) {
+// S^T of M tiles of sixteen keys (from tile m0 of the LDS tile on) and a wavefront's rows: lane (c, j) gets keys 4j..4j+3 of row c.
+template <typename TQ, int NQ, int M, bool LDS>
+__device__ __forceinline__ void tree_scores(const char* k, int m0, const TreeQuery<TQ, NQ, LDS>& q, f32x4_t (&d)[M][NQ]) {
   const int lane = threadIdx.x & 63, c = lane & 15, j = lane >> 4;
+  constexpr int kSums = sizeof(TQ) == 2 ? 1 : 4;       // float32: a product has 4 of the 128 channels, four sums of 8 each round less
+  f32x4_t sum[kSums][M][NQ];
 #pragma unroll
-  for (int t = 0; t < NQ; ++t) d[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int s = 0; s < TreeQuery<TQ, NQ>::kSteps; ++s) {
-    const uint4 a = *reinterpret_cast<const uint4*>(k + tree_piece<TQ>(16 * m + c, 4 * s + j));
+  for (int m = 0; m < M; ++m) {
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
-      if constexpr (sizeof(TQ) == 2) {
-        d[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, q.v[t][s]), d[t], 0, 0, 0);
-      } else {
-        const f32x4_t x = __builtin_bit_cast(f32x4_t, a), y = __builtin_bit_cast(f32x4_t, q.v[t][s]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) d[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], d[t], 0, 0, 0);
+      for (int e = 0; e < kSums; ++e) sum[e][m][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < TreeQuery<TQ, NQ, LDS>::kSteps; ++s) {
+    uint4 row[NQ];
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) row[t] = q.get(t, s);
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      const uint4 a = *reinterpret_cast<const uint4*>(k + tree_piece<TQ>(16 * (m0 + m) + c, 4 * s + j));
+#pragma unroll
+      for (int t = 0; t < NQ; ++t) {
+        if constexpr (sizeof(TQ) == 2) {
+          sum[0][m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, row[t]), sum[0][m][t], 0, 0, 0);
+        } else {
+          const f32x4_t x = __builtin_bit_cast(f32x4_t, a), y = __builtin_bit_cast(f32x4_t, row[t]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[e][m][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], sum[e][m][t], 0, 0, 0);
+        }
       }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+      if constexpr (sizeof(TQ) == 2) d[m][t] = sum[0][m][t];
+      else d[m][t] = (sum[0][m][t] + sum[1][m][t]) + (sum[2][m][t] + sum[3][m][t]);
     }
   }
 }
@@ -206,10 +288,10 @@ __device__ __forceinline__ int tree_workgroup() {
 }
 
 // The work of a launch: the steps of all lists (for every block of `rows` rows its tiles of `keys` positions, and one step for the
-// drafted keys), in order, of which every workgroup takes an even, contiguous share; or, per_unit, a block of rows whole.  seg(unit, R,
+// drafted keys), in order, of which every workgroup takes an even, contiguous share; or, per_unit, a block of rows whole.  seg(wg, unit, list,
 // blk, st0, st1, steps, first) is called for every stretch [st0, st1) of a block's `steps`; first: the workgroup's first one.
 // pre_lds: dynamic LDS for the steps before a list.
-template <int ROWS, int KEYS, typename F>
+template <int THREADS, int ROWS, int KEYS, typename F>
 __device__ __forceinline__ void tree_work(const TreeArgs& A, int* pre_lds, int* wsum, F&& seg) {
   const bool in_lds = A.pre_g == nullptr;
   const int wg = A.per_unit ? (int)blockIdx.x : tree_workgroup();
@@ -222,15 +304,16 @@ __device__ __forceinline__ void tree_work(const TreeArgs& A, int* pre_lds, int* 
   };
   if (A.per_unit) {
     unit = wg / A.blocks;
-    const int steps = tree_steps(A, unit, KEYS), blk = wg - unit * A.blocks;
-    if (blk >= tree_blocks(A, tree_rows(A, unit / A.L).count, ROWS)) return;
+    const TreeList l = tree_list(A, unit);
+    const int steps = (l.n_pos + KEYS - 1) / KEYS + 1, blk = wg - unit * A.blocks;
+    if (blk >= tree_blocks(A, l.R.count, ROWS)) return;
     begin = blk * steps;
     end = begin + steps;
   } else if (in_lds) {
-    block_exclusive_prefix<kTreeThreads>(A.U, [&](int u) { return tree_unit_steps(A, u, KEYS, ROWS); }, pre_lds, wsum);
+    block_exclusive_prefix<THREADS>(A.U, [&](int u) { return tree_unit_steps(A, u, KEYS, ROWS); }, pre_lds, wsum);
     range((const int*)pre_lds);
     if (blockIdx.x == 0)
-      for (int u = threadIdx.x; u <= A.U; u += kTreeThreads) A.pre[u] = pre_lds[u];
+      for (int u = threadIdx.x; u <= A.U; u += THREADS) A.pre[u] = pre_lds[u];
   } else {
     range(A.pre_g);
   }
@@ -243,10 +326,10 @@ __device__ __forceinline__ void tree_work(const TreeArgs& A, int* pre_lds, int* 
     if (A.per_unit) u_end = end;
     else if (in_lds) bounds((const int*)pre_lds);
     else bounds(A.pre_g);
-    const TreeRows R = tree_rows(A, unit / A.L);
-    const int steps = tree_steps(A, unit, KEYS), blk = (at - u_begin) / steps, blk_begin = u_begin + blk * steps;
+    const TreeList l = tree_list(A, unit);
+    const int steps = (l.n_pos + KEYS - 1) / KEYS + 1, blk = (at - u_begin) / steps, blk_begin = u_begin + blk * steps;
     const int seg_end = min(min(end, u_end), blk_begin + steps);
-    seg(wg, unit, R, blk, at - blk_begin, seg_end - blk_begin, steps, at == begin);
+    seg(wg, unit, l, blk, at - blk_begin, seg_end - blk_begin, steps, at == begin);
     at = seg_end;
   }
 }

@@ -9,23 +9,26 @@ namespace ekv {
 
 constexpr int kGroup = 64;                       // keys per maximum
 
-template <typename TQ, typename TC, int NQ, int WQ>
-__global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2)))
+template <typename TQ, typename TC, int NQ, int WQ, bool LISTS>
+__global__ __launch_bounds__(64 * (WQ == 1 ? 4 : WQ)) __attribute__((amdgpu_waves_per_eu(WQ == 1 ? 3 : 2)))
 void tree_scores_kernel(const TreeArgs A) {
   using S = TreeShape<TQ, TC, NQ, WQ, 1>;
   constexpr int kPer = kGroup / S::kKeys;        // tiles of a group
   extern __shared__ int pre_lds[];
   __shared__ __attribute__((aligned(16))) char s_tile[S::kLds];
-  __shared__ int wsum[kTreeWaves];
+  using Q = TreeQuery<TQ, NQ, WQ == 1 && NQ == 2>;
+  __shared__ __attribute__((aligned(16))) char s_q[Q::kLds];               // all wavefronts have the same rows
+  __shared__ int wsum[S::kWaves];
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), c = lane & 15, j = lane >> 4;
   const int grp = WQ == 1 ? w : 0, tid = WQ == 1 ? lane : threadIdx.x;
-  char* tile = s_tile + grp * S::kSideBytes;
-  tree_work<S::kRows, kGroup>(A, pre_lds, wsum, [&](int wg, int unit, const TreeRows& R, int blk, int st0, int st1, int steps, bool) {
-    const int b = unit / A.L, list = unit - b * A.L, list_head = list * A.GL, hkv = list_head / (A.Hq / A.Hkv);
-    const int g0 = min(st0, steps - 1), g1 = min(st1, steps - 1), n_rows = R.count * A.GL;
-    const int r0 = blk * S::kRows + (WQ == 4 ? w * 16 * NQ : 0);
-    TreeQuery<TQ, NQ> q;
-    q.load(A, R, list_head, r0);
+  char* tile = s_tile + grp * S::kTileBytes;
+  tree_work<S::kWork, S::kRows, kGroup>(A, pre_lds, wsum, [&](int, int unit, const TreeList& list, int blk, int st0, int st1, int steps, bool) {
+    const TreeRows R = list.R;
+    const int list_head = list.head, hkv = list.hkv;
+    const int n_rows = R.count * A.GL;
+    const int r0 = blk * S::kRows + (WQ > 1 ? w * 16 * NQ : 0);
+    Q q;
+    q.load(A, R, list_head, r0, s_q);
     float* z[NQ]; float* zmax[NQ];
     bool there[NQ];
 #pragma unroll
@@ -36,8 +39,9 @@ void tree_scores_kernel(const TreeArgs A) {
       z[t] = A.z + at * A.zstride + 4 * j;
       zmax[t] = A.zmax + at * A.n_groups;
     }
-    const int n_g = g1 - g0, t0 = (g0 + n_g * grp / S::kGroups) * kPer, t1 = (g0 + n_g * (grp + 1) / S::kGroups) * kPer;
-    const TreeLook look(A, unit, hkv);
+    // a group's share of the steps, as tiles of the cache (the drafted keys are the last one's)
+    const int n_g = st1 - st0, t0 = min(st0 + n_g * grp / S::kGroups, steps - 1) * kPer, t1 = min(st0 + n_g * (grp + 1) / S::kGroups, steps - 1) * kPer;
+    const TreeLook<LISTS> look(A, unit, list);
     const int row = lane % S::kKeys;
     auto pos_of = [&](int t) { return min(t, t1 - 1) * S::kKeys + row; };
     TreeStage<TQ, TC, NQ, WQ, 1> stage;
@@ -55,76 +59,101 @@ void tree_scores_kernel(const TreeArgs A) {
       ph1 = look.phys(lp1);
       fetch(t0, lp0, ph0);
     }
-    const bool drafted = st1 == steps && (WQ == 4 || w == kTreeWaves - 1);
-    const int t2 = drafted ? t1 + kPer : t1;
     float top[NQ];
-    for (int t = t0; t < t2; ++t) {
-      const bool cached = t < t1;
-      uint64_t seen[NQ];
-      bool all = false;
-      if constexpr (WQ == 4) __syncthreads(); else wave_order();           // the tile before is read
-      if (cached) {
-        const uint64_t valid = valid_next;
-        stage.commit(tile, tid, valid);
-        const int ph2 = look.phys(lp2), lp3 = look.page(pos_of(t + 3));
-        fetch(t + 1, lp1, ph1);
-        lp1 = lp2; ph1 = ph2; lp2 = lp3;
+    // scores of the LDS tile to places from `to` on of the rows' scores, and into the maxima
+    auto score = [&](const char* k, size_t to, auto drafted, uint64_t valid, const uint64_t (&seen)[NQ]) {
+      constexpr bool kDrafted = decltype(drafted)::value != 0;
+      constexpr uint64_t full = S::kKeys == 64 ? ~0ull : (1ull << (S::kKeys & 63)) - 1;
+      f32x4_t d[S::kTiles][NQ];
+      tree_scores<TQ, NQ, S::kTiles>(k, 0, q, d);
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) seen[i] = valid;
-        constexpr uint64_t full = S::kKeys == 64 ? ~0ull : (1ull << (S::kKeys & 63)) - 1;
-        all = (valid & full) == full;
-      } else {
-        constexpr int pieces = S::kRowBytes / 16;
-        const int d0 = (t - t1) * S::kKeys;
-#pragma unroll 1
-        for (int i = tid; i < S::kKeys * pieces; i += S::kThreads) {
-          const int key_row = i / pieces, piece = i % pieces, key = d0 + key_row;
-          const int kc = R.first + min(key, R.count - 1);
-          uint4 kv = load16((const char*)((const TQ*)A.k_new + kc * A.ks + hkv * kD) + 16 * piece);
-          if (key >= R.count) kv = make_uint4(0u, 0u, 0u, 0u);
-          *reinterpret_cast<uint4*>(tile + tree_piece<TQ>(key_row, piece)) = kv;
+      for (int i = 0; i < NQ; ++i) {
+#pragma unroll
+        for (int m = 0; m < S::kTiles; ++m) {
+          d[m][i] *= A.zscale;
+          if (kDrafted || (valid & full) != full) {
+            const uint32_t bits = (uint32_t)((kDrafted ? seen[i] : valid) >> (16 * m + 4 * j));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[m][i][e] = bits >> e & 1 ? d[m][i][e] : -INFINITY;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top[i] = fmaxf(top[i], d[m][i][e]);
         }
+        if (there[i]) {
+#pragma unroll
+          for (int m = 0; m < S::kTiles; ++m) *reinterpret_cast<f32x4_t*>(z[i] + to + 16 * m) = d[m][i];
+        }
+      }
+    };
+    auto clear_top = [&]() {
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) top[i] = -INFINITY;
+    };
+    auto store_top = [&](int group) {
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        float x = fmaxf(top[i], __shfl_xor(top[i], 16));
+        x = fmaxf(x, __shfl_xor(x, 32));
+        if (j == 0 && there[i]) zmax[i][group] = x;
+      }
+    };
+    const uint64_t none[NQ] = {};
+    auto ahead = [&](int t) {                              // tile t's data under way, the lookups of the two behind it
+      const int ph2 = look.phys(lp2), lp3 = look.page(pos_of(t + 2));
+      fetch(t, lp1, ph1);
+      lp1 = lp2; ph1 = ph2; lp2 = lp3;
+    };
+    auto work = [&](const char* k, int t, uint64_t valid) {
+      if (kPer == 1 || t % kPer == 0) clear_top();
+      score(k, (size_t)t * S::kKeys, IntC<0>{}, valid, none);
+      if (kPer == 1 || t % kPer == kPer - 1) store_top(t / kPer);
+    };
+    if constexpr (WQ == 1) {
+      for (int t = t0; t < t1; ++t) {
+        const uint64_t valid = valid_next;
+        wave_order();                                      // the tile before is read
+        stage.commit(tile, tid, valid);
+        ahead(t + 1);
+        wave_order();
+        work(tile, t, valid);
+      }
+    } else if (t0 < t1) {
+      // tile t + 1 goes to the half of LDS that nobody reads while tile t is worked on: one meeting a tile
+      __syncthreads();                                     // the last list's tiles are read
+      uint64_t valid = valid_next;
+      stage.commit(tile, tid, valid);
+      ahead(t0 + 1);
+      for (int t = t0; t < t1; ++t) {
+        __syncthreads();
+        const uint64_t after = valid_next;
+        if (t + 1 < t1) stage.commit(tile + ((t + 1 - t0) & 1) * S::kTileBytes, tid, after);
+        ahead(t + 2);
+        work(tile + ((t - t0) & 1) * S::kTileBytes, t, valid);
+        valid = after;
+      }
+    }
+    // the drafted keys, the list's last step; keys behind the last have no score, and nobody reads one
+    if (st1 == steps && (WQ > 1 || w == S::kWaves - 1)) {
+      clear_top();
+#pragma unroll 1
+      for (int d0 = 0; d0 < R.count; d0 += S::kKeys) {
+        if constexpr (WQ > 1) __syncthreads(); else wave_order();
+        stage_drafted<TQ, S, 1>(A, tile, tid, R, hkv, d0, [](int, uint4&) {});
         const int left = R.count - d0;
-        const uint64_t there_keys = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0;
+        const uint64_t there_keys = left >= 64 ? ~0ull : (1ull << left) - 1;
+        uint64_t seen[NQ];
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
           const int r = min(r0 + 16 * i + c, n_rows - 1);
           seen[i] = (A.visible[R.first + r / A.GL] >> d0) & there_keys;
         }
+        if constexpr (WQ > 1) __syncthreads(); else wave_order();
+        score(tile, (size_t)(steps - 1) * kGroup + d0, IntC<1>{}, 0, seen);
       }
-      if constexpr (WQ == 4) __syncthreads(); else wave_order();
-      if (kPer == 1 || t % kPer == 0) {
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) top[i] = -INFINITY;
-      }
-      const int group = cached ? t / kPer : steps - 1, sub = kPer == 1 ? 0 : t % kPer * S::kKeys;
-#pragma unroll
-      for (int m = 0; m < S::kTiles; ++m) {
-        f32x4_t d[NQ];
-        tree_scores<TQ, NQ>(tile, m, q, d);
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-          d[i] *= A.zscale;
-          if (!all) {
-            const uint32_t bits = (uint32_t)(seen[i] >> (16 * m + 4 * j));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) d[i][e] = bits >> e & 1 ? d[i][e] : -INFINITY;
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) top[i] = fmaxf(top[i], d[i][e]);
-          if (there[i]) *reinterpret_cast<f32x4_t*>(z[i] + (size_t)group * kGroup + sub + 16 * m) = d[i];
-        }
-      }
-      if (kPer == 1 || t % kPer == kPer - 1) {
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-          float x = fmaxf(top[i], __shfl_xor(top[i], 16));
-          x = fmaxf(x, __shfl_xor(x, 32));
-          if (j == 0 && there[i]) zmax[i][group] = x;
-        }
-      }
+      store_top(steps - 1);
     }
-    if constexpr (WQ == 1) wave_order();
+    if constexpr (WQ == 1 && NQ == 2) __syncthreads();     // the queries are read
+    else if constexpr (WQ == 1) wave_order();
   });
 }
 
@@ -134,7 +163,7 @@ constexpr int kScoreWgs = 1024;
 static int score_rows(const Dims& dm, int list_rows) {
   if (list_rows <= 16) return 16;
   if (dm.dtype == EKV_F32) return 64;
-  return list_rows <= 32 ? 32 : list_rows <= 64 ? 64 : 128;
+  return list_rows <= 32 ? 32 : list_rows <= 64 ? 64 : list_rows <= 128 ? 128 : 256;
 }
 static long long score_steps(const Dims& dm, bool dense, int lists, int list_rows) {
   const int rows = score_rows(dm, list_rows);
@@ -154,16 +183,16 @@ size_t tree_entmax_ws_bytes(const Dims& dm, bool dense, int lists, int n_tokens)
 
 template <typename TQ, typename TC, int NQ, int WQ>
 static void launch_scores_shape(const TreeArgs& a, size_t lds, hipStream_t st) {
-  hipLaunchKernelGGL((tree_scores_kernel<TQ, TC, NQ, WQ>), dim3(a.W), dim3(kTreeThreads), lds, st, a);
+  if (a.page_idx != nullptr) hipLaunchKernelGGL((tree_scores_kernel<TQ, TC, NQ, WQ, true>), dim3(a.W), dim3(64 * (WQ == 1 ? 4 : WQ)), lds, st, a);
+  else hipLaunchKernelGGL((tree_scores_kernel<TQ, TC, NQ, WQ, false>), dim3(a.W), dim3(64 * (WQ == 1 ? 4 : WQ)), lds, st, a);
 }
 template <typename TQ, typename TC>
 static void launch_scores_T(const Dims& dm, TreeArgs& a, hipStream_t st) {
   const int list_rows = a.most * a.GL, rows = score_rows(dm, list_rows);
   a.blocks = (list_rows + rows - 1) / rows;
   const long long steps = score_steps(dm, a.page_idx == nullptr, a.L, list_rows);
-  const int share = rows <= 32 ? kTreeWaves : 1, most = 2 * device_compute_units();
-  const long long wgs = (steps + share - 1) / share;
-  a.W = (int)(wgs < most ? wgs : most);
+  const int most = (rows == 256 ? 1 : rows <= 32 ? 3 : 2) * device_compute_units();
+  a.W = (int)(steps < most ? steps : most);
   size_t lds = 0;
   if (a.U > kUnitsLdsMax) {
     launch_tree_prefix(a, kGroup, rows, st);
@@ -175,7 +204,8 @@ static void launch_scores_T(const Dims& dm, TreeArgs& a, hipStream_t st) {
   else if (rows == 64) launch_scores_shape<TQ, TC, 1, 4>(a, lds, st);
   if constexpr (sizeof(TQ) == 2) {
     if (rows == 32) launch_scores_shape<TQ, TC, 2, 1>(a, lds, st);
-    else if (rows == 128) launch_scores_shape<TQ, TC, 2, 4>(a, lds, st);
+    else if (rows == 128) launch_scores_shape<TQ, TC, 1, 8>(a, lds, st);
+    else if (rows == 256) launch_scores_shape<TQ, TC, 2, 8>(a, lds, st);
   }
 }
 

@@ -32,43 +32,39 @@ template <typename TQ, int NQ, int TILES> struct TreeSoftmax {
       for (int i = 0; i < 8; ++i) o[t][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
   }
-  // One LDS tile.  all: every key counts; else seen[t] has bit i for the tile's key i, of the lane's row.  bad: keys whose values are added
-  // by themselves, from v_bad.
-  __device__ __forceinline__ void add(const char* k, const char* v, const TreeQuery<TQ, NQ>& q, float zscale, bool all,
+  // One LDS tile of the cache (bit i of valid: key i counts) or of drafted keys (bit i of seen[t]: for the lane's row of tile t).  bad: drafted
+  // keys whose values are added by themselves, from v_bad.
+  template <bool DRAFTED, typename Q>
+  __device__ __forceinline__ void add(const char* k, const char* v, const Q& q, float zscale, uint64_t valid,
                                       const uint64_t (&seen)[NQ], uint64_t bad, const TQ* v_bad, int64_t v_stride) {
     const int lane = threadIdx.x & 63, c = lane & 15, j = lane >> 4;
+    constexpr uint64_t full = TILES == 4 ? ~0ull : (1ull << (16 * TILES & 63)) - 1;
     f32x4_t p[TILES][NQ];
-    bool higher = false;
-    float top[NQ];
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) top[t] = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < TILES; ++i) {
-      tree_scores<TQ, NQ>(k, i, q, p[i]);
-#pragma unroll
-      for (int t = 0; t < NQ; ++t) p[i][t] *= zscale;
-    }
-    if (!all) {
+    tree_scores<TQ, NQ, TILES>(k, 0, q, p);
+    if (DRAFTED || (valid & full) != full) {
 #pragma unroll
       for (int i = 0; i < TILES; ++i) {
 #pragma unroll
         for (int t = 0; t < NQ; ++t) {
-          const uint32_t bits = (uint32_t)(seen[t] >> (16 * i + 4 * j));
+          const uint32_t bits = (uint32_t)((DRAFTED ? seen[t] : valid) >> (16 * i + 4 * j));
 #pragma unroll
           for (int e = 0; e < 4; ++e) p[i][t][e] = bits >> e & 1 ? p[i][t][e] : -INFINITY;
         }
       }
     }
+    float top[NQ];
+    bool higher = false;
 #pragma unroll
-    for (int i = 0; i < TILES; ++i) {
+    for (int t = 0; t < NQ; ++t) {
+      top[t] = -INFINITY;
 #pragma unroll
-      for (int t = 0; t < NQ; ++t) {
+      for (int i = 0; i < TILES; ++i) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) top[t] = fmaxf(top[t], p[i][t][e]);
       }
+      top[t] *= zscale;
+      higher |= top[t] > m[t] + kSlack;
     }
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) higher |= top[t] > m[t] + kSlack;
     if (__any(higher)) {
 #pragma unroll
       for (int t = 0; t < NQ; ++t) {
@@ -81,19 +77,24 @@ template <typename TQ, int NQ, int TILES> struct TreeSoftmax {
         for (int i = 0; i < 8; ++i) o[t][i] *= f;
       }
     }
+    // weights of key tiles i0..i1-1 in the scores' place
+    auto weigh = [&](int i0, int i1) {
 #pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-      const float base = m[t] > -INFINITY ? m[t] : 0.f;
+      for (int t = 0; t < NQ; ++t) {
+        const float base = m[t] > -INFINITY ? -m[t] : 0.f;
 #pragma unroll
-      for (int i = 0; i < TILES; ++i) {
+        for (int i = 0; i < TILES; ++i) {
+          if (i < i0 || i >= i1) continue;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[i][t][e] = __builtin_amdgcn_exp2f(p[i][t][e] - base);
-          l[t] += p[i][t][e];
+          for (int e = 0; e < 4; ++e) {
+            p[i][t][e] = __builtin_amdgcn_exp2f(fmaf(p[i][t][e], zscale, base));
+            l[t] += p[i][t][e];
+          }
         }
       }
-    }
-    if (bad != 0) {
+    };
+    if constexpr (DRAFTED) weigh(0, TILES);
+    if (DRAFTED && bad != 0) {
       for (uint64_t left = bad; left != 0; left &= left - 1) {
         const int key = __builtin_ctzll(left);
         const TQ* row = v_bad + (int64_t)key * v_stride + 4 * j;
@@ -134,9 +135,10 @@ template <typename TQ, int NQ, int TILES> struct TreeSoftmax {
       }
     }
     if constexpr (sizeof(TQ) == 2) {
-#pragma unroll
-      for (int i = 0; i < TILES; i += 2) {       // 32 keys: lane group j has keys 4j..4j+3 of either tile
-        bf16x8_t w[3][NQ];
+      // 32 keys at a time (lane group j has keys 4j..4j+3 of either tile); the next 32 keys' weights are computed while these are multiplied
+      bf16x8_t w[3][NQ];
+      auto terms = [&](int i) {
+        if constexpr (!DRAFTED) weigh(i, i + 2);
 #pragma unroll
         for (int t = 0; t < NQ; ++t) {
           float x[8];
@@ -154,20 +156,41 @@ template <typename TQ, int NQ, int TILES> struct TreeSoftmax {
             }
           }
         }
+      };
+      terms(0);
 #pragma unroll
-        for (int ch = 0; ch < 8; ++ch) {
-          const int row = 16 * i + 4 * j + (c >> 2), piece = 2 * ch + ((c & 3) >> 1), half = (c & 1) * 8;
-          const s16x4_t a0 = read_transposed(v + tree_piece<TQ>(row, piece) + half), a1 = read_transposed(v + tree_piece<TQ>(row + 16, piece) + half);
-          const bf16x8_t a = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+      for (int i = 0; i < TILES; i += 2) {
+        // a sum's terms are apart from each other: 2 (4) channels' by the rows' tiles between them
+        constexpr int CH = NQ == 1 ? 4 : 2;
+        bf16x8_t now[3][NQ];
 #pragma unroll
-          for (int t = 0; t < NQ; ++t) {
+        for (int term = 0; term < 3; ++term) {
 #pragma unroll
-            for (int term = 2; term >= 0; --term)          // the smallest terms first
-              o[t][ch] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[term][t], o[t][ch], 0, 0, 0);
+          for (int t = 0; t < NQ; ++t) now[term][t] = w[term][t];
+        }
+        if (i + 2 < TILES) terms(i + 2);
+#pragma unroll
+        for (int ch = 0; ch < 8; ch += CH) {
+          bf16x8_t a[CH];
+#pragma unroll
+          for (int h = 0; h < CH; ++h) {
+            const int row = 16 * i + 4 * j + (c >> 2), piece = 2 * (ch + h) + ((c & 3) >> 1), half = (c & 1) * 8;
+            const s16x4_t a0 = read_transposed(v + tree_piece<TQ>(row, piece) + half), a1 = read_transposed(v + tree_piece<TQ>(row + 16, piece) + half);
+            a[h] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+          }
+#pragma unroll
+          for (int term = 2; term >= 0; --term) {                          // the smallest terms first
+#pragma unroll
+            for (int h = 0; h < CH; ++h) {
+#pragma unroll
+              for (int t = 0; t < NQ; ++t)
+                o[t][ch + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[h], now[term][t], o[t][ch + h], 0, 0, 0);
+            }
           }
         }
       }
     } else {
+      if constexpr (!DRAFTED) weigh(0, TILES);
 #pragma unroll
       for (int i = 0; i < TILES; ++i) {
 #pragma unroll
@@ -195,32 +218,35 @@ template <typename TQ> __device__ __forceinline__ bool has_no_number(const uint4
   return no;
 }
 
-template <typename TQ, typename TC, int NQ, int WQ>
-__global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2)))
+template <typename TQ, typename TC, int NQ, int WQ, bool LISTS>
+__global__ __launch_bounds__(64 * (WQ == 1 ? 4 : WQ)) __attribute__((amdgpu_waves_per_eu(2)))
 void tree_softmax_kernel(const TreeArgs A) {
   using S = TreeShape<TQ, TC, NQ, WQ, 2>;
   extern __shared__ int pre_lds[];
   __shared__ __attribute__((aligned(16))) char s_tile[S::kLds];
+  using Q = TreeQuery<TQ, NQ, WQ == 1 && NQ == 2>;
+  __shared__ __attribute__((aligned(16))) char s_q[Q::kLds];               // all wavefronts have the same rows
   __shared__ uint32_t s_bad[S::kGroups][2];
-  __shared__ int wsum[kTreeWaves];
+  __shared__ int wsum[S::kWaves];
   constexpr int RS = kD + 4;                     // floats between rows of partial outputs in LDS
-  static_assert(WQ == 4 || NQ * 16 * RS * 4 * 2 <= S::kLds, "two wavefronts' partial outputs take the tiles' place");
-  __shared__ float s_m[kTreeWaves][16 * NQ], s_l[kTreeWaves][16 * NQ];
+  static_assert(WQ > 1 || NQ * 16 * RS * 4 * 2 <= S::kLds, "two wavefronts' partial outputs take the tiles' place");
+  __shared__ float s_m[S::kWaves][16 * NQ], s_l[S::kWaves][16 * NQ];
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), c = lane & 15, j = lane >> 4;
   const int grp = WQ == 1 ? w : 0, tid = WQ == 1 ? lane : threadIdx.x;
-  char* tile = s_tile + grp * 2 * S::kSideBytes;
-  tree_work<S::kRows, S::kKeys>(A, pre_lds, wsum, [&](int wg, int unit, const TreeRows& R, int blk, int st0, int st1, int steps, bool first) {
-    const int b = unit / A.L, list = unit - b * A.L, list_head = list * A.GL, hkv = list_head / (A.Hq / A.Hkv);
+  char* tile = s_tile + grp * S::kTileBytes;
+  tree_work<S::kWork, S::kRows, S::kKeys>(A, pre_lds, wsum, [&](int wg, int unit, const TreeList& list, int blk, int st0, int st1, int steps, bool first) {
+    const TreeRows R = list.R;
+    const int list_head = list.head, hkv = list.hkv;
     const int tiles0 = min(st0, steps - 1), tiles1 = min(st1, steps - 1);          // the steps' tiles of the cache
     const bool drafted = st1 == steps;
-    const int r0 = blk * S::kRows + (WQ == 4 ? w * 16 * NQ : 0);         // the wavefront's first row
-    TreeQuery<TQ, NQ> q;
-    q.load(A, R, list_head, r0);
+    const int r0 = blk * S::kRows + (WQ > 1 ? w * 16 * NQ : 0);         // the wavefront's first row
+    Q q;
+    q.load(A, R, list_head, r0, s_q);
     TreeSoftmax<TQ, NQ, S::kTiles> acc;
     acc.clear();
     // a group's share of the tiles
     const int n_t = tiles1 - tiles0, t0 = tiles0 + n_t * grp / S::kGroups, t1 = tiles0 + n_t * (grp + 1) / S::kGroups;
-    const TreeLook look(A, unit, hkv);
+    const TreeLook<LISTS> look(A, unit, list);
     const int row = lane % S::kKeys;
     auto pos_of = [&](int t) { return min(t, t1 - 1) * S::kKeys + row; };
     TreeStage<TQ, TC, NQ, WQ, 2> stage;
@@ -238,56 +264,61 @@ void tree_softmax_kernel(const TreeArgs A) {
       ph1 = look.phys(lp1);
       fetch(t0, lp0, ph0);
     }
-    // after the cache's tiles the drafted keys', which the groups take in turn
-    int d0 = WQ == 1 ? grp * S::kKeys : 0;
-    for (int t = t0; t < t1 || (drafted && d0 < R.count); ++t) {
-      const bool cached = t < t1;
-      uint64_t seen[NQ], bad = 0;
-      bool all = false;
-      const TQ* v_bad = nullptr;
-      if constexpr (WQ == 4) __syncthreads(); else wave_order();           // the tile before is read
-      if (cached) {
+    const uint64_t none[NQ] = {};
+    auto ahead = [&](int t) {                              // tile t's data under way, the lookups of the two behind it
+      const int ph2 = look.phys(lp2), lp3 = look.page(pos_of(t + 2));
+      fetch(t, lp1, ph1);
+      lp1 = lp2; ph1 = ph2; lp2 = lp3;
+    };
+    if constexpr (WQ == 1) {
+      for (int t = t0; t < t1; ++t) {
         const uint64_t valid = valid_next;
+        wave_order();                                      // the tile before is read
         stage.commit(tile, tid, valid);
-        const int ph2 = look.phys(lp2), lp3 = look.page(pos_of(t + 3));
-        fetch(t + 1, lp1, ph1);
-        lp1 = lp2; ph1 = ph2; lp2 = lp3;
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) seen[i] = valid;
-        constexpr uint64_t full = S::kKeys == 64 ? ~0ull : (1ull << (S::kKeys & 63)) - 1;
-        all = (valid & full) == full;
-      } else {
-        if (tid < 2) s_bad[grp][tid] = 0;
-        if constexpr (WQ == 4) __syncthreads(); else wave_order();
-        constexpr int pieces = S::kRowBytes / 16;
+        ahead(t + 1);
+        wave_order();
+        acc.template add<false>(tile, tile + S::kSideBytes, q, A.zscale, valid, none, 0, nullptr, 0);
+      }
+    } else if (t0 < t1) {
+      // tile t + 1 goes to the half of LDS that nobody reads while tile t is worked on: one meeting a tile
+      __syncthreads();                                     // the last list's tiles are read
+      uint64_t valid = valid_next;
+      stage.commit(tile, tid, valid);
+      ahead(t0 + 1);
+      for (int t = t0; t < t1; ++t) {
+        char* now = tile + ((t - t0) & 1) * S::kTileBytes;
+        __syncthreads();
+        const uint64_t after = valid_next;
+        if (t + 1 < t1) stage.commit(tile + ((t + 1 - t0) & 1) * S::kTileBytes, tid, after);
+        ahead(t + 2);
+        acc.template add<false>(now, now + S::kSideBytes, q, A.zscale, valid, none, 0, nullptr, 0);
+        valid = after;
+      }
+    }
+    // the drafted keys, whose tiles the groups take in turn
+    if (drafted) {
 #pragma unroll 1
-        for (int i = tid; i < S::kKeys * pieces; i += S::kThreads) {
-          const int key_row = i / pieces, piece = i % pieces, key = d0 + key_row;
-          const bool in = key < R.count;
-          const int kc = R.first + min(key, R.count - 1);
-          uint4 kv = load16((const char*)((const TQ*)A.k_new + kc * A.ks + hkv * kD) + 16 * piece);
-          uint4 vv = load16((const char*)((const TQ*)A.v_new + kc * A.vs + hkv * kD) + 16 * piece);
-          const bool no = has_no_number<TQ>(vv);
-          if (in && no) atomicOr(&s_bad[grp][key_row >> 5], 1u << (key_row & 31));
-          if (!in) kv = make_uint4(0u, 0u, 0u, 0u);
-          if (!in || no) vv = make_uint4(0u, 0u, 0u, 0u);
-          *reinterpret_cast<uint4*>(tile + tree_piece<TQ>(key_row, piece)) = kv;
-          *reinterpret_cast<uint4*>(tile + S::kSideBytes + tree_piece<TQ>(key_row, piece)) = vv;
-        }
+      for (int d0 = WQ == 1 ? grp * S::kKeys : 0; d0 < R.count; d0 += S::kGroups * S::kKeys) {
+        if constexpr (WQ > 1) __syncthreads(); else wave_order();
+        if (tid < 2) s_bad[grp][tid] = 0;
+        if constexpr (WQ > 1) __syncthreads(); else wave_order();
+        stage_drafted<TQ, S, 2>(A, tile, tid, R, hkv, d0, [&](int key_row, uint4& v) {
+          if (has_no_number<TQ>(v)) {
+            atomicOr(&s_bad[grp][key_row >> 5], 1u << (key_row & 31));
+            v = make_uint4(0u, 0u, 0u, 0u);
+          }
+        });
         const uint64_t there = R.count - d0 >= 64 ? ~0ull : (1ull << (R.count - d0)) - 1;
+        uint64_t seen[NQ];
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
           const int r = min(r0 + 16 * i + c, R.count * A.GL - 1);
           seen[i] = (A.visible[R.first + r / A.GL] >> d0) & there;
         }
-        v_bad = (const TQ*)A.v_new + (int64_t)(R.first + d0) * A.vs + hkv * kD;
+        if constexpr (WQ > 1) __syncthreads(); else wave_order();
+        const uint64_t bad = (uint64_t)(uint32_t)uniform((int)s_bad[grp][0]) | (uint64_t)(uint32_t)uniform((int)s_bad[grp][1]) << 32;
+        acc.template add<true>(tile, tile + S::kSideBytes, q, A.zscale, 0, seen, bad, (const TQ*)A.v_new + (int64_t)(R.first + d0) * A.vs + hkv * kD, A.vs);
       }
-      if constexpr (WQ == 4) __syncthreads(); else wave_order();
-      if (!cached) {
-        bad = (uint64_t)(uint32_t)uniform((int)s_bad[grp][0]) | (uint64_t)(uint32_t)uniform((int)s_bad[grp][1]) << 32;
-        d0 += S::kGroups * S::kKeys;
-      }
-      acc.add(tile, tile + S::kSideBytes, q, A.zscale, all, seen, bad, v_bad, A.vs);
     }
     // the rows' sums
 #pragma unroll
@@ -311,7 +342,7 @@ void tree_softmax_kernel(const TreeArgs A) {
         if (ch == 0) *reinterpret_cast<float2*>(rec + (size_t)S::kRows * kD + 2 * r) = make_float2(m, l);
       }
     };
-    if constexpr (WQ == 4) {
+    if constexpr (WQ > 1) {
 #pragma unroll
       for (int t = 0; t < NQ; ++t) {
 #pragma unroll
@@ -333,7 +364,7 @@ void tree_softmax_kernel(const TreeArgs A) {
         f[t] = acc.m[t] > -INFINITY ? __builtin_amdgcn_exp2f(acc.m[t] - M[t]) : 0.f;
         Ls[t] = 0.f;
 #pragma unroll
-        for (int i = 0; i < kTreeWaves; ++i) {
+        for (int i = 0; i < S::kWaves; ++i) {
           const float mi = s_m[i][16 * t + c];
           Ls[t] = fmaf(s_l[i][16 * t + c], mi > -INFINITY ? __builtin_amdgcn_exp2f(mi - M[t]) : 0.f, Ls[t]);
         }
@@ -377,10 +408,11 @@ void tree_softmax_kernel(const TreeArgs A) {
 __global__ __launch_bounds__(256) void tree_join_kernel(const TreeArgs A, int rows, int keys) {
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
   const int most = A.most * A.GL, per = (most + 3) / 4;
-  const int unit = (int)(blockIdx.x / (unsigned)per), r = (int)(blockIdx.x % (unsigned)per) * 4 + w, b = unit / A.L;
-  const TreeRows R = tree_rows(A, b);
+  const int unit = (int)(blockIdx.x / (unsigned)per), r = (int)(blockIdx.x % (unsigned)per) * 4 + w;
+  const TreeList l = tree_list(A, unit);
+  const TreeRows R = l.R;
   if (r >= R.count * A.GL) return;
-  const int blk = r / rows, steps = tree_steps(A, unit, keys);
+  const int blk = r / rows, steps = (l.n_pos + keys - 1) / keys + 1;
   const int total = A.pre[A.U], share = total / A.W, rem = total - share * A.W;
   const int begin = A.pre[unit] + blk * steps, end = begin + steps;
   auto wg_of = [&](int s) { return s < rem * (share + 1) ? s / (share + 1) : rem + (s - rem * (share + 1)) / share; };
@@ -395,17 +427,24 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeArgs A, int ro
   M = wave_max(M);
   float L = 0.f;
   float2 o = make_float2(0.f, 0.f);
-  for (int i = w0; i <= w1; ++i) {
-    const float* rec = rec_of(i);
-    const float2 ml = *reinterpret_cast<const float2*>(rec + (size_t)rows * kD + 2 * in_blk);
-    const float2 x = *reinterpret_cast<const float2*>(rec + (size_t)in_blk * kD + 2 * lane);
-    const float f = ml.x > -INFINITY ? __builtin_amdgcn_exp2f(ml.x - M) : 0.f;
-    L = fmaf(ml.y, f, L);
-    o.x = fmaf(x.x, f, o.x);
-    o.y = fmaf(x.y, f, o.y);
+  for (int i0 = w0; i0 <= w1; i0 += 8) {                                   // eight records in flight
+    float2 ml[8], x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float* rec = rec_of(min(i0 + k, w1));
+      ml[k] = *reinterpret_cast<const float2*>(rec + (size_t)rows * kD + 2 * in_blk);
+      x[k] = *reinterpret_cast<const float2*>(rec + (size_t)in_blk * kD + 2 * lane);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float f = i0 + k <= w1 && ml[k].x > -INFINITY ? __builtin_amdgcn_exp2f(ml[k].x - M) : 0.f;
+      L = fmaf(ml[k].y, f, L);
+      o.x = fmaf(x[k].x, f, o.x);
+      o.y = fmaf(x[k].y, f, o.y);
+    }
   }
-  const int list = unit - b * A.L, tok = r / A.GL;
-  const size_t to = (size_t)(R.first + tok) * A.Hq + list * A.GL + (r - tok * A.GL);
+  const int tok = r / A.GL;
+  const size_t to = (size_t)(R.first + tok) * A.Hq + l.head + (r - tok * A.GL);
   const float f = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
   *reinterpret_cast<float2*>(A.out + to * kD + 2 * lane) = make_float2(o.x * f, o.y * f);
   if (lane == 0) A.norm[to] = L == 0.f ? -INFINITY : M * kLn2 + __logf(L);
@@ -425,7 +464,7 @@ constexpr int kTreeWgs = 512;                    // workgroups of a launch at mo
 struct TreeDims { int rows, keys; };             // of a workgroup, of a tile
 static TreeDims softmax_dims(const Dims& dm, int list_rows) {
   if (dm.dtype == EKV_F32) return list_rows <= 16 ? TreeDims{16, 16} : TreeDims{64, 32};
-  return list_rows <= 16 ? TreeDims{16, 32} : list_rows <= 32 ? TreeDims{32, 32} : list_rows <= 64 ? TreeDims{64, 64} : TreeDims{128, 64};
+  return list_rows <= 16 ? TreeDims{16, 32} : list_rows <= 32 ? TreeDims{32, 32} : TreeDims{list_rows <= 64 ? 64 : list_rows <= 128 ? 128 : 256, 64};
 }
 static long long softmax_steps(const Dims& dm, bool dense, int lists, int list_rows) {
   const TreeDims td = softmax_dims(dm, list_rows);
@@ -442,7 +481,8 @@ size_t tree_softmax_ws_bytes(const Dims& dm, int lists, int most) {
 
 template <typename TQ, typename TC, int NQ, int WQ>
 static void launch_softmax_shape(const TreeArgs& a, int grid, size_t lds, hipStream_t st) {
-  hipLaunchKernelGGL((tree_softmax_kernel<TQ, TC, NQ, WQ>), dim3(grid), dim3(kTreeThreads), lds, st, a);
+  if (a.page_idx != nullptr) hipLaunchKernelGGL((tree_softmax_kernel<TQ, TC, NQ, WQ, true>), dim3(grid), dim3(64 * (WQ == 1 ? 4 : WQ)), lds, st, a);
+  else hipLaunchKernelGGL((tree_softmax_kernel<TQ, TC, NQ, WQ, false>), dim3(grid), dim3(64 * (WQ == 1 ? 4 : WQ)), lds, st, a);
 }
 template <typename TQ, typename TC>
 static void launch_softmax_T(const Dims& dm, TreeArgs a, hipStream_t st) {
@@ -454,7 +494,7 @@ static void launch_softmax_T(const Dims& dm, TreeArgs a, hipStream_t st) {
   const long long units = (long long)a.U * a.blocks, tokens = (long long)(dense ? dm.Mmax : dm.cap) * dm.P;
   a.per_unit = tokens <= (units >= cus ? 8192 : units >= cus / 2 ? 2560 : 1024);
   const long long steps = softmax_steps(dm, dense, a.L, list_rows);
-  const int most = 2 * cus < kTreeWgs ? 2 * cus : kTreeWgs, share = td.rows <= 32 ? kTreeWaves : 1;
+  const int most = (td.rows == 256 ? 1 : 2) * cus < kTreeWgs ? (td.rows == 256 ? 1 : 2) * cus : kTreeWgs, share = td.rows <= 32 ? 4 : 1;
   const long long wgs = (steps + share - 1) / share;
   a.W = (int)(wgs < most ? wgs : most);
   size_t lds = 0;
@@ -471,7 +511,8 @@ static void launch_softmax_T(const Dims& dm, TreeArgs a, hipStream_t st) {
   else if (td.rows == 64) launch_softmax_shape<TQ, TC, 1, 4>(a, grid, lds, st);
   if constexpr (sizeof(TQ) == 2) {
     if (td.rows == 32) launch_softmax_shape<TQ, TC, 2, 1>(a, grid, lds, st);
-    else if (td.rows == 128) launch_softmax_shape<TQ, TC, 2, 4>(a, grid, lds, st);
+    else if (td.rows == 128) launch_softmax_shape<TQ, TC, 1, 8>(a, grid, lds, st);
+    else if (td.rows == 256) launch_softmax_shape<TQ, TC, 2, 8>(a, grid, lds, st);
   }
   if (!a.per_unit)
     hipLaunchKernelGGL(tree_join_kernel, dim3((unsigned)a.U * ((list_rows + 3) / 4)), dim3(256), 0, st, a, td.rows, td.keys);

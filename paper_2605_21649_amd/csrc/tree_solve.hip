@@ -49,83 +49,133 @@ __device__ __forceinline__ void add_rows(const T* v, int64_t stride, const float
 template <typename TQ, typename TC, int NW>
 __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs S) {
 #pragma clang fp contract(off)
-  constexpr int NT = 64 * NW, SEG = NW == 1 ? 1024 : 512, R = 8;
+  constexpr int NT = 64 * NW, SEG = 512, R = 8, kOneGroups = 64 * R, kRegs = 4;
   __shared__ float s_u[NW][SEG];
   __shared__ uint32_t s_at[NW][SEG];
   __shared__ float s_o[NW][kD];
-  __shared__ float s_red[2][NW][3], s_one[NW];
+  __shared__ float s_red[2][NW][3], s_one[NW < 2 ? 2 : NW];
   __shared__ int s_n[NW], s_supp;
   __shared__ float s_tau;
+  __shared__ uint16_t s_list[kOneGroups];
   const TreeArgs& A = S.t;
   const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
   const uint64_t lt = (1ull << lane) - 1;
   // consecutive rows, the heads of a token, on one XCD
   const int row = gridDim.x % kXcds == 0 ? (int)(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
   const int n = row / A.Hq, hq = row - n * A.Hq;
-  const int b = wave_last_at_most(A.start, A.B, n);
-  const TreeRows T = tree_rows(A, b);
+  const int b = uniform(wave_last_at_most(A.start, A.B, n));
+  const int unit = b * A.L + hq / A.GL;
+  const TreeList list = tree_list(A, unit);
+  const TreeRows T = list.R;
   if (n < T.first || n >= T.first + T.count) return;         // of no sequence
-  const int list = hq / A.GL, unit = b * A.L + list, hkv = hq / (A.Hq / A.Hkv);
-  const int groups = (list_positions(A, unit) + kGroup - 1) / kGroup;      // of the cache; one more of drafted keys
+  const int groups = (list.n_pos + kGroup - 1) / kGroup;     // of the cache; one more of drafted keys
   const float* z = A.z + (size_t)row * A.zstride;
   const float* zm = A.zmax + (size_t)row * A.n_groups;
-  const float zd = z[(size_t)groups * kGroup + lane];
-  // maxima, several groups to a register where there are more than registers (their mass is still no more than the row's)
-  float m[R];
+  const float zd = lane < T.count ? z[(size_t)groups * kGroup + lane] : -INFINITY;
+  // Row maximum and bound: by one wavefront where its registers hold all maxima (rows of up to 32 704 cached tokens), which then lists the
+  // groups above the bound for all; else by all, several groups to a register where there are more than registers (their
+  // mass is still no more than the row's), and every wavefront looks up its own.
+  const bool one = NW == 1 || groups < kOneGroups;
+  float m[R], zmax = 0.f, bound = 0.f;
+  bool folded = false;
+  auto relative = [&](auto&& sums) {
 #pragma unroll
-  for (int k = 0; k < R; ++k) m[k] = k * NT + tid <= groups ? zm[k * NT + tid] : -INFINITY;
-  const bool folded = groups >= R * NT;
-  if (folded) {
-    for (int g = R * NT + tid; g <= groups; g += R * NT) {
+    for (int k = 0; k < R; ++k) m[k] -= zmax;
+    const float eps = 4e-6f * fmaxf(1.f, fabsf(zmax)), t = group_bound(m, -1.0f - eps, S.beta, S.ibeta, sums);
+    bound = fmaxf(t - eps, -1.0f - eps);
+  };
+  if (one) {
+    if (w == 0) {
+      folded = groups >= kOneGroups;             // NW 1 alone
 #pragma unroll
-      for (int k = 0; k < R; ++k) m[k] = fmaxf(m[k], zm[min(g + k * NT, groups)]);
+      for (int k = 0; k < R; ++k) m[k] = k * 64 + lane <= groups ? zm[k * 64 + lane] : -INFINITY;
+      for (int g = kOneGroups + lane; g <= groups; g += kOneGroups) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) m[k] = fmaxf(m[k], zm[min(g + k * 64, groups)]);
+      }
+      float mx = m[0];
+#pragma unroll
+      for (int k = 1; k < R; ++k) mx = fmaxf(mx, m[k]);
+      zmax = wave_max(mx);
+      int n_list = 0;
+      if (zmax > -INFINITY) {
+        relative([&](float& f, float& d) { f = wave_sum(f); d = wave_sum(d); });
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+          const bool in = m[k] > bound && k * 64 + lane < groups;
+          const uint64_t mk = __ballot(in);
+          if (in) s_list[n_list + __popcll(mk & lt)] = (uint16_t)(k * 64 + lane);
+          n_list += __popcll(mk);
+        }
+      }
+      if constexpr (NW > 1) {
+        if (lane == 0) { s_one[0] = zmax; s_one[1] = bound; s_supp = n_list; }
+      } else {
+        s_supp = n_list;
+        wave_order();
+      }
+    }
+    if constexpr (NW > 1) {
+      __syncthreads();
+      zmax = s_one[0]; bound = s_one[1];
+    }
+  } else {
+    if constexpr (NW > 1) {
+#pragma unroll
+      for (int k = 0; k < R; ++k) m[k] = k * NT + tid <= groups ? zm[k * NT + tid] : -INFINITY;
+      folded = groups >= R * NT;
+      for (int g = R * NT + tid; g <= groups; g += R * NT) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) m[k] = fmaxf(m[k], zm[min(g + k * NT, groups)]);
+      }
+      float mx = m[0];
+#pragma unroll
+      for (int k = 1; k < R; ++k) mx = fmaxf(mx, m[k]);
+      zmax = block_max(mx, s_one);
+      if (zmax > -INFINITY) {
+        int parity = 0;
+        relative([&](float& f, float& d) {
+          f = wave_sum(f); d = wave_sum(d);
+          if (lane == 0) { s_red[parity][w][0] = f; s_red[parity][w][1] = d; }
+          __syncthreads();
+          f = 0.f; d = 0.f;
+#pragma unroll
+          for (int i = 0; i < NW; ++i) { f += s_red[parity][i][0]; d += s_red[parity][i][1]; }
+          parity ^= 1;
+        });
+      }
     }
   }
-  float mx = m[0];
-#pragma unroll
-  for (int k = 1; k < R; ++k) mx = fmaxf(mx, m[k]);
-  const float zmax = NW == 1 ? wave_max(mx) : block_max(mx, s_one);
   float* out = A.out + (size_t)row * kD;
   if (!(zmax > -INFINITY)) {                                 // no key at all
     if (tid < kD / 4) *reinterpret_cast<float4*>(out + 4 * tid) = make_float4(0.f, 0.f, 0.f, 0.f);
     if (tid == 0) { A.norm[row] = INFINITY; S.supp[row] = 0; }
     return;
   }
+  const float lo_u = fminf(bound, -1e-7f), ud = zd - zmax;
+  // each(u, position) for the keys of four groups at a time, 64 lanes
+  auto each_four = [&](const int (&g)[4], auto&& each) {
+    float zz[4];
 #pragma unroll
-  for (int k = 0; k < R; ++k) m[k] -= zmax;
-  const float eps = 4e-6f * fmaxf(1.f, fabsf(zmax));
-  int parity = 0;
-  float bound = group_bound(m, -1.0f - eps, S.beta, S.ibeta, [&](float& f, float& d) {
-    f = wave_sum(f); d = wave_sum(d);
-    if constexpr (NW > 1) {
-      if (lane == 0) { s_red[parity][w][0] = f; s_red[parity][w][1] = d; }
-      __syncthreads();
-      f = 0.f; d = 0.f;
+    for (int k = 0; k < 4; ++k) zz[k] = z[(size_t)max(g[k], 0) * kGroup + lane];
 #pragma unroll
-      for (int i = 0; i < NW; ++i) { f += s_red[parity][i][0]; d += s_red[parity][i][1]; }
-      parity ^= 1;
+    for (int k = 0; k < 4; ++k) {
+      if (g[k] < 0) break;
+      each(zz[k] - zmax, g[k] * kGroup + lane);
     }
-  });
-  bound = fmaxf(bound - eps, -1.0f - eps);
-  const float thr = zmax + bound, lo_u = fminf(bound, -1e-7f), ud = zd - zmax;
-  // each(u, position) for every candidate of this wavefront's groups above `above` (relative), 64 lanes at a time
+  };
   auto each_group = [&](uint64_t mask, int base, auto&& each) {
     while (mask != 0) {
-      float zz[4];
       int g[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         g[k] = mask != 0 ? base + __builtin_ctzll(mask) : -1;
         mask &= mask - 1;
-        zz[k] = z[(size_t)max(g[k], 0) * kGroup + lane];
       }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (g[k] < 0) break;
-        each(zz[k] - zmax, g[k] * kGroup + lane);
-      }
+      each_four(g, each);
     }
   };
+  // those of this wavefront's share of all groups that have a key above `above` (relative)
   auto each_candidate = [&](float above, auto&& each) {
     for (int base = 64 * w; base < groups; base += NT) {
       const float x = base + lane < groups ? zm[base + lane] : -INFINITY;
@@ -140,13 +190,20 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
     if (in && o < SEG) { s_u[w][o] = u; s_at[w][o] = (uint32_t)pos; }
     count += __popcll(mk);
   };
-  if (folded) {
+  if (one && !folded) {
+    const int n_list = uniform(s_supp);
+    for (int i = 4 * w; i < n_list; i += 4 * NW) {
+      int g[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) g[k] = i + k < n_list ? uniform(s_list[min(i + k, n_list - 1)]) : -1;
+      each_four(g, keep);
+    }
+  } else if (one || folded) {
     each_candidate(bound, keep);
   } else {
 #pragma unroll
     for (int k = 0; k < R; ++k) each_group(__ballot(m[k] > bound && k * NT + tid < groups), k * NT + 64 * w, keep);
   }
-  (void)thr;
   if (lane == 0) s_n[w] = count;
   __syncthreads();
   bool fits = true;
@@ -155,7 +212,39 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
   int supp = 0, evals = 0;
   float tau;
   if (fits) {
-    if (w == 0) {
+    int total = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) total += s_n[i];
+    if (w == 0 && total <= 64 * kRegs) {                     // the usual row: its candidates in one wavefront's registers
+      float u[kRegs + 1];
+#pragma unroll
+      for (int k = 0; k < kRegs; ++k) {
+        int e = lane + 64 * k, seg = 0;
+#pragma unroll
+        for (int i = 0; i < NW - 1; ++i) {
+          const bool next = seg == i && e >= s_n[i];
+          e -= next ? s_n[i] : 0;
+          seg += next ? 1 : 0;
+        }
+        u[k] = lane + 64 * k < total ? s_u[seg][e] : -INFINITY;
+      }
+      u[kRegs] = ud;
+      tau = with_beta(S.ibeta, [&](auto ib) {
+        constexpr int IB = decltype(ib)::value;
+        return solve_tau_core([&](float t, float& F, float& D, int& cnt) {
+          float f = 0.f, d = 0.f;
+          cnt = 0;
+#pragma unroll
+          for (int k = 0; k <= kRegs; ++k) {
+            const float x = fmaxf(u[k] - t, 0.f);
+            add_mass<IB>(x, S.beta, f, d);
+            cnt += __popcll(__ballot(x > 0.f));
+          }
+          F = wave_sum(f); D = S.beta * wave_sum(d);
+        }, lo_u, NAN, IB, supp, evals);
+      });
+      if (lane == 0) { s_tau = tau; s_supp = supp; }
+    } else if (w == 0) {
       tau = with_beta(S.ibeta, [&](auto ib) {
         constexpr int IB = decltype(ib)::value;
         return solve_tau_core([&](float t, float& F, float& D, int& cnt) {
@@ -180,7 +269,7 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
     __syncthreads();
     tau = s_tau; supp = s_supp;
   } else {
-    parity = 0;
+    int parity = 0;
     tau = solve_tau_core([&](float t, float& F, float& D, int& cnt) {
       float f = 0.f, d = 0.f;
       int c = 0;
@@ -202,8 +291,11 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
     __syncthreads();
   }
   // weights and value rows of the support, in place
-  const TreeLook look(A, unit, hkv);
-  auto value_row = [&](int pos) { return look.row(pos, look.phys(look.page(pos))); };
+  const TreeLook<true> in_list(A, unit, list);
+  const TreeLook<false> in_all(A, unit, list);
+  auto value_row = [&](int pos) {
+    return A.page_idx != nullptr ? in_list.row(pos, in_list.phys(in_list.page(pos))) : in_all.row(pos, in_all.phys(in_all.page(pos)));
+  };
   auto scaled = [&](float p, uint32_t at) {
     if constexpr (sizeof(TC) == 1) return p * A.v_scale[page_div(at, A.page_div)];
     else return p;
@@ -254,7 +346,7 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
       s_at[w][o] = (uint32_t)lane;
     }
     wave_order();
-    add_rows((const TQ*)A.v_new + T.first * A.vs + hkv * kD, A.vs, s_u[w], s_at[w], __popcll(mk), acc, [](float p, uint32_t) { return p; });
+    add_rows((const TQ*)A.v_new + T.first * A.vs + list.hkv * kD, A.vs, s_u[w], s_at[w], __popcll(mk), acc, [](float p, uint32_t) { return p; });
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -278,8 +370,10 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
 
 template <typename TQ, typename TC>
 static void launch_solve_T(const TreeSolveArgs& s, hipStream_t st) {
-  if (s.rows > 8 * device_compute_units() && s.t.n_groups <= 512)
+  if (s.rows > 8 * device_compute_units() && s.t.n_groups <= 128)
     hipLaunchKernelGGL((tree_solve_kernel<TQ, TC, 1>), dim3(s.rows), dim3(64), 0, st, s);
+  else if (s.rows <= 2 * device_compute_units())
+    hipLaunchKernelGGL((tree_solve_kernel<TQ, TC, 8>), dim3(s.rows), dim3(512), 0, st, s);
   else
     hipLaunchKernelGGL((tree_solve_kernel<TQ, TC, 4>), dim3(s.rows), dim3(256), 0, st, s);
 }
