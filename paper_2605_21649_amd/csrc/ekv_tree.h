@@ -9,8 +9,10 @@
 // Keys and values pass through LDS once for all rows of a workgroup: rows of a tile lie at their length, their 16-byte pieces in an
 // order that their number turns (piece ^ row % 16), so that neither sixteen rows' same piece nor the transposing reads of V
 // meet in a bank.  An 8-bit cache's codes become bf16 or float32 with their page's scale (exact) on the way into LDS.
-// Two kinds of shape: few rows (32): every wavefront has all of them and keys of its own, nothing is waited for together; more: four
-// or eight wavefronts share the keys, twice a tile's in LDS so that they meet once a tile, and have 16 or 32 rows each.
+// Two kinds of shape: up to 16 rows: every wavefront has all of them and keys of its own, nothing is waited for together; more: four
+// or eight wavefronts share the keys, twice a tile's in LDS so that they meet once a tile, and have 16 or 32 rows each.  (17 to 32
+// rows, two tiles of them in every wavefront with keys of its own: registers spill, and a spilled one read back waits for all loads
+// under way; lists of 4 x 128K tokens, 32 rows, softmax 97 us, by four wavefronts that share, half of them idle, 83.)
 #pragma once
 #include "ekv_attn8.h"
 
@@ -34,6 +36,7 @@ struct TreeArgs {
   float* part;                                   // softmax: two partial results a workgroup
   float* out; float* norm;
   float* z; float* zmax; size_t zstride; int n_groups;      // entmax: scores and group maxima
+  float beta; int ibeta;
 };
 
 // Drafted rows of a sequence: [first, first + count).
@@ -208,38 +211,25 @@ __device__ __forceinline__ void stage_drafted(const TreeArgs& A, char* lds, int 
 }
 
 // Query operands of a wavefront's NQ tiles of rows: lane (c, j) has of row c of a tile channels 32 s + 8 j + 0..7 (bf16), 16 s + 4 j +
-// 0..3 (float32).  Rows behind the last one repeat it.  LDS: kept there, 16 bytes a lane side by side: two tiles of rows beside a whole tile of
-// keys and values under way make the kernel spill, and a spilled register read back waits for every load before it (112 -> 96 us
-// for softmax over lists of 4 x 128K tokens, 32 rows).
-template <typename TQ, int NQ, bool LDS> struct TreeQuery {
+// 0..3 (float32).  Rows behind the last one repeat it.
+template <typename TQ, int NQ> struct TreeQuery {
   static constexpr int kSteps = sizeof(TQ) == 2 ? 4 : 8;
-  static constexpr int kLds = LDS ? NQ * kSteps * 1024 : 16;             // of a wavefront
-  uint4 v[LDS ? 1 : NQ][kSteps];
-  char* lds;
-  __device__ __forceinline__ void load(const TreeArgs& A, const TreeRows& R, int list_head, int r0, char* to) {
+  uint4 v[NQ][kSteps];
+  __device__ __forceinline__ void load(const TreeArgs& A, const TreeRows& R, int list_head, int r0) {
     const int lane = threadIdx.x & 63, c = lane & 15, j = lane >> 4;
-    lds = to + 16 * lane;
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
       const int r = min(r0 + 16 * t + c, R.count * A.GL - 1), tok = r / A.GL;
       const TQ* row = (const TQ*)A.q + ((size_t)(R.first + tok) * A.Hq + list_head + (r - tok * A.GL)) * kD;
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const uint4 x = *reinterpret_cast<const uint4*>(row + (sizeof(TQ) == 2 ? 32 * s + 8 * j : 16 * s + 4 * j));
-        if constexpr (LDS) *reinterpret_cast<uint4*>(lds + (t * kSteps + s) * 1024) = x;
-        else v[t][s] = x;
-      }
+      for (int s = 0; s < kSteps; ++s) v[t][s] = *reinterpret_cast<const uint4*>(row + (sizeof(TQ) == 2 ? 32 * s + 8 * j : 16 * s + 4 * j));
     }
-  }
-  __device__ __forceinline__ uint4 get(int t, int s) const {
-    if constexpr (LDS) return *reinterpret_cast<const uint4*>(lds + (t * kSteps + s) * 1024);
-    else return v[t][s];
   }
 };
 
 // S^T of M tiles of sixteen keys (from tile m0 of the LDS tile on) and a wavefront's rows: lane (c, j) gets keys 4j..4j+3 of row c.
-template <typename TQ, int NQ, int M, bool LDS>
-__device__ __forceinline__ void tree_scores(const char* k, int m0, const TreeQuery<TQ, NQ, LDS>& q, f32x4_t (&d)[M][NQ]) {
+template <typename TQ, int NQ, int M>
+__device__ __forceinline__ void tree_scores(const char* k, int m0, const TreeQuery<TQ, NQ>& q, f32x4_t (&d)[M][NQ]) {
   const int lane = threadIdx.x & 63, c = lane & 15, j = lane >> 4;
   constexpr int kSums = sizeof(TQ) == 2 ? 1 : 4;       // float32: a product has 4 of the 128 channels, four sums of 8 each round less
   f32x4_t sum[kSums][M][NQ];
@@ -252,19 +242,16 @@ __device__ __forceinline__ void tree_scores(const char* k, int m0, const TreeQue
     }
   }
 #pragma unroll
-  for (int s = 0; s < TreeQuery<TQ, NQ, LDS>::kSteps; ++s) {
-    uint4 row[NQ];
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) row[t] = q.get(t, s);
+  for (int s = 0; s < TreeQuery<TQ, NQ>::kSteps; ++s) {
 #pragma unroll
     for (int m = 0; m < M; ++m) {
       const uint4 a = *reinterpret_cast<const uint4*>(k + tree_piece<TQ>(16 * (m0 + m) + c, 4 * s + j));
 #pragma unroll
       for (int t = 0; t < NQ; ++t) {
         if constexpr (sizeof(TQ) == 2) {
-          sum[0][m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, row[t]), sum[0][m][t], 0, 0, 0);
+          sum[0][m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, q.v[t][s]), sum[0][m][t], 0, 0, 0);
         } else {
-          const f32x4_t x = __builtin_bit_cast(f32x4_t, a), y = __builtin_bit_cast(f32x4_t, row[t]);
+          const f32x4_t x = __builtin_bit_cast(f32x4_t, a), y = __builtin_bit_cast(f32x4_t, q.v[t][s]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum[e][m][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], sum[e][m][t], 0, 0, 0);
         }
@@ -277,6 +264,22 @@ __device__ __forceinline__ void tree_scores(const char* k, int m0, const TreeQue
     for (int t = 0; t < NQ; ++t) {
       if constexpr (sizeof(TQ) == 2) d[m][t] = sum[0][m][t];
       else d[m][t] = (sum[0][m][t] + sum[1][m][t]) + (sum[2][m][t] + sum[3][m][t]);
+    }
+  }
+}
+
+// All tiles of the LDS tile: together, or in float32, whose sums take four registers for one, a tile after the other.
+template <typename TQ, int NQ, int M>
+__device__ __forceinline__ void tree_scores_all(const char* k, const TreeQuery<TQ, NQ>& q, f32x4_t (&d)[M][NQ]) {
+  if constexpr (sizeof(TQ) == 2) {
+    tree_scores<TQ, NQ, M>(k, 0, q, d);
+  } else {
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      f32x4_t one[1][NQ];
+      tree_scores<TQ, NQ, 1>(k, m, q, one);
+#pragma unroll
+      for (int t = 0; t < NQ; ++t) d[m][t] = one[0][t];
     }
   }
 }

@@ -1,8 +1,11 @@
 // Entmax attention of drafted rows, first launch: scores of every row with its list's keys and with the drafted keys that its mask
 // names, and the maximum of every 64 of them (ekv_tree.h has the layout of the products).
 //
-// K is read once per block of rows; what bounds long lists is the scores' own bytes, 4 per row and key, beside K's.
+// K is read once per block of rows; what bounds long lists is the scores' own bytes, 4 per row and key, beside K's.  So where rows are many
+// a workgroup keeps a lower bound of every row's threshold, the root of the mass of the maxima that it has seen (32 a row, several
+// groups folded into one), and a group none of whose keys is above it is not stored: its maximum is put down as -inf, nobody will read it.
 // The drafted keys are a row's last group.  Hidden and missing keys score -inf.
+#include "ekv_solve.h"
 #include "ekv_tree.h"
 
 namespace ekv {
@@ -10,14 +13,12 @@ namespace ekv {
 constexpr int kGroup = 64;                       // keys per maximum
 
 template <typename TQ, typename TC, int NQ, int WQ, bool LISTS>
-__global__ __launch_bounds__(64 * (WQ == 1 ? 4 : WQ)) __attribute__((amdgpu_waves_per_eu(WQ == 1 ? 3 : 2)))
+__global__ __launch_bounds__(64 * (WQ == 1 ? 4 : WQ)) __attribute__((amdgpu_waves_per_eu(WQ == 1 ? 3 : WQ == 8 && NQ == 1 ? 4 : 2)))
 void tree_scores_kernel(const TreeArgs A) {
   using S = TreeShape<TQ, TC, NQ, WQ, 1>;
   constexpr int kPer = kGroup / S::kKeys;        // tiles of a group
   extern __shared__ int pre_lds[];
   __shared__ __attribute__((aligned(16))) char s_tile[S::kLds];
-  using Q = TreeQuery<TQ, NQ, WQ == 1 && NQ == 2>;
-  __shared__ __attribute__((aligned(16))) char s_q[Q::kLds];               // all wavefronts have the same rows
   __shared__ int wsum[S::kWaves];
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), c = lane & 15, j = lane >> 4;
   const int grp = WQ == 1 ? w : 0, tid = WQ == 1 ? lane : threadIdx.x;
@@ -27,8 +28,7 @@ void tree_scores_kernel(const TreeArgs A) {
     const int list_head = list.head, hkv = list.hkv;
     const int n_rows = R.count * A.GL;
     const int r0 = blk * S::kRows + (WQ > 1 ? w * 16 * NQ : 0);
-    Q q;
-    q.load(A, R, list_head, r0, s_q);
+    TreeQuery<TQ, NQ> q;
     float* z[NQ]; float* zmax[NQ];
     bool there[NQ];
 #pragma unroll
@@ -52,20 +52,33 @@ void tree_scores_kernel(const TreeArgs A) {
       valid_next = __ballot(look.valid(pos, lp));
       stage.request(A, tid, [&](int i) { return (uint32_t)__shfl((int)at_row, i); });
     };
+    q.load(A, R, list_head, r0);
     int lp1 = 0, ph1 = 0, lp2 = 0;
     if (t0 < t1) {
-      const int lp0 = look.page(pos_of(t0)), ph0 = look.phys(lp0);
+      const int lp0 = look.page(pos_of(t0));
       lp1 = look.page(pos_of(t0 + 1)); lp2 = look.page(pos_of(t0 + 2));
+      const int ph0 = look.phys(lp0);
       ph1 = look.phys(lp1);
       fetch(t0, lp0, ph0);
     }
     float top[NQ];
+    constexpr bool kHold = WQ > 1 && kPer == 1;
+    constexpr int kSlots = 8;                              // maxima of a row: kSlots in each of its four lanes
+    float slot[kHold ? NQ : 1][kSlots], bound[kHold ? NQ : 1], most[kHold ? NQ : 1];
+    if constexpr (kHold) {
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        bound[i] = most[i] = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kSlots; ++k) slot[i][k] = -INFINITY;
+      }
+    }
     // scores of the LDS tile to places from `to` on of the rows' scores, and into the maxima
     auto score = [&](const char* k, size_t to, auto drafted, uint64_t valid, const uint64_t (&seen)[NQ]) {
       constexpr bool kDrafted = decltype(drafted)::value != 0;
       constexpr uint64_t full = S::kKeys == 64 ? ~0ull : (1ull << (S::kKeys & 63)) - 1;
       f32x4_t d[S::kTiles][NQ];
-      tree_scores<TQ, NQ, S::kTiles>(k, 0, q, d);
+      tree_scores_all<TQ, NQ, S::kTiles>(k, q, d);
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
 #pragma unroll
@@ -79,7 +92,13 @@ void tree_scores_kernel(const TreeArgs A) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) top[i] = fmaxf(top[i], d[m][i][e]);
         }
-        if (there[i]) {
+        bool store = there[i];
+        if constexpr (kHold && !kDrafted) {
+          top[i] = fmaxf(top[i], __shfl_xor(top[i], 16));
+          top[i] = fmaxf(top[i], __shfl_xor(top[i], 32));
+          if (top[i] <= bound[i]) { store = false; top[i] = -INFINITY; }
+        }
+        if (store) {
 #pragma unroll
           for (int m = 0; m < S::kTiles; ++m) *reinterpret_cast<f32x4_t*>(z[i] + to + 16 * m) = d[m][i];
         }
@@ -106,7 +125,35 @@ void tree_scores_kernel(const TreeArgs A) {
     auto work = [&](const char* k, int t, uint64_t valid) {
       if (kPer == 1 || t % kPer == 0) clear_top();
       score(k, (size_t)t * S::kKeys, IntC<0>{}, valid, none);
-      if (kPer == 1 || t % kPer == kPer - 1) store_top(t / kPer);
+      if constexpr (kHold) {
+        const int seen_groups = t - t0, at = (seen_groups >> 2) & (kSlots - 1);
+        const bool mine = j == (seen_groups & 3);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+          if (j == 0 && there[i]) zmax[i][t] = top[i];
+          most[i] = fmaxf(most[i], top[i]);
+#pragma unroll
+          for (int k = 0; k < kSlots; ++k) slot[i][k] = mine && k == at ? fmaxf(slot[i][k], top[i]) : slot[i][k];
+        }
+        if ((seen_groups & 7) == 7) {                      // wave-uniform
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) {
+            float u[kSlots];
+#pragma unroll
+            for (int k = 0; k < kSlots; ++k) u[k] = slot[i][k] - most[i];
+            const float eps = 4e-6f * fmaxf(1.f, fabsf(most[i]));
+            // one key alone has mass 1 a step of 1 below it; the bound of fewer maxima is one of more
+            const float from = fmaxf(bound[i] + eps - most[i], -1.0f - eps);
+            const float b = group_bound(u, from, A.beta, A.ibeta, [&](float& f, float& d) {
+              f += __shfl_xor(f, 16); d += __shfl_xor(d, 16);
+              f += __shfl_xor(f, 32); d += __shfl_xor(d, 32);
+            });
+            if (most[i] > -INFINITY) bound[i] = fmaxf(bound[i], b + most[i] - eps);
+          }
+        }
+      } else {
+        if (kPer == 1 || t % kPer == kPer - 1) store_top(t / kPer);
+      }
     };
     if constexpr (WQ == 1) {
       for (int t = t0; t < t1; ++t) {
@@ -152,8 +199,7 @@ void tree_scores_kernel(const TreeArgs A) {
       }
       store_top(steps - 1);
     }
-    if constexpr (WQ == 1 && NQ == 2) __syncthreads();     // the queries are read
-    else if constexpr (WQ == 1) wave_order();
+    if constexpr (WQ == 1) wave_order();
   });
 }
 
@@ -163,7 +209,7 @@ constexpr int kScoreWgs = 1024;
 static int score_rows(const Dims& dm, int list_rows) {
   if (list_rows <= 16) return 16;
   if (dm.dtype == EKV_F32) return 64;
-  return list_rows <= 32 ? 32 : list_rows <= 64 ? 64 : list_rows <= 128 ? 128 : 256;
+  return list_rows <= 64 ? 64 : list_rows <= 128 ? 128 : 256;
 }
 static long long score_steps(const Dims& dm, bool dense, int lists, int list_rows) {
   const int rows = score_rows(dm, list_rows);
@@ -191,7 +237,7 @@ static void launch_scores_T(const Dims& dm, TreeArgs& a, hipStream_t st) {
   const int list_rows = a.most * a.GL, rows = score_rows(dm, list_rows);
   a.blocks = (list_rows + rows - 1) / rows;
   const long long steps = score_steps(dm, a.page_idx == nullptr, a.L, list_rows);
-  const int most = (rows == 256 ? 1 : rows <= 32 ? 3 : 2) * device_compute_units();
+  const int most = (rows == 256 ? 1 : rows == 16 ? 3 : 2) * device_compute_units();
   a.W = (int)(steps < most ? steps : most);
   size_t lds = 0;
   if (a.U > kUnitsLdsMax) {
@@ -203,8 +249,7 @@ static void launch_scores_T(const Dims& dm, TreeArgs& a, hipStream_t st) {
   if (rows == 16) launch_scores_shape<TQ, TC, 1, 1>(a, lds, st);
   else if (rows == 64) launch_scores_shape<TQ, TC, 1, 4>(a, lds, st);
   if constexpr (sizeof(TQ) == 2) {
-    if (rows == 32) launch_scores_shape<TQ, TC, 2, 1>(a, lds, st);
-    else if (rows == 128) launch_scores_shape<TQ, TC, 1, 8>(a, lds, st);
+    if (rows == 128) launch_scores_shape<TQ, TC, 1, 8>(a, lds, st);
     else if (rows == 256) launch_scores_shape<TQ, TC, 2, 8>(a, lds, st);
   }
 }
@@ -217,6 +262,7 @@ void launch_tree_entmax(const Dims& dm, TreeArgs a, bool codes, int32_t* supp, v
   a.z = (float*)((char*)ws + tree_pre_bytes(a.U));
   a.zmax = a.z + (size_t)a.N * dm.Hq * a.zstride;
   a.zscale = dm.a * dm.scale;
+  a.beta = dm.beta; a.ibeta = dm.ibeta;
   if (dm.dtype == EKV_F32) {
     if (codes) launch_scores_T<float, e4m3_t>(dm, a, st);
     else launch_scores_T<float, float>(dm, a, st);

@@ -34,13 +34,13 @@ template <typename TQ, int NQ, int TILES> struct TreeSoftmax {
   }
   // One LDS tile of the cache (bit i of valid: key i counts) or of drafted keys (bit i of seen[t]: for the lane's row of tile t).  bad: drafted
   // keys whose values are added by themselves, from v_bad.
-  template <bool DRAFTED, typename Q>
-  __device__ __forceinline__ void add(const char* k, const char* v, const Q& q, float zscale, uint64_t valid,
+  template <bool DRAFTED>
+  __device__ __forceinline__ void add(const char* k, const char* v, const TreeQuery<TQ, NQ>& q, float zscale, uint64_t valid,
                                       const uint64_t (&seen)[NQ], uint64_t bad, const TQ* v_bad, int64_t v_stride) {
     const int lane = threadIdx.x & 63, c = lane & 15, j = lane >> 4;
     constexpr uint64_t full = TILES == 4 ? ~0ull : (1ull << (16 * TILES & 63)) - 1;
     f32x4_t p[TILES][NQ];
-    tree_scores<TQ, NQ, TILES>(k, 0, q, p);
+    tree_scores_all<TQ, NQ, TILES>(k, q, p);
     if (DRAFTED || (valid & full) != full) {
 #pragma unroll
       for (int i = 0; i < TILES; ++i) {
@@ -224,8 +224,6 @@ void tree_softmax_kernel(const TreeArgs A) {
   using S = TreeShape<TQ, TC, NQ, WQ, 2>;
   extern __shared__ int pre_lds[];
   __shared__ __attribute__((aligned(16))) char s_tile[S::kLds];
-  using Q = TreeQuery<TQ, NQ, WQ == 1 && NQ == 2>;
-  __shared__ __attribute__((aligned(16))) char s_q[Q::kLds];               // all wavefronts have the same rows
   __shared__ uint32_t s_bad[S::kGroups][2];
   __shared__ int wsum[S::kWaves];
   constexpr int RS = kD + 4;                     // floats between rows of partial outputs in LDS
@@ -240,8 +238,7 @@ void tree_softmax_kernel(const TreeArgs A) {
     const int tiles0 = min(st0, steps - 1), tiles1 = min(st1, steps - 1);          // the steps' tiles of the cache
     const bool drafted = st1 == steps;
     const int r0 = blk * S::kRows + (WQ > 1 ? w * 16 * NQ : 0);         // the wavefront's first row
-    Q q;
-    q.load(A, R, list_head, r0, s_q);
+    TreeQuery<TQ, NQ> q;
     TreeSoftmax<TQ, NQ, S::kTiles> acc;
     acc.clear();
     // a group's share of the tiles
@@ -257,10 +254,12 @@ void tree_softmax_kernel(const TreeArgs A) {
       valid_next = __ballot(look.valid(pos, lp));
       stage.request(A, tid, [&](int i) { return (uint32_t)__shfl((int)at_row, i); });
     };
+    q.load(A, R, list_head, r0);
     int lp1 = 0, ph1 = 0, lp2 = 0;
     if (t0 < t1) {
-      const int lp0 = look.page(pos_of(t0)), ph0 = look.phys(lp0);
+      const int lp0 = look.page(pos_of(t0));
       lp1 = look.page(pos_of(t0 + 1)); lp2 = look.page(pos_of(t0 + 2));
+      const int ph0 = look.phys(lp0);
       ph1 = look.phys(lp1);
       fetch(t0, lp0, ph0);
     }
@@ -464,7 +463,7 @@ constexpr int kTreeWgs = 512;                    // workgroups of a launch at mo
 struct TreeDims { int rows, keys; };             // of a workgroup, of a tile
 static TreeDims softmax_dims(const Dims& dm, int list_rows) {
   if (dm.dtype == EKV_F32) return list_rows <= 16 ? TreeDims{16, 16} : TreeDims{64, 32};
-  return list_rows <= 16 ? TreeDims{16, 32} : list_rows <= 32 ? TreeDims{32, 32} : TreeDims{list_rows <= 64 ? 64 : list_rows <= 128 ? 128 : 256, 64};
+  return list_rows <= 16 ? TreeDims{16, 32} : TreeDims{list_rows <= 64 ? 64 : list_rows <= 128 ? 128 : 256, 64};
 }
 static long long softmax_steps(const Dims& dm, bool dense, int lists, int list_rows) {
   const TreeDims td = softmax_dims(dm, list_rows);
@@ -494,7 +493,7 @@ static void launch_softmax_T(const Dims& dm, TreeArgs a, hipStream_t st) {
   const long long units = (long long)a.U * a.blocks, tokens = (long long)(dense ? dm.Mmax : dm.cap) * dm.P;
   a.per_unit = tokens <= (units >= cus ? 8192 : units >= cus / 2 ? 2560 : 1024);
   const long long steps = softmax_steps(dm, dense, a.L, list_rows);
-  const int most = (td.rows == 256 ? 1 : 2) * cus < kTreeWgs ? (td.rows == 256 ? 1 : 2) * cus : kTreeWgs, share = td.rows <= 32 ? 4 : 1;
+  const int most = (td.rows == 256 ? 1 : 2) * cus < kTreeWgs ? (td.rows == 256 ? 1 : 2) * cus : kTreeWgs, share = td.rows == 16 ? 4 : 1;
   const long long wgs = (steps + share - 1) / share;
   a.W = (int)(wgs < most ? wgs : most);
   size_t lds = 0;
@@ -510,8 +509,7 @@ static void launch_softmax_T(const Dims& dm, TreeArgs a, hipStream_t st) {
   if (td.rows == 16) launch_softmax_shape<TQ, TC, 1, 1>(a, grid, lds, st);
   else if (td.rows == 64) launch_softmax_shape<TQ, TC, 1, 4>(a, grid, lds, st);
   if constexpr (sizeof(TQ) == 2) {
-    if (td.rows == 32) launch_softmax_shape<TQ, TC, 2, 1>(a, grid, lds, st);
-    else if (td.rows == 128) launch_softmax_shape<TQ, TC, 1, 8>(a, grid, lds, st);
+    if (td.rows == 128) launch_softmax_shape<TQ, TC, 1, 8>(a, grid, lds, st);
     else if (td.rows == 256) launch_softmax_shape<TQ, TC, 2, 8>(a, grid, lds, st);
   }
   if (!a.per_unit)
