@@ -389,20 +389,24 @@ def ekv_decode8_full_softmax(cfg, q, cache, out, lse, workspace, stream=None):
 
 
 def ekv_norm_rotate(cfg, x_q, x_k, w_q, w_k, eps, freq, pos, q_out, k_out, pairs=False, stream=None):
-    qn, kn, t = x_q.shape, x_k.shape, _TYPES.get(cfg.kv_dtype)
+    t, d = _TYPES.get(cfg.kv_dtype), cfg.head_dim
+    qn, kn = x_q.shape, x_k.shape
     (q, qs), (k, ks) = _rows(x_q, qn), _rows(x_k, kn)
-    n = qn[0]
-    assert kn[0] == n and qn[1:] == (cfg.n_q_heads, cfg.head_dim) and kn[1:] == (cfg.n_kv_heads, cfg.head_dim), \
-        "rows of the config's heads and head size"
+    n, hq, hk = qn[0], qn[1], kn[1]
+    assert kn[0] == n and hq == cfg.n_q_heads and hk == cfg.n_kv_heads and qn[2] == d == kn[2], "rows of the config's heads and head size"
     assert x_q.dtype is t and x_k.dtype is t and q_out.dtype is t and k_out.dtype is t, "rows and outputs of the config's type"
-    assert q_out.shape == qn and k_out.shape == kn, "an output row for every token"
-    for w in (w_q, w_k):
-        assert w is None or (w.dtype is t and w.numel() == cfg.head_dim), "weights of the config's type and head size"
-    assert freq is None or freq.dtype is torch.float32, "frequencies are float32"
+    assert q_out.numel() == n * hq * d and k_out.numel() == n * hk * d, "an output row for every token"
+    assert w_q is None or (w_q.dtype is t and w_q.numel() == d), "weights of the config's type and head size"
+    assert w_k is None or (w_k.dtype is t and w_k.numel() == d), "weights of the config's type and head size"
+    turned = 0
+    if freq is not None:
+        turned = freq.numel()
+        assert freq.dtype is torch.float32, "frequencies are float32"
     assert pos is None or (pos.dtype is torch.int32 and pos.numel() >= n), "positions: int32, one for every token"
-    _check(load_library().ekv_norm_rotate(byref(cfg), q, qs, k, ks, _ptr(w_q), _ptr(w_k), eps, _ptr(freq),
-                                          freq.numel() if freq is not None else 0, _ptr(pos), n, 1 if pairs else 0, _ptr(q_out),
-                                          _ptr(k_out), _stream(stream)))
+    status = load_library().ekv_norm_rotate(byref(cfg), q, qs, k, ks, _ptr(w_q), _ptr(w_k), eps, _ptr(freq), turned, _ptr(pos), n,
+                                            1 if pairs else 0, _ptr(q_out), _ptr(k_out), _stream(stream))
+    if status:
+        _check(status)
 
 
 def ekv_cache_append(cfg, cache, stats, tokens, k_new, v_new, rows=None, stream=None):
@@ -427,7 +431,7 @@ def tree_view(start, visible, k_new, v_new, max_tree):
     assert start.dtype is torch.int32 and visible.element_size() == 8 and not visible.is_floating_point(), "start int32, masks of 64 bits"
     assert visible.numel() == kn[0], "a mask for every drafted row"
     tree = ekv_tree_view(k, v, ks, vs, _ptr(start), _ptr(visible), kn[0], max_tree)
-    tree.of = (kn[1:], k_new.dtype, start.numel())            # what the calls check against their config
+    tree.of = (kn[1], kn[2], k_new.dtype, start.numel())      # what the calls check against their config
     return tree
 
 
@@ -438,21 +442,28 @@ def ekv_tree_workspace_bytes(cfg, op, max_tokens, max_tree):
 
 
 def _tree(call, cfg, q, cache, tree, page_idx, n_sel, heads, outs, workspace, stream):
-    t = _TYPES.get(cfg.kv_dtype)
-    assert q.dtype is t and q.numel() == tree.max_tokens * cfg.n_q_heads * cfg.head_dim, "a query of the config's type for every row and head"
-    heads_of, dtype, starts = tree.of
-    assert heads_of == (cfg.n_kv_heads, cfg.head_dim) and dtype is t, "drafted rows of the config's type, KV heads and head size"
-    assert starts == cfg.batch + 1, "start has an entry for every sequence and one more"
-    rows = tree.max_tokens * cfg.n_q_heads
-    assert outs[0].dtype is torch.float32 and outs[0].numel() == rows * cfg.head_dim, "out: float32, like q"
-    for o in outs[1:]:
-        assert o.element_size() == 4 and o.numel() == rows, "tau or lse float32, supp int32: one for every row and head"
+    t, hq, d, batch, n = _TYPES.get(cfg.kv_dtype), cfg.n_q_heads, cfg.head_dim, cfg.batch, tree.max_tokens
+    rows = n * hq
+    assert q.dtype is t and q.numel() == rows * d, "a query of the config's type for every row and head"
+    kv_heads, size, dtype, starts = tree.of
+    assert kv_heads == cfg.n_kv_heads and size == d and dtype is t, "drafted rows of the config's type, KV heads and head size"
+    assert starts == batch + 1, "start has an entry for every sequence and one more"
+    out, norm = outs[0], outs[1]
+    assert out.dtype is torch.float32 and out.numel() == rows * d, "out: float32, like q"
+    assert norm.dtype is torch.float32 and norm.numel() == rows, "tau or lse: float32, one for every row and head"
     args = [byref(cfg), _ptr(q), byref(cache), byref(tree)]
     if heads:
         assert page_idx.dtype is torch.int32 and n_sel.dtype is torch.int32, "page lists are int32"
-        assert n_sel.numel() == cfg.batch * heads and page_idx.numel() == n_sel.numel() * cfg.max_sel_pages, "a list of cap pages for every sequence and head"
-        args += [_ptr(page_idx), _ptr(n_sel)]
-    _check(call(*args, *[_ptr(o) for o in outs], _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+        assert n_sel.numel() == batch * heads and page_idx.numel() == batch * heads * cfg.max_sel_pages, "a list of cap pages for every sequence and head"
+        args += (_ptr(page_idx), _ptr(n_sel))
+    args += (_ptr(out), _ptr(norm))
+    if len(outs) > 2:
+        supp = outs[2]
+        assert supp.dtype is torch.int32 and supp.numel() == rows, "supp: int32, one for every row and head"
+        args.append(_ptr(supp))
+    status = call(*args, _ptr(workspace), workspace.nbytes, _stream(stream))
+    if status:
+        _check(status)
 
 
 def ekv_tree_sparse(cfg, q, cache, tree, page_idx, n_sel, out, tau, supp, workspace, stream=None):

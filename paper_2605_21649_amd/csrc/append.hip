@@ -5,7 +5,7 @@
 // of the page's rows r, r + 4, ..: the rows' order of ekv_stats_build in the sums, whose result is that call's to the last bit.
 // V and, without statistics, K are a copy; with statistics the run's page is gone through from its first token, the older ones
 // from the cache and the new ones from their rows.  Bound by the bytes: rows read and written once, old keys of partly filled
-// pages, records.
+// pages, records; 24000 tokens of prompts without statistics 196 MB in 49 us, 4.0 TB/s (a copy: 4.7).
 #include "ekv_internal.h"
 #include "ekv_stats.h"
 
@@ -148,6 +148,10 @@ void launch_cache_append(const Dims& dm, const ekv_cache_view& c, const ekv_stat
   a.rows = rows; a.n_rows = n_rows;
   a.T = tok.max_tokens; a.B = dm.B; a.Hkv = dm.Hkv; a.HkvPool = dm.HkvPool; a.P = dm.P; a.Mmax = dm.Mmax;
   a.n_slots = (int64_t)c.n_phys_pages * dm.P;
+  // Tokens per wavefront: one where there are few, so that a step's go on at once, up to 32 (64 with pages that long) where most
+  // are prompts', of which one in P begins a run.  us, up to 4096 wavefronts / 16384 / 65536: 157 single tokens 8.4 / 8.5 / 8.5, 1000
+  // 23.3 / 25.1 / 25.1, 2000 tokens of 20 chunks 11.8 / 14.4 / 18.5, 24000 of 6 prompts 64.1 / 64.3 / 70.6, 16411 float32 in pages of 12
+  // 75.3 / 75.3 / 71.7, 16000 in pages of 64 48.9 / 45.0 / 62.1.
   a.block = 1;
   while (a.block < (dm.P < 64 ? 32 : 64) && (long long)a.T * dm.Hkv * 2 / a.block > 4096) a.block *= 2;
   const long long waves = (long long)((a.T + a.block - 1) / a.block) * dm.Hkv * 2;

@@ -32,14 +32,15 @@ template <typename TQ, int NQ, int TILES> struct TreeSoftmax {
       for (int i = 0; i < 8; ++i) o[t][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
   }
-  // One LDS tile of the cache (bit i of valid: key i counts) or of drafted keys (bit i of seen[t]: for the lane's row of tile t).  bad: drafted
-  // keys whose values are added by themselves, from v_bad.
+  struct Weights { f32x4_t p[TILES][NQ]; };                // of a tile: lane (c, j) has keys 16 i + 4 j + 0..3 of row c
+  // From an LDS tile of keys of the cache (bit i of valid: key i counts) or drafted ones (bit i of seen[t]: for the lane's row of tile t) to
+  // weights; maxima and sums go on.  bad: drafted keys whose values are added here, by themselves, from v_bad.
   template <bool DRAFTED>
-  __device__ __forceinline__ void add(const char* k, const char* v, const TreeQuery<TQ, NQ>& q, float zscale, uint64_t valid,
-                                      const uint64_t (&seen)[NQ], uint64_t bad, const TQ* v_bad, int64_t v_stride) {
+  __device__ __forceinline__ void weigh(const char* k, const TreeQuery<TQ, NQ>& q, float zscale, uint64_t valid, const uint64_t (&seen)[NQ],
+                                        uint64_t bad, const TQ* v_bad, int64_t v_stride, Weights& out) {
     const int lane = threadIdx.x & 63, c = lane & 15, j = lane >> 4;
     constexpr uint64_t full = TILES == 4 ? ~0ull : (1ull << (16 * TILES & 63)) - 1;
-    f32x4_t p[TILES][NQ];
+    f32x4_t (&p)[TILES][NQ] = out.p;
     tree_scores_all<TQ, NQ, TILES>(k, q, p);
     if (DRAFTED || (valid & full) != full) {
 #pragma unroll
@@ -77,23 +78,18 @@ template <typename TQ, int NQ, int TILES> struct TreeSoftmax {
         for (int i = 0; i < 8; ++i) o[t][i] *= f;
       }
     }
-    // weights of key tiles i0..i1-1 in the scores' place
-    auto weigh = [&](int i0, int i1) {
 #pragma unroll
-      for (int t = 0; t < NQ; ++t) {
-        const float base = m[t] > -INFINITY ? -m[t] : 0.f;
+    for (int t = 0; t < NQ; ++t) {
+      const float base = m[t] > -INFINITY ? -m[t] : 0.f;
 #pragma unroll
-        for (int i = 0; i < TILES; ++i) {
-          if (i < i0 || i >= i1) continue;
+      for (int i = 0; i < TILES; ++i) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            p[i][t][e] = __builtin_amdgcn_exp2f(fmaf(p[i][t][e], zscale, base));
-            l[t] += p[i][t][e];
-          }
+        for (int e = 0; e < 4; ++e) {
+          p[i][t][e] = __builtin_amdgcn_exp2f(fmaf(p[i][t][e], zscale, base));
+          l[t] += p[i][t][e];
         }
       }
-    };
-    if constexpr (DRAFTED) weigh(0, TILES);
+    }
     if (DRAFTED && bad != 0) {
       for (uint64_t left = bad; left != 0; left &= left - 1) {
         const int key = __builtin_ctzll(left);
@@ -134,41 +130,34 @@ template <typename TQ, int NQ, int TILES> struct TreeSoftmax {
         }
       }
     }
+  }
+  // The weighted values of the tile.
+  __device__ __forceinline__ void multiply(const char* v, const Weights& x) {
+    const int lane = threadIdx.x & 63, c = lane & 15, j = lane >> 4;
     if constexpr (sizeof(TQ) == 2) {
-      // 32 keys at a time (lane group j has keys 4j..4j+3 of either tile); the next 32 keys' weights are computed while these are multiplied
-      bf16x8_t w[3][NQ];
-      auto terms = [&](int i) {
-        if constexpr (!DRAFTED) weigh(i, i + 2);
+#pragma unroll
+      for (int i = 0; i < TILES; i += 2) {
+        // 32 keys at a time, lane group j has keys 4j..4j+3 of either tile of sixteen: three terms of their weights
+        bf16x8_t w[3][NQ];
 #pragma unroll
         for (int t = 0; t < NQ; ++t) {
-          float x[8];
+          float y[8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) { x[e] = p[i][t][e]; x[4 + e] = p[i + 1][t][e]; }
+          for (int e = 0; e < 4; ++e) { y[e] = x.p[i][t][e]; y[4 + e] = x.p[i + 1][t][e]; }
 #pragma unroll
           for (int term = 0; term < 3; ++term) {
             u32x4_t r;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) r[e] = top_halves(x[2 * e], x[2 * e + 1]);
+            for (int e = 0; e < 4; ++e) r[e] = top_halves(y[2 * e], y[2 * e + 1]);
             w[term][t] = __builtin_bit_cast(bf16x8_t, r);
             if (term < 2) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] = below(x[e]);
+              for (int e = 0; e < 8; ++e) y[e] = below(y[e]);
             }
           }
         }
-      };
-      terms(0);
-#pragma unroll
-      for (int i = 0; i < TILES; i += 2) {
         // a sum's terms are apart from each other: 2 (4) channels' by the rows' tiles between them
         constexpr int CH = NQ == 1 ? 4 : 2;
-        bf16x8_t now[3][NQ];
-#pragma unroll
-        for (int term = 0; term < 3; ++term) {
-#pragma unroll
-          for (int t = 0; t < NQ; ++t) now[term][t] = w[term][t];
-        }
-        if (i + 2 < TILES) terms(i + 2);
 #pragma unroll
         for (int ch = 0; ch < 8; ch += CH) {
           bf16x8_t a[CH];
@@ -184,13 +173,12 @@ template <typename TQ, int NQ, int TILES> struct TreeSoftmax {
             for (int h = 0; h < CH; ++h) {
 #pragma unroll
               for (int t = 0; t < NQ; ++t)
-                o[t][ch + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[h], now[term][t], o[t][ch + h], 0, 0, 0);
+                o[t][ch + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[h], w[term][t], o[t][ch + h], 0, 0, 0);
             }
           }
         }
       }
     } else {
-      if constexpr (!DRAFTED) weigh(0, TILES);
 #pragma unroll
       for (int i = 0; i < TILES; ++i) {
 #pragma unroll
@@ -199,11 +187,17 @@ template <typename TQ, int NQ, int TILES> struct TreeSoftmax {
           for (int e = 0; e < 4; ++e) {
             const float a = *reinterpret_cast<const float*>(v + tree_piece<TQ>(16 * i + 4 * j + e, 4 * ch + (c >> 2)) + 4 * (c & 3));
 #pragma unroll
-            for (int t = 0; t < NQ; ++t) o[t][ch] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p[i][t][e], o[t][ch], 0, 0, 0);
+            for (int t = 0; t < NQ; ++t) o[t][ch] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, x.p[i][t][e], o[t][ch], 0, 0, 0);
           }
         }
       }
     }
+  }
+  __device__ __forceinline__ void add(const char* k, const char* v, const TreeQuery<TQ, NQ>& q, float zscale, uint64_t valid) {
+    const uint64_t none[NQ] = {};
+    Weights x;
+    weigh<false>(k, q, zscale, valid, none, 0, nullptr, 0, x);
+    multiply(v, x);
   }
 };
 
@@ -263,7 +257,6 @@ void tree_softmax_kernel(const TreeArgs A) {
       ph1 = look.phys(lp1);
       fetch(t0, lp0, ph0);
     }
-    const uint64_t none[NQ] = {};
     auto ahead = [&](int t) {                              // tile t's data under way, the lookups of the two behind it
       const int ph2 = look.phys(lp2), lp3 = look.page(pos_of(t + 2));
       fetch(t, lp1, ph1);
@@ -276,7 +269,7 @@ void tree_softmax_kernel(const TreeArgs A) {
         stage.commit(tile, tid, valid);
         ahead(t + 1);
         wave_order();
-        acc.template add<false>(tile, tile + S::kSideBytes, q, A.zscale, valid, none, 0, nullptr, 0);
+        acc.add(tile, tile + S::kSideBytes, q, A.zscale, valid);
       }
     } else if (t0 < t1) {
       // tile t + 1 goes to the half of LDS that nobody reads while tile t is worked on: one meeting a tile
@@ -290,7 +283,7 @@ void tree_softmax_kernel(const TreeArgs A) {
         const uint64_t after = valid_next;
         if (t + 1 < t1) stage.commit(tile + ((t + 1 - t0) & 1) * S::kTileBytes, tid, after);
         ahead(t + 2);
-        acc.template add<false>(now, now + S::kSideBytes, q, A.zscale, valid, none, 0, nullptr, 0);
+        acc.add(now, now + S::kSideBytes, q, A.zscale, valid);
         valid = after;
       }
     }
@@ -316,7 +309,9 @@ void tree_softmax_kernel(const TreeArgs A) {
         }
         if constexpr (WQ > 1) __syncthreads(); else wave_order();
         const uint64_t bad = (uint64_t)(uint32_t)uniform((int)s_bad[grp][0]) | (uint64_t)(uint32_t)uniform((int)s_bad[grp][1]) << 32;
-        acc.template add<true>(tile, tile + S::kSideBytes, q, A.zscale, 0, seen, bad, (const TQ*)A.v_new + (int64_t)(R.first + d0) * A.vs + hkv * kD, A.vs);
+        typename TreeSoftmax<TQ, NQ, S::kTiles>::Weights x;
+        acc.template weigh<true>(tile, q, A.zscale, 0, seen, bad, (const TQ*)A.v_new + (int64_t)(R.first + d0) * A.vs + hkv * kD, A.vs, x);
+        acc.multiply(tile + S::kSideBytes, x);
       }
     }
     // the rows' sums
@@ -491,7 +486,13 @@ static void launch_softmax_T(const Dims& dm, TreeArgs a, hipStream_t st) {
   const int cus = device_compute_units();
   a.blocks = (list_rows + td.rows - 1) / td.rows;
   const long long units = (long long)a.U * a.blocks, tokens = (long long)(dense ? dm.Mmax : dm.cap) * dm.P;
-  a.per_unit = tokens <= (units >= cus ? 8192 : units >= cus / 2 ? 2560 : 1024);
+  // A block of rows whole by one workgroup, without prefix sums, records and join, where blocks are many and no list can be long.  Calls, us,
+  // split / whole, a sequence's KV heads one unit: of 16 rows, 8 units of 200 tokens 12.4 / 13.0, of 2000 14.9 / 29.4, 128 of 1000 26.4 / 20.9, of
+  // 2000 36.3 / 34.9, 256 of 1000 38.4 / 28.9, of 2000 56.9 / 47.4, 512 of 4000 175 / 161, of 8000 328 / 309; of 64 rows, 32 of 1000 24.3 / 32.0, 128
+  // of 2000 46.1 / 57.1, 256 of 1000 52.6 / 39.7, of 4000 108.9 / 113.5, 512 of 1000 85.9 / 60.7, of 4000 212 / 190; of 256 rows, 64 of 1000 55.3 /
+  // 66.9, 128 of 3000 128 / 164, 512 of 1000 192 / 143.  The line is the capacity's: a long sequence among short ones is one workgroup's.
+  const long long whole = units >= 2 * cus ? 8192 : units >= cus ? (td.rows == 16 ? 8192 : 2048) : units >= cus / 2 && td.rows == 16 ? 2048 : 0;
+  a.per_unit = tokens <= whole;
   const long long steps = softmax_steps(dm, dense, a.L, list_rows);
   const int most = (td.rows == 256 ? 1 : 2) * cus < kTreeWgs ? (td.rows == 256 ? 1 : 2) * cus : kTreeWgs, share = td.rows == 16 ? 4 : 1;
   const long long wgs = (steps + share - 1) / share;

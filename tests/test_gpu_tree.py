@@ -25,6 +25,8 @@ SHAPES = [
     ([99, 450], [4, 21], (2, 1), 20, "f32", "e4m3"),
     ([64, 333], [50, 64], (4, 2), 48, "f32", "e4m3"),
     ([2900, 17], [4, 2], (4, 1), 8, "bf16", "e4m3"),
+    ([260, 100], [32, 20], (4, 1), 16, "bf16", "same"),
+    ([150, 300], [30, 26], (8, 2), 8, "bf16", "e4m3"),
 ]
 IDS = ["x".join(map(str, s[0])) + "-" + "x".join(map(str, s[1])) + f"-{s[2][0]}.{s[2][1]}-p{s[3]}-{s[4]}-{s[5]}" for s in SHAPES]
 
