@@ -431,7 +431,8 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeArgs A, int ro
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float f = i0 + k <= w1 && ml[k].x > -INFINITY ? __builtin_amdgcn_exp2f(ml[k].x - M) : 0.f;
+      if (i0 + k > w1) break;                                              // the last record over again, infinities and all
+      const float f = ml[k].x > -INFINITY ? __builtin_amdgcn_exp2f(ml[k].x - M) : 0.f;
       L = fmaf(ml[k].y, f, L);
       o.x = fmaf(x[k].x, f, o.x);
       o.y = fmaf(x[k].y, f, o.y);
