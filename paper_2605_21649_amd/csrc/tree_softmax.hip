@@ -431,9 +431,10 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeArgs A, int ro
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      if (i0 + k > w1) break;                                              // the last record over again, infinities and all
-      const float f = ml[k].x > -INFINITY ? __builtin_amdgcn_exp2f(ml[k].x - M) : 0.f;
-      L = fmaf(ml[k].y, f, L);
+      const bool in = i0 + k <= w1;                                        // else the last record over again, infinities and all
+      const float f = in && ml[k].x > -INFINITY ? __builtin_amdgcn_exp2f(ml[k].x - M) : 0.f;
+      x[k] = in ? x[k] : make_float2(0.f, 0.f);
+      L = fmaf(in ? ml[k].y : 0.f, f, L);
       o.x = fmaf(x[k].x, f, o.x);
       o.y = fmaf(x[k].y, f, o.y);
     }
