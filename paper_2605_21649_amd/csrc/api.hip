@@ -537,7 +537,7 @@ static bool tree_supported(const Dims& dm, int lists, bool entmax, int n_tokens,
 }
 static size_t tree_ws_bytes(const Dims& dm, int lists, bool entmax, int n_tokens, int most) {
   const int L = lists == kAllPages ? dm.Hkv : dm.Hq;         // one size for lists per query head and per KV head
-  return entmax ? tree_entmax_ws_bytes(dm, lists == kAllPages, L, n_tokens) : tree_softmax_ws_bytes(dm, L, most);
+  return entmax ? tree_entmax_ws_bytes(dm, lists == kAllPages, L, n_tokens) : tree_softmax_ws_bytes(dm, lists == kAllPages, L, most);
 }
 
 // one of cache and c8; entmax: norm is tau, else the log-sum-exp and supp is null

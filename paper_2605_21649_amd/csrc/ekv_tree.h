@@ -347,7 +347,7 @@ void launch_tree_entmax(const Dims& dm, TreeArgs a, bool codes, int32_t* supp, v
 // lists: page lists per sequence (query heads or KV heads), most: drafted rows of a sequence
 bool tree_softmax_supported(const Dims& dm, bool dense, int lists, int most);      // steps are counted in 31 bits
 bool tree_entmax_supported(const Dims& dm, bool dense, int lists, int n_tokens, int most);
-size_t tree_softmax_ws_bytes(const Dims& dm, int lists, int most);
+size_t tree_softmax_ws_bytes(const Dims& dm, bool dense, int lists, int most);
 size_t tree_entmax_ws_bytes(const Dims& dm, bool dense, int lists, int n_tokens);
 
 // cache type of an instantiation

@@ -458,20 +458,27 @@ void launch_tree_prefix(const TreeArgs& a, int keys, int rows, hipStream_t st) {
 constexpr int kTreeWgs = 512;                    // workgroups of a launch at most; workspaces are sized for them
 
 struct TreeDims { int rows, keys; };             // of a workgroup, of a tile
-static TreeDims softmax_dims(const Dims& dm, int list_rows) {
+static long long list_tokens(const Dims& dm, bool dense) { return (long long)(dense ? dm.Mmax : dm.cap) * dm.P; }
+// Blocks as large as the rows of a list, or of 64 rows where there is so little to go through that more workgroups count for more than reading
+// keys once.  Calls, us, blocks of 64 / of 128 / of 256 rows: lists of 256 rows, 8 of 4000 tokens 27 / 38 / 34, 16 of 2049 8-bit 24 / 30 / 28, 64 of
+// 1000 35 / 57 / 53, 32 of 4000 57 / 64 / 54, 16 of 32000 184 / 177 / 149, 64 of 16000 312 / 290 / 238; of 128 rows, 64 of 4096 57 / 71, 32 of 8000
+// 65 / 73, 8 of 128000 205 / 184.
+static TreeDims softmax_dims(const Dims& dm, bool dense, int lists, int list_rows) {
   if (dm.dtype == EKV_F32) return list_rows <= 16 ? TreeDims{16, 16} : TreeDims{64, 32};
-  return list_rows <= 16 ? TreeDims{16, 32} : TreeDims{list_rows <= 64 ? 64 : list_rows <= 128 ? 128 : 256, 64};
+  if (list_rows <= 16) return {16, 32};
+  const long long all = list_tokens(dm, dense) * dm.B * lists;
+  if (list_rows <= 64 || all <= (list_rows <= 128 ? 1ll << 19 : 3ll << 15)) return {64, 64};
+  return {list_rows <= 128 ? 128 : 256, 64};
 }
 static long long softmax_steps(const Dims& dm, bool dense, int lists, int list_rows) {
-  const TreeDims td = softmax_dims(dm, list_rows);
-  const long long tokens = (long long)(dense ? dm.Mmax : dm.cap) * dm.P;
-  return (long long)dm.B * lists * ((list_rows + td.rows - 1) / td.rows) * ((tokens + td.keys - 1) / td.keys + 1);
+  const TreeDims td = softmax_dims(dm, dense, lists, list_rows);
+  return (long long)dm.B * lists * ((list_rows + td.rows - 1) / td.rows) * ((list_tokens(dm, dense) + td.keys - 1) / td.keys + 1);
 }
 bool tree_softmax_supported(const Dims& dm, bool dense, int lists, int most) {
   return softmax_steps(dm, dense, lists, most * (dm.Hq / lists)) <= 0x7fffffff;
 }
-size_t tree_softmax_ws_bytes(const Dims& dm, int lists, int most) {
-  const TreeDims td = softmax_dims(dm, most * (dm.Hq / lists));
+size_t tree_softmax_ws_bytes(const Dims& dm, bool dense, int lists, int most) {
+  const TreeDims td = softmax_dims(dm, dense, lists, most * (dm.Hq / lists));
   return tree_pre_bytes((size_t)dm.B * lists) + 2 * kTreeWgs * tree_rec(td.rows) * sizeof(float);
 }
 
@@ -483,11 +490,11 @@ static void launch_softmax_shape(const TreeArgs& a, int grid, size_t lds, hipStr
 template <typename TQ, typename TC>
 static void launch_softmax_T(const Dims& dm, TreeArgs a, hipStream_t st) {
   const int list_rows = a.most * a.GL;
-  const TreeDims td = softmax_dims(dm, list_rows);
   const bool dense = a.page_idx == nullptr;
+  const TreeDims td = softmax_dims(dm, dense, a.L, list_rows);
   const int cus = device_compute_units();
   a.blocks = (list_rows + td.rows - 1) / td.rows;
-  const long long units = (long long)a.U * a.blocks, tokens = (long long)(dense ? dm.Mmax : dm.cap) * dm.P;
+  const long long units = (long long)a.U * a.blocks, tokens = list_tokens(dm, dense);
   // A block of rows whole by one workgroup, without prefix sums, records and join, where blocks are many and no list can be long.  Calls, us,
   // split / whole, a sequence's KV heads one unit: of 16 rows, 8 units of 200 tokens 12.4 / 13.0, of 2000 14.9 / 29.4, 128 of 1000 26.4 / 20.9, of
   // 2000 36.3 / 34.9, 256 of 1000 38.4 / 28.9, of 2000 56.9 / 47.4, 512 of 4000 175 / 161, of 8000 328 / 309; of 64 rows, 32 of 1000 24.3 / 32.0, 128
