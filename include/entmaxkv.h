@@ -417,8 +417,8 @@ ekv_status ekv_decode8_full_softmax(const ekv_config* cfg, const void* q, const 
  * parts of a fused projection need no copy.  w_q, w_k kv_dtype; freq float32 [n_freq]; pos int32 [n_tokens] (the pos of a token
  * map, as it is): a token with pos < 0 is passed over, its rows of q_out [n_tokens][Hq][d] and k_out [n_tokens][Hkv][d] are left
  * as they were (with pos NULL there is none).  Of cfg the head counts, head_dim and kv_dtype are used.
- * One launch, no workspace.  Range: n_freq a multiple of 8 up to 64, n_tokens * (Hq + Hkv) < 2^31 (else EKV_ERR_UNSUPPORTED);
- * eps finite and >= 0. */
+ * One launch, no workspace.  Range: n_freq a multiple of 8 up to 64, n_tokens <= 2^24 and n_tokens * (Hq + Hkv) < 2^31 (else
+ * EKV_ERR_UNSUPPORTED); eps finite and >= 0. */
 ekv_status ekv_norm_rotate(const ekv_config* cfg, const void* x_q, int64_t q_stride, const void* x_k, int64_t k_stride,
                            const void* w_q, const void* w_k, float eps, const float* freq, int32_t n_freq, const int32_t* pos,
                            int32_t n_tokens, int32_t pairs, void* q_out, void* k_out, void* stream);
@@ -429,7 +429,7 @@ ekv_status ekv_norm_rotate(const ekv_config* cfg, const void* x_q, int64_t q_str
  * (may be NULL) and tokens->seq / pos as there; a call may name a page in one run only.  box, gauss and, if given, box8 of page pos/P are written for
  * its tokens 0 .. t0 + run - 1 (t0: the run's first token in the page), bit for bit what ekv_stats_build computes for them.  seq_lens and
  * block_table of `cache` are not read and may be NULL.  One launch, no workspace.
- * Range: max_tokens < 2^30 and max_tokens * Hkv < 2^31, else EKV_ERR_UNSUPPORTED. */
+ * Range: max_tokens * Hkv < 2^29, else EKV_ERR_UNSUPPORTED. */
 ekv_status ekv_cache_append(const ekv_config* cfg, const ekv_cache_view* cache, const ekv_stats_view* stats,
                             const ekv_token_map* tokens, const int32_t* rows, int32_t n_rows, const void* k_new, int64_t k_stride,
                             const void* v_new, int64_t v_stride, void* stream);
@@ -440,8 +440,9 @@ ekv_status ekv_cache_append(const ekv_config* cfg, const ekv_cache_view* cache, 
  *   start   int32 [B+1]: sequence b's rows are start[b] .. start[b+1]-1, the first max_tree of them at most
  *   visible uint64 [max_tokens]: bit i of a row's word: it sees row i of its sequence.  For a tree the row itself and the rows that
  *           it follows, (1 << i) | visible[parent]; for a chain the rows up to it.  Any other mask is as good, none of them too.
- * max_tree (1 .. 64) and max_tokens size grids and workspaces.  max_tokens is also the number of rows of q and of the outputs.  Entries of start
- * are clamped into [0, max_tokens] and kept ascending; rows of no sequence, behind start[B] or beyond max_tree, are neither read nor written. */
+ * max_tree (1 .. 64) and max_tokens size grids and workspaces.  max_tokens is also the number of rows of q and of the outputs.  start
+ * ascends; what does not, or lies outside [0, max_tokens], gives undefined values, no undefined access.  Rows of no sequence, behind start[B] or
+ * beyond max_tree, are neither read nor written. */
 typedef struct {
   const void* k_new;
   const void* v_new;
@@ -463,8 +464,9 @@ typedef struct {
  * What is hidden counts for nothing, infinities and NaN included.  Keys that are no number: the entmax calls pass them over, every
  * softmax that sees one is NaN.  (Softmax sums: values below 2^120 / (n 2^8) keep them finite, n keys.)
  * The workspace holds 4 bytes per row, query head and position for entmax (a capacity of a million tokens, 16 rows, 32 heads: 2.1 GB).
- * Range: as the single-token calls; the steps of all lists, B * lists * blocks of rows * tiles of 16 keys or more, and max_tokens * Hq < 2^31,
- * n_phys_pages * pool heads * P < 2^31 (8 bits: 2^30), else EKV_ERR_UNSUPPORTED. */
+ * Range: max_tree <= 64; max_tokens * Hq < 2^24; B * lists * ceil(max_tree * (Hq / lists) / 4) < 2^24; the tiles of all lists (B * lists *
+ * ceil(max_tree * (Hq / lists) / 16) * (capacity / 16 + 1) at most) < 2^31; n_phys_pages * pool heads * P < 2^31 (8 bits: 2^30); else
+ * EKV_ERR_UNSUPPORTED. */
 ekv_status ekv_tree_sparse(const ekv_config* cfg, const void* q, const ekv_cache_view* cache, const ekv_tree_view* tree,
                            const int32_t* page_idx, const int32_t* n_sel, float* out, float* tau, int32_t* supp, void* workspace,
                            size_t workspace_bytes, void* stream);

@@ -498,7 +498,7 @@ ekv_status ekv_norm_rotate(const ekv_config* cfg, const void* x_q, int64_t q_str
   const int64_t d = cfg->head_dim;
   if (q_stride < dm.Hq * d || k_stride < dm.Hkv * d || q_stride % 8 != 0 || k_stride % 8 != 0) return EKV_ERR_INVALID_ARG;
   if (q_out == x_q || q_out == x_k || k_out == x_q || k_out == x_k || q_out == k_out) return EKV_ERR_INVALID_ARG;
-  if (n_freq % 8 != 0 || n_freq > d / 2 || (int64_t)n_tokens * (dm.Hq + dm.Hkv) > 0x7fffffff) return EKV_ERR_UNSUPPORTED;
+  if (n_freq % 8 != 0 || n_freq > d / 2 || n_tokens > 1 << 24 || (int64_t)n_tokens * (dm.Hq + dm.Hkv) > 0x7fffffff) return EKV_ERR_UNSUPPORTED;
   launch_norm_rotate(dm, x_q, q_stride, x_k, k_stride, w_q, w_k, eps, freq, n_freq, pos, n_tokens, pairs != 0, q_out, k_out,
                      (hipStream_t)stream);
   return finish((hipStream_t)stream);
@@ -520,7 +520,7 @@ ekv_status ekv_cache_append(const ekv_config* cfg, const ekv_cache_view* cache, 
     if (!ok_ptr(stats->box) || !ok_ptr(stats->gauss) || !ok_ptr4(tokens->seq) || !ok_ptr4(tokens->pos)) return EKV_ERR_INVALID_ARG;
     if ((s = check_box8(dm, stats, false)) != EKV_OK) return s;
   }
-  if (tokens->max_tokens >= 1 << 30 || (int64_t)tokens->max_tokens * dm.Hkv > 0x7fffffff) return EKV_ERR_UNSUPPORTED;
+  if ((int64_t)tokens->max_tokens * dm.Hkv >= 1 << 29) return EKV_ERR_UNSUPPORTED;      // threads of a launch are counted in 32 bits
   launch_cache_append(dm, *cache, stats, *tokens, rows, n_rows, k_new, k_stride, v_new, v_stride, (hipStream_t)stream);
   return finish((hipStream_t)stream);
 }
@@ -532,8 +532,8 @@ static ekv_status check_tree_sizes(int32_t max_tokens, int32_t max_tree) {
 // lists: kPerHead, kAllPages or kGroupList
 static bool tree_supported(const Dims& dm, int lists, bool entmax, int n_tokens, int most) {
   const int L = lists == kPerHead ? dm.Hq : dm.Hkv;
-  if (entmax) return tree_entmax_supported(dm, lists == kAllPages, L, n_tokens, most);
-  return tree_softmax_supported(dm, lists == kAllPages, L, most) && (int64_t)n_tokens * dm.Hq <= 0x7fffffff;
+  if ((int64_t)n_tokens * dm.Hq >= 1 << 24 || (int64_t)dm.B * L * ((most * (dm.Hq / L) + 3) / 4) >= 1 << 24) return false;
+  return entmax ? tree_entmax_supported(dm, lists == kAllPages, L, most) : tree_softmax_supported(dm, lists == kAllPages, L, most);
 }
 static size_t tree_ws_bytes(const Dims& dm, int lists, bool entmax, int n_tokens, int most) {
   const int L = lists == kAllPages ? dm.Hkv : dm.Hq;         // one size for lists per query head and per KV head

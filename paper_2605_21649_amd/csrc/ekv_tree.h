@@ -345,8 +345,9 @@ void launch_tree_solve(const Dims& dm, const TreeArgs& a, bool codes, int32_t* s
 void launch_tree_softmax(const Dims& dm, TreeArgs a, bool codes, void* ws, hipStream_t st);
 void launch_tree_entmax(const Dims& dm, TreeArgs a, bool codes, int32_t* supp, void* ws, hipStream_t st);
 // lists: page lists per sequence (query heads or KV heads), most: drafted rows of a sequence
-bool tree_softmax_supported(const Dims& dm, bool dense, int lists, int most);      // steps are counted in 31 bits
-bool tree_entmax_supported(const Dims& dm, bool dense, int lists, int n_tokens, int most);
+// steps are counted in 31 bits, threads of a launch in 32
+bool tree_softmax_supported(const Dims& dm, bool dense, int lists, int most);
+bool tree_entmax_supported(const Dims& dm, bool dense, int lists, int most);
 size_t tree_softmax_ws_bytes(const Dims& dm, bool dense, int lists, int most);
 size_t tree_entmax_ws_bytes(const Dims& dm, bool dense, int lists, int n_tokens);
 

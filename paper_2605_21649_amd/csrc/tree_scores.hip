@@ -219,8 +219,8 @@ static long long score_steps(const Dims& dm, bool dense, int lists, int list_row
 static int tree_groups(const Dims& dm, bool dense) {
   return (int)(((long long)(dense ? dm.Mmax : dm.cap) * dm.P + kGroup - 1) / kGroup) + 1;
 }
-bool tree_entmax_supported(const Dims& dm, bool dense, int lists, int n_tokens, int most) {
-  return score_steps(dm, dense, lists, most * (dm.Hq / lists)) <= 0x7fffffff && (long long)n_tokens * dm.Hq <= 0x7fffffff;
+bool tree_entmax_supported(const Dims& dm, bool dense, int lists, int most) {
+  return score_steps(dm, dense, lists, most * (dm.Hq / lists)) <= 0x7fffffff;
 }
 size_t tree_entmax_ws_bytes(const Dims& dm, bool dense, int lists, int n_tokens) {
   const size_t rows = (size_t)n_tokens * dm.Hq, groups = (size_t)tree_groups(dm, dense);

@@ -222,3 +222,59 @@ def test_graph_replays_and_another_stream(form, lens, trees):
         torch.cuda.synchronize()
         t.check(form, (d["out"].cpu(), d["norm"].cpu(), d["supp"].cpu()))
     assert all(torch.equal(d[x], y) for x, y in zip(("out", "norm", "supp"), first))
+
+
+@pytest.mark.parametrize("form", ["softmax", "entmax"])
+def test_nearly_as_many_lists_as_lds_holds_the_lengths_of(form):
+    t = Tree([(7 * i) % 50 for i in range(2040)], [1] * 2040, heads=(4, 4), page=16)
+    got = t.run(form)
+    keep = [0, 1, 7, 50, 1999, 2039]
+    t.trees = [1 if i in keep else 0 for i in range(2040)]
+    for x in got:
+        x[[i for i in range(2040) if i not in keep]] = 77
+    t.check(form, got)
+
+
+@pytest.mark.parametrize("form", ["softmax", "entmax"])
+@pytest.mark.parametrize("cache", ["same", "e4m3"])
+def test_pages_beyond_4_gb_of_a_pool(form, cache):
+    """The same pages at the far end of large pools, bit for bit."""
+    t = Tree([300, 77], [9, 3], heads=(4, 2), page=16, cache=cache)
+    near = t.run(form)
+    d = t.device(form)
+    per = 2 * 16 * D * (1 if cache == "e4m3" else 2)
+    n = (5 << 30) // per + 1
+    move = n - t.n_phys
+    big = [torch.zeros(n, *d["k"].shape[1:], dtype=d["k"].dtype, device="cuda") for _ in "kv"]
+    big[0][move:], big[1][move:] = d["k"], d["v"]
+    table = d["table"] + move
+    if cache == "e4m3":
+        scales = [torch.ones(n, 2, device="cuda") for _ in "kv"]
+        scales[0][move:], scales[1][move:] = d["ks"], d["vs"]
+        d["cache"] = ekv.cache8_view(*big, *scales, table, d["lens"])
+    else:
+        d["cache"] = ekv.cache_view(*big, table, d["lens"])
+    t.call(d, form)
+    torch.cuda.synchronize()
+    assert torch.equal(d["out"].cpu(), near[0]) and torch.equal(d["norm"].cpu(), near[1])
+
+
+@pytest.mark.parametrize("form", ["softmax", "entmax"])
+def test_the_same_bits_from_run_to_run(form):
+    t = Tree([9000, 4000], [40, 64], heads=(8, 2), seed=11)
+    first = t.run(form)
+    for _ in range(3):
+        assert all(torch.equal(x, y) for x, y in zip(first, t.run(form)))
+
+
+@pytest.mark.parametrize("alpha", [1.25, 1.5, 2.0, 2.7])
+@pytest.mark.parametrize("rising", [False, True])
+def test_groups_that_are_not_stored(alpha, rising):
+    """Long rows, most of whose groups a workgroup finds to be without weight; with scores that rise along the sequence none is."""
+    t = Tree([12000], [17], heads=(4, 1), alpha=alpha, seed=12, scale=0.15)
+    if rising:
+        lift = torch.zeros(t.n_phys)
+        lift[t.table[0].long()] = torch.arange(t.m).float() / t.m
+        t.k = (t.k.float() + 0.5 * lift[:, None, None, None] * t.q.float().mean((0, 1))).to(t.dt)
+        t.values[0] = t.k.double()
+    t.check("entmax", t.run("entmax"))
