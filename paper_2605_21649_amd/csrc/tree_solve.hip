@@ -75,7 +75,7 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
   // Row maximum and bound: by one wavefront where its registers hold all maxima (rows of up to 32 704 cached tokens), which then lists the
   // groups above the bound for all; else by all, several groups to a register where there are more than registers (their
   // mass is still no more than the row's), and every wavefront looks up its own.
-  const bool one = NW == 1 || groups < kOneGroups;
+  const bool one = NW == 1 || groups < kOneGroups;           // (with NW 1 there are 128 groups at most)
   float m[R], zmax = 0.f, bound = 0.f;
   bool folded = false;
   auto relative = [&](auto&& sums) {
@@ -86,13 +86,8 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
   };
   if (one) {
     if (w == 0) {
-      folded = groups >= kOneGroups;             // NW 1 alone
 #pragma unroll
       for (int k = 0; k < R; ++k) m[k] = k * 64 + lane <= groups ? zm[k * 64 + lane] : -INFINITY;
-      for (int g = kOneGroups + lane; g <= groups; g += kOneGroups) {
-#pragma unroll
-        for (int k = 0; k < R; ++k) m[k] = fmaxf(m[k], zm[min(g + k * 64, groups)]);
-      }
       float mx = m[0];
 #pragma unroll
       for (int k = 1; k < R; ++k) mx = fmaxf(mx, m[k]);
@@ -126,7 +121,10 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
       folded = groups >= R * NT;
       for (int g = R * NT + tid; g <= groups; g += R * NT) {
 #pragma unroll
-        for (int k = 0; k < R; ++k) m[k] = fmaxf(m[k], zm[min(g + k * NT, groups)]);
+        for (int k = 0; k < R; ++k) {            // a maximum counts once: what lies behind the last is not it again
+          const float x = zm[min(g + k * NT, groups)];
+          m[k] = g + k * NT <= groups ? fmaxf(m[k], x) : m[k];
+        }
       }
       float mx = m[0];
 #pragma unroll
@@ -190,7 +188,7 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
     if (in && o < SEG) { s_u[w][o] = u; s_at[w][o] = (uint32_t)pos; }
     count += __popcll(mk);
   };
-  if (one && !folded) {
+  if (one) {
     const int n_list = uniform(s_supp);
     for (int i = 4 * w; i < n_list; i += 4 * NW) {
       int g[4];
@@ -198,7 +196,7 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
       for (int k = 0; k < 4; ++k) g[k] = i + k < n_list ? uniform(s_list[min(i + k, n_list - 1)]) : -1;
       each_four(g, keep);
     }
-  } else if (one || folded) {
+  } else if (folded) {
     each_candidate(bound, keep);
   } else {
 #pragma unroll

@@ -259,22 +259,54 @@ def test_pages_beyond_4_gb_of_a_pool(form, cache):
     assert torch.equal(d["out"].cpu(), near[0]) and torch.equal(d["norm"].cpu(), near[1])
 
 
+def long_batch(rows, heads, alpha=1.5, rising=False):
+    """64 sequences of 94 groups of 64 keys: a workgroup goes through a dozen and more of them, so that it bounds rows and leaves groups out."""
+    t = Tree([6000 - 7 * i for i in range(64)], [rows] * 64, heads=heads, alpha=alpha, seed=12, scale=0.15)
+    if rising:                                             # scores that rise along the sequence: every group has the largest so far
+        lift = torch.zeros(t.n_phys)
+        for row in t.table:
+            pages = row[row >= 0].long()
+            lift[pages] = torch.arange(len(pages)) / t.m
+        t.k = (t.k.float() + 0.5 * lift[:, None, None, None] * t.q.float().mean((0, 1))).to(t.dt)
+        t.values[0] = t.k.double()
+    return t
+
+
+def check_some(t, form, got, keep):
+    """The sequences `keep` alone, the others' rows as if they were none's: the definition takes its time."""
+    start = t.start.tolist()
+    for b in range(t.b):
+        if b not in keep:
+            t.trees[b] = 0
+            for x in got:
+                x[start[b]:start[b + 1]] = 77
+    t.check(form, got)
+
+
 @pytest.mark.parametrize("form", ["softmax", "entmax"])
 def test_the_same_bits_from_run_to_run(form):
-    t = Tree([9000, 4000], [40, 64], heads=(8, 2), seed=11)
+    t = long_batch(40, (8, 2))
     first = t.run(form)
     for _ in range(3):
         assert all(torch.equal(x, y) for x, y in zip(first, t.run(form)))
 
 
+@pytest.mark.parametrize("rows,heads", [(17, (1, 1)), (30, (4, 1)), (40, (4, 1))])
 @pytest.mark.parametrize("alpha", [1.25, 1.5, 2.0, 2.7])
-@pytest.mark.parametrize("rising", [False, True])
-def test_groups_that_are_not_stored(alpha, rising):
-    """Long rows, most of whose groups a workgroup finds to be without weight; with scores that rise along the sequence none is."""
-    t = Tree([12000], [17], heads=(4, 1), alpha=alpha, seed=12, scale=0.15)
-    if rising:
-        lift = torch.zeros(t.n_phys)
-        lift[t.table[0].long()] = torch.arange(t.m).float() / t.m
-        t.k = (t.k.float() + 0.5 * lift[:, None, None, None] * t.q.float().mean((0, 1))).to(t.dt)
-        t.values[0] = t.k.double()
+def test_groups_that_are_not_stored(rows, heads, alpha):
+    t = long_batch(rows, heads, alpha)
+    check_some(t, "entmax", t.run("entmax"), (0, 63) if rows == 17 else (31,))
+
+
+@pytest.mark.parametrize("alpha", [1.5, 2.0])
+def test_scores_that_rise_along_the_sequence(alpha):
+    t = long_batch(18, (1, 1), alpha, rising=True)
+    check_some(t, "entmax", t.run("entmax"), (0, 30, 63))
+
+
+@pytest.mark.parametrize("length,others", [(262144 + 70, 0), (262144 - 1, 0), (131072 + 70, 600), (32768, 0), (32768, 600)])
+@pytest.mark.parametrize("alpha", [1.5, 2.0])
+def test_more_maxima_than_registers(length, others, alpha):
+    """Rows whose drafted key has the largest score: it counts once, however the maxima are folded; with few rows in the call and with many."""
+    t = Tree([length], [4], heads=(1, 1), alpha=alpha, seed=13, extra_rows=others)
     t.check("entmax", t.run("entmax"))
