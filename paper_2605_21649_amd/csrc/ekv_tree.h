@@ -74,6 +74,26 @@ __device__ __forceinline__ TreeList tree_list(const TreeArgs& A, int u) {
   return l;
 }
 
+// Entmax scores of a list, [group of 64 keys][row][key]: what a workgroup stores of a group is in one piece.  (Rows one after the other, us
+// before / now: 64 rows a KV head, 128K tokens 144 / 125, 2 of 128K 233 / 213, 8 of 32K 186 / 185, 4 of 128K 326 / 330; 256 rows, 128K
+// 314 / 273.)  The lists of a sequence lie in the place of its rows.
+constexpr int kGroup = 64;
+struct TreeScores { float* z; size_t group; };           // floats from a group to the next
+__device__ __forceinline__ TreeScores tree_z(const TreeArgs& A, const TreeList& l, int u) {
+  const size_t rows = (size_t)l.R.count * A.GL;
+  return {A.z + (l.R.first * (size_t)A.Hq + (u - l.b * A.L) * rows) * A.zstride, rows * kGroup};
+}
+
+// Largest value and sum of the four lanes (c, 0..3) of a column, in all four: two exchanges between registers, where __shfl_xor goes by LDS.
+template <typename F> __device__ __forceinline__ float over_column(float x, F&& f) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float column_max(float x) { return over_column(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float column_sum(float x) { return over_column(x, [](float a, float b) { return a + b; }); }
+
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 __device__ __forceinline__ s16x4_t read_transposed(const char* p) {

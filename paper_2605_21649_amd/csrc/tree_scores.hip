@@ -10,8 +10,6 @@
 
 namespace ekv {
 
-constexpr int kGroup = 64;                       // keys per maximum
-
 template <typename TQ, typename TC, int NQ, int WQ, bool LISTS>
 __global__ __launch_bounds__(64 * (WQ == 1 ? 4 : WQ)) __attribute__((amdgpu_waves_per_eu(WQ == 1 ? 3 : WQ == 8 && NQ == 1 ? 4 : 2)))
 void tree_scores_kernel(const TreeArgs A) {
@@ -28,6 +26,7 @@ void tree_scores_kernel(const TreeArgs A) {
     const int list_head = list.head, hkv = list.hkv;
     const int n_rows = R.count * A.GL;
     const int r0 = blk * S::kRows + (WQ > 1 ? w * 16 * NQ : 0);
+    const TreeScores scores = tree_z(A, list, unit);
     TreeQuery<TQ, NQ> q;
     float* z[NQ]; float* zmax[NQ];
     bool there[NQ];
@@ -36,7 +35,7 @@ void tree_scores_kernel(const TreeArgs A) {
       const int r = min(r0 + 16 * t + c, n_rows - 1), tok = r / A.GL;
       const size_t at = (size_t)(R.first + tok) * A.Hq + list_head + (r - tok * A.GL);
       there[t] = r0 + 16 * t + c < n_rows;
-      z[t] = A.z + at * A.zstride + 4 * j;
+      z[t] = scores.z + min(r0 + 16 * t + c, n_rows - 1) * kGroup + 4 * j;
       zmax[t] = A.zmax + at * A.n_groups;
     }
     // a group's share of the steps, as tiles of the cache (the drafted keys are the last one's)
@@ -64,6 +63,7 @@ void tree_scores_kernel(const TreeArgs A) {
     float top[NQ];
     constexpr bool kHold = WQ > 1 && kPer == 1;
     constexpr int kSlots = 8;                              // maxima of a row: kSlots in each of its four lanes
+    float held_top[kHold ? NQ : 1][4];                     // maxima of sixteen groups, lane (c, j) has those of 4j..4j+3
     float slot[kHold ? NQ : 1][kSlots], bound[kHold ? NQ : 1], most[kHold ? NQ : 1];
     if constexpr (kHold) {
 #pragma unroll
@@ -94,8 +94,7 @@ void tree_scores_kernel(const TreeArgs A) {
         }
         bool store = there[i];
         if constexpr (kHold && !kDrafted) {
-          top[i] = fmaxf(top[i], __shfl_xor(top[i], 16));
-          top[i] = fmaxf(top[i], __shfl_xor(top[i], 32));
+          top[i] = column_max(top[i]);
           if (top[i] <= bound[i]) { store = false; top[i] = -INFINITY; }
         }
         if (store) {
@@ -111,8 +110,7 @@ void tree_scores_kernel(const TreeArgs A) {
     auto store_top = [&](int group) {
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
-        float x = fmaxf(top[i], __shfl_xor(top[i], 16));
-        x = fmaxf(x, __shfl_xor(x, 32));
+        const float x = column_max(top[i]);
         if (j == 0 && there[i]) zmax[i][group] = x;
       }
     };
@@ -124,16 +122,26 @@ void tree_scores_kernel(const TreeArgs A) {
     };
     auto work = [&](const char* k, int t, uint64_t valid) {
       if (kPer == 1 || t % kPer == 0) clear_top();
-      score(k, (size_t)t * S::kKeys, IntC<0>{}, valid, none);
+      score(k, t / kPer * scores.group + t % kPer * S::kKeys, IntC<0>{}, valid, none);
       if constexpr (kHold) {
         const int seen_groups = t - t0, at = (seen_groups >> 2) & (kSlots - 1);
         const bool mine = j == (seen_groups & 3);
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
-          if (j == 0 && there[i]) zmax[i][t] = top[i];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) held_top[i][k] = j == (t >> 2 & 3) && k == (t & 3) ? top[i] : held_top[i][k];
           most[i] = fmaxf(most[i], top[i]);
 #pragma unroll
           for (int k = 0; k < kSlots; ++k) slot[i][k] = mine && k == at ? fmaxf(slot[i][k], top[i]) : slot[i][k];
+        }
+        if ((t & 15) == 15 || t == t1 - 1) {               // sixteen maxima of a row at a time, four in each of its lanes
+          const int g0 = (t & ~15) + 4 * j;
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (there[i] && g0 + k >= t0 && g0 + k <= t) zmax[i][g0 + k] = held_top[i][k];
+          }
         }
         if ((seen_groups & 7) == 7) {                      // wave-uniform
 #pragma unroll
@@ -145,8 +153,7 @@ void tree_scores_kernel(const TreeArgs A) {
             // one key alone has mass 1 a step of 1 below it; the bound of fewer maxima is one of more
             const float from = fmaxf(bound[i] + eps - most[i], -1.0f - eps);
             const float b = group_bound(u, from, A.beta, A.ibeta, [&](float& f, float& d) {
-              f += __shfl_xor(f, 16); d += __shfl_xor(d, 16);
-              f += __shfl_xor(f, 32); d += __shfl_xor(d, 32);
+              f = column_sum(f); d = column_sum(d);
             });
             if (most[i] > -INFINITY) bound[i] = fmaxf(bound[i], b + most[i] - eps);
           }
@@ -195,7 +202,7 @@ void tree_scores_kernel(const TreeArgs A) {
           seen[i] = (A.visible[R.first + r / A.GL] >> d0) & there_keys;
         }
         if constexpr (WQ > 1) __syncthreads(); else wave_order();
-        score(tile, (size_t)(steps - 1) * kGroup + d0, IntC<1>{}, 0, seen);
+        score(tile, (steps - 1) * scores.group + d0, IntC<1>{}, 0, seen);
       }
       store_top(steps - 1);
     }
@@ -237,7 +244,11 @@ static void launch_scores_T(const Dims& dm, TreeArgs& a, hipStream_t st) {
   const int list_rows = a.most * a.GL, rows = score_rows(dm, list_rows);
   a.blocks = (list_rows + rows - 1) / rows;
   const long long steps = score_steps(dm, a.page_idx == nullptr, a.L, list_rows);
-  const int most = (rows == 256 ? 1 : rows == 16 ? 3 : 2) * device_compute_units();
+  // Workgroups per compute unit.  A second and third one of four wavefronts share the waiting, but each goes through less of a row and bounds it
+  // less closely.  us, two / three: lists of 512 8-bit keys, 64 sequences 40.2 / 39.3, 8 of 4096 tokens 49.3 / 48.1, 64 of 1024 61.7 / 62.7, 128K
+  // 125 / 131, 4 of 128K 330 / 347; float32, which stores all, 4 of 64K 381 / 364.
+  const bool third = rows == 16 || (rows == 64 && (dm.dtype == EKV_F32 || steps <= 8192));
+  const int most = (rows == 256 ? 1 : third ? 3 : 2) * device_compute_units();
   a.W = (int)(steps < most ? steps : most);
   size_t lds = 0;
   if (a.U > kUnitsLdsMax) {

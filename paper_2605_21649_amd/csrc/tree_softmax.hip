@@ -69,9 +69,7 @@ template <typename TQ, int NQ, int TILES> struct TreeSoftmax {
     if (__any(higher)) {
 #pragma unroll
       for (int t = 0; t < NQ; ++t) {
-        float x = fmaxf(top[t], __shfl_xor(top[t], 16));
-        x = fmaxf(x, __shfl_xor(x, 32));
-        const float now = fmaxf(m[t], x), f = now > -INFINITY ? __builtin_amdgcn_exp2f(m[t] - now) : 1.f;
+        const float now = fmaxf(m[t], column_max(top[t])), f = now > -INFINITY ? __builtin_amdgcn_exp2f(m[t] - now) : 1.f;
         m[t] = now;
         l[t] *= f;
 #pragma unroll
@@ -316,10 +314,7 @@ void tree_softmax_kernel(const TreeArgs A) {
     }
     // the rows' sums
 #pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-      acc.l[t] += __shfl_xor(acc.l[t], 16);
-      acc.l[t] += __shfl_xor(acc.l[t], 32);
-    }
+    for (int t = 0; t < NQ; ++t) acc.l[t] = column_sum(acc.l[t]);
     const bool whole = st0 == 0 && st1 == steps;
     float* rec = A.part + tree_rec(S::kRows) * (2 * (size_t)wg + (first ? 0 : 1));
     auto put = [&](int r, int ch, float4 o, float m, float l) {            // four channels of row r of the block

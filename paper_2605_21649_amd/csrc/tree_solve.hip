@@ -10,8 +10,6 @@
 
 namespace ekv {
 
-constexpr int kGroup = 64;
-
 struct TreeSolveArgs {
   TreeArgs t;
   int32_t* supp;
@@ -69,9 +67,10 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
   const TreeRows T = list.R;
   if (n < T.first || n >= T.first + T.count) return;         // of no sequence
   const int groups = (list.n_pos + kGroup - 1) / kGroup;     // of the cache; one more of drafted keys
-  const float* z = A.z + (size_t)row * A.zstride;
+  const TreeScores scores = tree_z(A, list, unit);
+  const float* z = scores.z + ((n - T.first) * A.GL + hq - list.head) * kGroup;
   const float* zm = A.zmax + (size_t)row * A.n_groups;
-  const float zd = lane < T.count ? z[(size_t)groups * kGroup + lane] : -INFINITY;
+  const float zd = lane < T.count ? z[groups * scores.group + lane] : -INFINITY;
   // Row maximum and bound: by one wavefront where its registers hold all maxima (rows of up to 32 704 cached tokens), which then lists the
   // groups above the bound for all; else by all, several groups to a register where there are more than registers (their
   // mass is still no more than the row's), and every wavefront looks up its own.
@@ -155,7 +154,7 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
   auto each_four = [&](const int (&g)[4], auto&& each) {
     float zz[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) zz[k] = z[(size_t)max(g[k], 0) * kGroup + lane];
+    for (int k = 0; k < 4; ++k) zz[k] = z[max(g[k], 0) * scores.group + lane];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if (g[k] < 0) break;
@@ -347,10 +346,7 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
     add_rows((const TQ*)A.v_new + T.first * A.vs + list.hkv * kD, A.vs, s_u[w], s_at[w], __popcll(mk), acc, [](float p, uint32_t) { return p; });
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    acc[i] += __shfl_xor(acc[i], 16);
-    acc[i] += __shfl_xor(acc[i], 32);
-  }
+  for (int i = 0; i < 8; ++i) acc[i] = column_sum(acc[i]);
   if constexpr (NW == 1) {
     if (lane < 16) store8(out + 8 * lane, acc);
   } else {
