@@ -310,3 +310,11 @@ def test_more_maxima_than_registers(length, others, alpha):
     """Rows whose drafted key has the largest score: it counts once, however the maxima are folded; with few rows in the call and with many."""
     t = Tree([length], [4], heads=(1, 1), alpha=alpha, seed=13, extra_rows=others)
     t.check("entmax", t.run("entmax"))
+
+
+@pytest.mark.parametrize("length,others", [(40000, 0), (40000, 600), (8000, 2100), (140000, 600)])
+@pytest.mark.parametrize("alpha", [1.05, 1.1, 1.25])
+def test_rows_with_thousands_of_candidates(length, others, alpha):
+    """Flat rows: more candidates than a workgroup keeps at its first try, or at any; with few rows in the call, with many, with very many."""
+    t = Tree([length], [3], heads=(1, 1), alpha=alpha, seed=14, extra_rows=others)
+    t.check("entmax", t.run("entmax"))
