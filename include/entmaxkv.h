@@ -417,8 +417,8 @@ ekv_status ekv_decode8_full_softmax(const ekv_config* cfg, const void* q, const 
  * parts of a fused projection need no copy.  w_q, w_k kv_dtype; freq float32 [n_freq]; pos int32 [n_tokens] (the pos of a token
  * map, as it is): a token with pos < 0 is passed over, its rows of q_out [n_tokens][Hq][d] and k_out [n_tokens][Hkv][d] are left
  * as they were (with pos NULL there is none).  Of cfg the head counts, head_dim and kv_dtype are used.
- * One launch, no workspace.  Range: n_freq a multiple of 8 up to 64, n_tokens <= 2^24 and n_tokens * (Hq + Hkv) < 2^31 (else
- * EKV_ERR_UNSUPPORTED); eps finite and >= 0. */
+ * Outputs lie apart from the inputs.  One launch, no workspace.  Range: n_freq a multiple of 8 up to 64, n_tokens <= 2^24 and
+ * n_tokens * (Hq + Hkv) < 2^31 (else EKV_ERR_UNSUPPORTED); eps finite and >= 0. */
 ekv_status ekv_norm_rotate(const ekv_config* cfg, const void* x_q, int64_t q_stride, const void* x_k, int64_t k_stride,
                            const void* w_q, const void* w_k, float eps, const float* freq, int32_t n_freq, const int32_t* pos,
                            int32_t n_tokens, int32_t pairs, void* q_out, void* k_out, void* stream);

@@ -9,7 +9,7 @@
 // Keys and values pass through LDS once for all rows of a workgroup: rows of a tile lie at their length, their 16-byte pieces in an
 // order that their number turns (piece ^ row % 16), so that neither sixteen rows' same piece nor the transposing reads of V
 // meet in a bank.  An 8-bit cache's codes become bf16 or float32 with their page's scale (exact) on the way into LDS.
-// Two kinds of shape: up to 16 rows: every wavefront has all of them and keys of its own, nothing is waited for together; more: four
+// Two kinds of shape: up to 16 rows: every wavefront has all of them and keys of its own, nothing is waited for together; more: two, four
 // or eight wavefronts share the keys, twice a tile's in LDS so that they meet once a tile, and have 16 or 32 rows each.  (17 to 32
 // rows, two tiles of them in every wavefront with keys of its own: registers spill, and a spilled one read back waits for all loads
 // under way; lists of 4 x 128K tokens, 32 rows, softmax 97 us, by four wavefronts that share, half of them idle, 83.)
@@ -101,12 +101,12 @@ __device__ __forceinline__ s16x4_t read_transposed(const char* p) {
 }
 
 // How a workgroup divides rows and keys.  TQ: type of queries and drafted rows, which the products have; TC: of the cache.  NQ: tiles of 16
-// rows a wavefront, WQ: wavefronts that share the keys (1: none of four; 4 or 8: all).  SIDES: K alone or K and V.
+// rows a wavefront, WQ: wavefronts that share the keys (1: none of four; 2, 4 or 8: all).  SIDES: K alone or K and V.
 template <typename TQ, typename TC, int NQ, int WQ, int SIDES> struct TreeShape {
   static constexpr int kWaves = WQ == 1 ? 4 : WQ, kWork = 64 * kWaves;   // of the workgroup
   static constexpr int kGroups = kWaves / WQ;                            // groups of wavefronts with keys of their own
   static constexpr int kRows = 16 * NQ * WQ;                             // rows of a workgroup
-  static constexpr int kKeys = (WQ == 1 ? 32 : 64) * 2 / (int)sizeof(TQ);       // keys of a tile
+  static constexpr int kKeys = (WQ == 1 || WQ == 2 && SIDES == 2 ? 32 : 64) * 2 / (int)sizeof(TQ);       // keys of a tile
   static constexpr int kTiles = kKeys / 16;
   static constexpr int kRowBytes = kD * (int)sizeof(TQ);
   static constexpr int kSideBytes = kKeys * kRowBytes;

@@ -452,18 +452,22 @@ void launch_tree_prefix(const TreeArgs& a, int keys, int rows, hipStream_t st) {
 }
 
 // ------------------------------------------------------------------------------------------
-constexpr int kTreeWgs = 512;                    // workgroups of a launch at most; workspaces are sized for them
+// workgroups of a launch at most; workspaces are sized for them
+static int most_wgs(int rows) { return rows == 32 ? 1024 : 512; }
 
 struct TreeDims { int rows, keys; };             // of a workgroup, of a tile
 static long long list_tokens(const Dims& dm, bool dense) { return (long long)(dense ? dm.Mmax : dm.cap) * dm.P; }
 // Blocks as large as the rows of a list, or of 64 rows where there is so little to go through that more workgroups count for more than reading
 // keys once.  Calls, us, blocks of 64 / of 128 / of 256 rows: lists of 256 rows, 8 of 4000 tokens 27 / 38 / 34, 16 of 2049 8-bit 24 / 30 / 28, 64 of
 // 1000 35 / 57 / 53, 32 of 4000 57 / 64 / 54, 16 of 32000 184 / 177 / 149, 64 of 16000 312 / 290 / 238; of 128 rows, 64 of 4096 57 / 71, 32 of 8000
-// 65 / 73, 8 of 128000 205 / 184.
+// 65 / 73, 8 of 128000 205 / 184.  17 to 32 rows over every page: by two wavefronts, tiles of 32 keys, where there is enough.  Blocks of 64 / of 32:
+// 16 caches of 2049 tokens 19.3 / 22.9, 8 of 4096 23.7 / 24.7, of 32 768 49.5 / 47.0, of 131 072 119 / 114, 32 of 8192 44.0 / 43.0, of 131 072 411 / 378,
+// 64 of 4096 8-bit 36.8 / 31.6, 512 of 1024 56 / 55; page lists, 128 of 5243 84.5 / 85.5.
 static TreeDims softmax_dims(const Dims& dm, bool dense, int lists, int list_rows) {
   if (dm.dtype == EKV_F32) return list_rows <= 16 ? TreeDims{16, 16} : TreeDims{64, 32};
   if (list_rows <= 16) return {16, 32};
   const long long all = list_tokens(dm, dense) * dm.B * lists;
+  if (list_rows <= 32 && dense && all > 1ll << 17) return {32, 32};
   if (list_rows <= 64 || all <= (list_rows <= 128 ? 1ll << 19 : 3ll << 15)) return {64, 64};
   return {list_rows <= 128 ? 128 : 256, 64};
 }
@@ -476,7 +480,7 @@ bool tree_softmax_supported(const Dims& dm, bool dense, int lists, int most) {
 }
 size_t tree_softmax_ws_bytes(const Dims& dm, bool dense, int lists, int most) {
   const TreeDims td = softmax_dims(dm, dense, lists, most * (dm.Hq / lists));
-  return tree_pre_bytes((size_t)dm.B * lists) + 2 * kTreeWgs * tree_rec(td.rows) * sizeof(float);
+  return tree_pre_bytes((size_t)dm.B * lists) + 2 * most_wgs(td.rows) * tree_rec(td.rows) * sizeof(float);
 }
 
 template <typename TQ, typename TC, int NQ, int WQ>
@@ -500,7 +504,9 @@ static void launch_softmax_T(const Dims& dm, TreeArgs a, hipStream_t st) {
   const long long whole = units >= 2 * cus ? 8192 : units >= cus ? (td.rows == 16 ? 8192 : 2048) : units >= cus / 2 && td.rows == 16 ? 2048 : 0;
   a.per_unit = tokens <= whole;
   const long long steps = softmax_steps(dm, dense, a.L, list_rows);
-  const int most = (td.rows == 256 ? 1 : 2) * cus < kTreeWgs ? (td.rows == 256 ? 1 : 2) * cus : kTreeWgs, share = td.rows == 16 ? 4 : 1;
+  // 32 rows: four workgroups a compute unit where a block of rows is not in so many pieces that the join takes longer.
+  const bool four = td.rows == 32 && units >= 64;
+  const int per_cu = td.rows == 256 ? 1 : four ? 4 : 2, most = per_cu * cus < most_wgs(td.rows) ? per_cu * cus : most_wgs(td.rows), share = td.rows == 16 ? 4 : 1;
   const long long wgs = (steps + share - 1) / share;
   a.W = (int)(wgs < most ? wgs : most);
   size_t lds = 0;
@@ -516,6 +522,7 @@ static void launch_softmax_T(const Dims& dm, TreeArgs a, hipStream_t st) {
   if (td.rows == 16) launch_softmax_shape<TQ, TC, 1, 1>(a, grid, lds, st);
   else if (td.rows == 64) launch_softmax_shape<TQ, TC, 1, 4>(a, grid, lds, st);
   if constexpr (sizeof(TQ) == 2) {
+    if (td.rows == 32) launch_softmax_shape<TQ, TC, 1, 2>(a, grid, lds, st);
     if (td.rows == 128) launch_softmax_shape<TQ, TC, 1, 8>(a, grid, lds, st);
     else if (td.rows == 256) launch_softmax_shape<TQ, TC, 2, 8>(a, grid, lds, st);
   }

@@ -318,3 +318,30 @@ def test_rows_with_thousands_of_candidates(length, others, alpha):
     """Flat rows: more candidates than a workgroup keeps at its first try, or at any; with few rows in the call, with many, with very many."""
     t = Tree([length], [3], heads=(1, 1), alpha=alpha, seed=14, extra_rows=others)
     t.check("entmax", t.run("entmax"))
+
+
+@pytest.mark.parametrize("lens,heads,cache", [([19000], (8, 8), "same"), ([3000] * 70, (4, 1), "same"), ([5000, 0, 4100, 4999] * 9, (4, 1), "e4m3")])
+def test_softmax_of_32_rows_by_two_wavefronts(lens, heads, cache):
+    t = Tree(lens, [20 if heads[1] == 8 else 7] * len(lens), heads=heads, cache=cache, seed=15)
+    check_some(t, "softmax", t.run("softmax"), (0, 1, 2, len(lens) - 1))
+
+
+@pytest.mark.parametrize("form", ["softmax", "entmax"])
+def test_two_graphs_that_share_a_workspace(form):
+    a, b = Tree([700, 90], [9, 4], heads=(4, 2), seed=16), Tree([40, 2000], [3, 16], heads=(4, 2), seed=17)
+    da, db = a.device(form), b.device(form)
+    db["ws"] = da["ws"] = max(da["ws"], db["ws"], key=lambda w: w.numel())
+    graphs = []
+    for t, d in ((a, da), (b, db)):
+        t.call(d, form)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            t.call(d, form)
+    for _ in range(3):
+        for t, d, g in ((a, da, graphs[0]), (b, db, graphs[1])):
+            for x in ("out", "norm", "supp"):
+                d[x].fill_(77)
+            g.replay()
+            torch.cuda.synchronize()
+            t.check(form, (d["out"].cpu(), d["norm"].cpu(), d["supp"].cpu()))
