@@ -3,6 +3,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include "ekv_search.h"
 
 namespace ekv {
 
@@ -328,21 +329,17 @@ __device__ __forceinline__ void block_exclusive_prefix(int U, F&& count_of, int*
   __syncthreads();
 }
 
-// The last of entries [0, n) of the ascending pre that is not above v (pre[0] <= v), the same for the whole wavefront: 64 entries
+// The last of entries [0, n) of the ascending pre that is not above v, entry 0 if all are, the same for the whole wavefront: 64 entries
 // compared at a time, so one LDS latency up to 64 entries and two up to 4096, where halving the range takes six and twelve.
 // Every launch over lists begins with the prefix of their lengths and this search.  By LDS permutes and halving, and with the
 // solve's segment ends so too, decode calls took 0.4 to 0.6 us more: over shared lists of 328 pages of 262144 tokens 12.9 -> 12.5 us,
 // of 16 pages for 64 sequences 17.8 -> 17.3, lists per head of 328 17.6 -> 17.0.
 template <typename P> __device__ __forceinline__ int wave_last_at_most(const P pre, int n, int v) {
   const int lane = threadIdx.x & 63;
-  int lo = 0;
-  while (n > 1) {
-    const int step = (n + 63) >> 6, at = lane * step;
-    const int k = __popcll(__ballot(at < n && pre[lo + min(at, n - 1)] <= v)) - 1;
-    lo += k * step;
-    n = min(step, n - k * step);
-  }
-  return lo;
+  return last_at_most_by_64(n, [&](int lo, int left, int step) {
+    const int at = lane * step;
+    return __popcll(__ballot(at < left && pre[lo + min(at, left - 1)] <= v));
+  });
 }
 // The same for ascending values of the lanes, v <= last in every lane; first: any entry not above all of them.
 template <typename P> __device__ __forceinline__ int lane_last_at_most(const P pre, int n, int first, int v, int last) {

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
   // consecutive rows, the heads of a token, on one XCD
   const int row = gridDim.x % kXcds == 0 ? (int)(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
   const int n = row / A.Hq, hq = row - n * A.Hq;
-  const int b = uniform(wave_last_at_most(A.start, A.B, n));
+  const int b = uniform(wave_last_at_most(A.start, A.B, n));   // sequence 0 for rows in front of its first: they are none's
   const int unit = b * A.L + hq / A.GL;
   const TreeList list = tree_list(A, unit);
   const TreeRows T = list.R;
