@@ -424,7 +424,7 @@ def ekv_cache_append(cfg, cache, stats, tokens, k_new, v_new, rows=None, stream=
 
 def tree_view(start, visible, k_new, v_new, max_tree):
     """Drafted rows: k_new, v_new [max_tokens][Hkv][d] (may be parts of longer rows), start int32 [B + 1], visible int64 [max_tokens],
-    the 64 bits of a row's mask."""
+    the 64 bits of a row's mask.  The view holds the tensors: it is used in several calls, and masks are made for it alone."""
     kn, vn = k_new.shape, v_new.shape
     (k, ks), (v, vs) = _rows(k_new, kn), _rows(v_new, vn)
     assert kn == vn and k_new.dtype is v_new.dtype, "drafted keys and values of one shape and type"
@@ -432,6 +432,7 @@ def tree_view(start, visible, k_new, v_new, max_tree):
     assert visible.numel() == kn[0], "a mask for every drafted row"
     tree = ekv_tree_view(k, v, ks, vs, _ptr(start), _ptr(visible), kn[0], max_tree)
     tree.of = (kn[1], kn[2], k_new.dtype, start.numel())      # what the calls check against their config
+    tree.holds = (start, visible, k_new, v_new)
     return tree
 
 
