@@ -462,7 +462,10 @@ typedef struct {
  * A row that sees nothing (an empty cache or list, no drafted row) has a zero output, tau = +inf, an empty support, lse = -inf.
  * Scores, thresholds, sums and outputs are float32 sums of exact products, as in the single-token calls, in another order.
  * What is hidden counts for nothing, infinities and NaN included.  Keys that are no number: the entmax calls pass them over, every
- * softmax that sees one is NaN.  (Softmax sums: values below 2^120 / (n 2^8) keep them finite, n keys.)
+ * softmax that sees one is NaN.  (Softmax sums: values below 2^120 / (n 2^8) keep them finite, n keys.)  A score of +inf (an infinity in the
+ * key, or a sum beyond float32) has no threshold: entmax gives the row a zero output, an empty support and tau = NaN, softmax NaN; one of
+ * -inf has no weight.  Infinite values of the cache: entmax has the infinity where the key has weight; softmax with bf16 queries takes
+ * a weight in three terms, of which one may be zero, so the channel is infinite or NaN, with the other channels as they are.
  * The workspace holds 4 bytes per row, query head and position for entmax (a capacity of a million tokens, 16 rows, 32 heads: 2.1 GB).
  * Range: max_tree <= 64; max_tokens * Hq < 2^24; B * lists * ceil(max_tree * (Hq / lists) / 4) < 2^24; the tiles of all lists (B * lists *
  * ceil(max_tree * (Hq / lists) / 16) * (capacity / 16 + 1) at most) < 2^31; n_phys_pages * pool heads * P < 2^31 (8 bits: 2^30); else

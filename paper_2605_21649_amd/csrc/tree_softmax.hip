@@ -7,6 +7,8 @@
 // products, as in the single-token call.  The maximum only has to keep exp in range: it moves when a score passes it by 2^kSlack.
 // What a mask hides counts for nothing, infinities and NaN in its value among them: such drafted values are taken out of the
 // product (0 * NaN) and added by themselves to the rows that see them.
+// An infinite value of the cache, which no mask hides, stays in the product: its channel is infinite, or NaN where one of the weight's terms is
+// zero (looking for one in every tile would cost every call).
 // Bound by the bytes with few rows (lists of 4 x 5243 tokens, 32 rows, 347 MB: 77 us, 4.5 TB/s) and by the products with many: 256 rows, 8 x
 // 32K tokens, 0.37 TFLOP with the three terms in 395 us, 0.94 PFLOP/s, matrix units 53 % busy (a library product of 8192^2 bf16 matrices: 1.37).
 #include "ekv_tree.h"
