@@ -213,8 +213,6 @@ void tree_scores_kernel(const TreeArgs A) {
 }
 
 // ------------------------------------------------------------------------------------------
-constexpr int kScoreWgs = 1024;
-
 static int score_rows(const Dims& dm, int list_rows) {
   if (list_rows <= 16) return 16;
   if (dm.dtype == EKV_F32) return 64;
