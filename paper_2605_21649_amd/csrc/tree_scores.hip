@@ -5,7 +5,7 @@
 // a workgroup keeps a lower bound of every row's threshold, the root of the mass of the maxima that it has seen (32 a row, several
 // groups folded into one), and a group none of whose keys is above it is not stored: its maximum is put down as -inf, nobody will read it.
 // The drafted keys are a row's last group.  Hidden and missing keys score -inf.
-// 64 rows a KV head, 4 x 128K tokens (977 MB of K): 305 us, 232 with no score stored, 4.2 TB/s; lists of 21 000 tokens, 16 rows, 176 MB:
+// 64 rows a KV head, 4 x 128K tokens, 963 MB of K: 305 us, 232 (4.15 TB/s) with no score stored; 32 lists of 21 000 tokens, 16 rows, 172 MB of K:
 // 51 us, 3.4 TB/s, seven tiles to a wavefront.
 #include "ekv_solve.h"
 #include "ekv_tree.h"

@@ -10,7 +10,7 @@
 // An infinite value of the cache, which no mask hides, stays in the product: its channel is infinite, or NaN where one of the weight's terms is
 // zero (looking for one in every tile would cost every call).
 // Bound by the bytes with few rows (lists of 4 x 5243 tokens, 32 rows, 347 MB: 77 us, 4.5 TB/s) and by the products with many: 256 rows, 8 x
-// 32K tokens, 0.37 TFLOP with the three terms in 395 us, 0.94 PFLOP/s, matrix units 53 % busy (a library product of 8192^2 bf16 matrices: 1.37).
+// 32K tokens, 0.37 TFLOP with the three terms in 395 us (the call's 412 without the join), 0.94 PFLOP/s, matrix units 53 % busy (a library product of 8192^2 bf16 matrices: 1.37).
 #include "ekv_tree.h"
 
 namespace ekv {
@@ -506,7 +506,9 @@ static void launch_softmax_T(const Dims& dm, TreeArgs a, hipStream_t st) {
   const long long whole = units >= 2 * cus ? 8192 : units >= cus ? (td.rows == 16 ? 8192 : 2048) : units >= cus / 2 && td.rows == 16 ? 2048 : 0;
   a.per_unit = tokens <= whole;
   const long long steps = softmax_steps(dm, dense, a.L, list_rows);
-  // 32 rows: four workgroups a compute unit where a block of rows is not in so many pieces that the join takes longer.
+  // 32 rows: four workgroups a compute unit where a block of rows is not in so many pieces that the join takes longer.  Calls, us, two / four, by
+  // blocks of rows: 8 of 131 072 tokens 113 / 125, 16 of 32 768 66.6 / 73.7, 32 109 / 113, 48 132 / 136; 64 of 8192 60.0 / 61.4, of 32 768 177 / 181, of
+  // 131 072 647 / 638, 128 of 8192 101 / 102, of 32 768 336 / 337, 256 of 4096 108 / 106, 512 of 16 384 660 / 653: from the line on within 3 % either way.
   const bool four = td.rows == 32 && units >= 64;
   const int per_cu = td.rows == 256 ? 1 : four ? 4 : 2, most = per_cu * cus < most_wgs(td.rows) ? per_cu * cus : most_wgs(td.rows), share = td.rows == 16 ? 4 : 1;
   const long long wgs = (steps + share - 1) / share;

@@ -4,9 +4,9 @@
 // groups above that bound are read, and of them the candidates above it go to LDS, in the order of their wavefronts; one
 // wavefront iterates to the exact root, then every wavefront adds up the value rows of its part of the support (V is read
 // where a weight is not zero, nowhere else).  A row too flat for LDS is gone through in its scores instead, evaluation by evaluation.
-// A chain of latencies (maxima, scores, root, lookups, values), several rows to a compute unit: 512 rows of 21 000 candidates 11.4 us, 1472 of
-// 131 000 24, 2008 of 512 18.8.  Rows with thousands of keys in their support are gone through in their scores: 1024 rows of 131 000 keys,
-// alpha 1.25, about 600 us.
+// A chain of latencies (maxima, scores, root, lookups, values), several rows to a compute unit: 512 rows (tokens times query heads) of 21 000
+// keys 11.4 us, 1472 of 131 000 24.6, 8032 of 512 19.3.  Rows with thousands of keys in their support are gone through in their scores: alpha 1.25,
+// 131 000 keys, 256 rows 81 us by eight wavefronts each, 1024 rows 645 by four.
 #include "ekv_solve.h"
 #include "ekv_tree.h"
 
@@ -366,10 +366,13 @@ __global__ __launch_bounds__(64 * NW) void tree_solve_kernel(const TreeSolveArgs
 
 template <typename TQ, typename TC>
 static void launch_solve_T(const TreeSolveArgs& s, hipStream_t st) {
-  // Wavefronts to a row: one where short rows are many, four, or eight where rows are so few that a compute unit has two at most, which is for
-  // rows with large supports.  Calls, us, one / four / eight: lists of 512 keys, 2008 rows 39.3 / 63.2 / 99.9; 2048 rows of 1024 keys 52.8 /
-  // 65.2 / 86.5; 4096 of 4096 47.3 / 51.0 / 61.6, of 8192 90.5 / 91.5 / 99.7, of 32 768 190.5 / 190.7 / 205; 1472 of 131 072 329 / 329 / 336; 40 of 777
-  // 26.8 / 21.7 / 22.0, 512 of 20 972 72.0 / 63.4 / 63.3; alpha 1.25, 256 of 131 072 - / 602 / 161, 64 of 32 768 - / 67.6 / 54.8.
+  // Wavefronts to a row: one where short rows are many, four, or eight where rows are so few that a compute unit has two at most.  Calls, us, by the
+  // launch's rows, tokens times query heads.  One / four / eight: 8032 rows of lists of 512 keys 38.9 / 62.6 / 101, of 1024 60.0 / 84.2 / 122, of 4096
+  // 159 / 181 / 216, of 8000 273 / 292 / 329; 2144 of 4096 52.8 / 56.0 / 63.2; 1120 of 8000 54.7 / 50.1 / 55.8; 40 of 777 25.7 / 21.6 / 22.1.  Four /
+  // eight: 512 of 20 972 61.7 / 61.1; of 131 072 keys 256 rows 97.7 / 95.4, 608 138 / 136, 1472 353 / 361, 2048 273 / 279 (one sequence).  The line at
+  // two rows a compute unit is these rows'.  With large supports (alpha 1.25) eight win far beyond it: of 32 768 keys 64 rows 62.0 / 50.5, 608 162 /
+  // 84.7, 2048 260 / 214, of 131 072 keys 256 rows 595 / 158, 608 667 / 214, 1024 802 / 353, 2048 1077 / 575, but 4160 of 4096 150 / 182; that such rows are
+  // gone through in their scores at all is what costs them.
   if (s.rows > 8 * device_compute_units() && s.t.n_groups <= 128)
     hipLaunchKernelGGL((tree_solve_kernel<TQ, TC, 1>), dim3(s.rows), dim3(64), 0, st, s);
   else if (s.rows <= 2 * device_compute_units())
