@@ -441,8 +441,8 @@ ekv_status ekv_cache_append(const ekv_config* cfg, const ekv_cache_view* cache, 
  *   visible uint64 [max_tokens]: bit i of a row's word: it sees row i of its sequence.  For a tree the row itself and the rows that
  *           it follows, (1 << i) | visible[parent]; for a chain the rows up to it.  Any other mask is as good, none of them too.
  * max_tree (1 .. 64) and max_tokens size grids and workspaces.  max_tokens is also the number of rows of q and of the outputs.  start
- * ascends; what does not, or lies outside [0, max_tokens], gives undefined values, no undefined access.  Rows of no sequence, behind start[B] or
- * beyond max_tree, are neither read nor written. */
+ * ascends; what does not, or lies outside [0, max_tokens], gives undefined values, no undefined access.  Rows of no sequence, in front of start[0] (a
+ * call for the later part of a batch, start + b0), behind start[B] or beyond max_tree, are neither read nor written. */
 typedef struct {
   const void* k_new;
   const void* v_new;
